@@ -42,7 +42,7 @@ typedef enum {
     LSH_ERR_SCRATCH_TOO_SMALL = 7 /* lsh_decode_step_static: the step needs more than the built-in buffer */
 } lsh_status;
 
-typedef enum { LSH_F32 = 0, LSH_BF16 = 1 } lsh_dtype;
+typedef enum { LSH_F32 = 0, LSH_BF16 = 1, LSH_F16 = 2 /* logits, keys, values and queries; not embeddings */ } lsh_dtype;
 
 /* The paper's hash hyper-parameters {K, u, W} (text after Eq. 8) plus the layout of E. */
 typedef struct {
@@ -172,6 +172,143 @@ lsh_status lsh_beam_advance(const lsh_beam_params* bp, int32_t step, const int32
 lsh_status lsh_beam_backtrace(const lsh_beam_params* bp, int32_t n_steps, const int32_t* backptr_dev,
                               const int32_t* words_dev, const float* scores_dev, int32_t* tokens_dev,
                               int32_t* length_dev, float* best_score_dev, void* hip_stream);
+
+/* ---- selection from logits that the caller's model made ------------------------------------- */
+
+typedef struct {
+    int32_t S;          /* sentences in the call, S * B <= 2^20                                        */
+    int32_t B;          /* beams per sentence, 1 .. 256                                                */
+    int32_t N;          /* results per sentence, 1 .. 256 (B for a step of a search, more to look at)  */
+    int32_t V;          /* words, 1 .. 2^24                                                            */
+    int32_t dtype;      /* lsh_dtype of the logits                                                     */
+    int64_t ld;         /* row pitch of the logits in elements, >= V                                   */
+    int64_t allowed_ld; /* row pitch of the allowed words in 32-bit words, >= ceil(V / 32), or 0: one
+                           row for all                                                                 */
+} lsh_select_params;
+
+/* Bytes of workspace lsh_beam_select needs (0 on invalid arguments; dtype and pitches do not matter). */
+size_t lsh_select_workspace_bytes(const lsh_select_params* p);
+
+/* Beam expansion from dense logits: what lsh_decode_step does behind its product, for a model with an output layer of its own.
+ *   logits_dev       [S*B, ld] of p->dtype, sentence-major; rows may begin at any element.
+ *   beam_scores_dev  fp32 [S*B]: accumulated log-probability of each beam (-inf = dead beam).
+ *   allowed_dev      NULL, or bits: bit w % 32 of 32-bit word w / 32 of a row says that word w may follow.  A word that may not
+ *                    counts as a logit of -inf, whatever stands there (a NaN too).
+ *   workspace_dev    as for lsh_decode_step.
+ * log-probability = logit - log sum exp over the row's allowed words; score = beam score + log-probability, both in 64 bits; per
+ * sentence the N best pairs, best first, equal scores ordered by lower beam then lower word.  Pairs whose score is not finite
+ * in fp32 are none: a row with a NaN or +inf among its allowed logits, or with no allowed word, has no pair.
+ *   out_beam_dev / out_word_dev / out_score_dev   [S, N]; behind the last pair (-1, -1, -inf).  With N = B as
+ *                    lsh_beam_advance takes them.
+ *   out_lse_dev      fp32 [S*B], or NULL: log sum exp of each row (-inf without an allowed word).
+ * Asynchronous on the stream, allocates nothing; the same inputs give the same outputs bit for bit. */
+lsh_status lsh_beam_select(const lsh_select_params* p, const void* logits_dev, const float* beam_scores_dev,
+                           const uint32_t* allowed_dev, void* workspace_dev, size_t workspace_bytes,
+                           int32_t* out_beam_dev, int32_t* out_word_dev, float* out_score_dev, float* out_lse_dev,
+                           void* hip_stream);
+
+/* ---- a paged cache of keys and values in 8 bits ----------------------------------------------
+ *
+ * State of a decoder that grows by a token per step, and that lsh_beam_advance therefore cannot move.  Rows (S sentences of B
+ * beams; B = 1 for unrelated rows) own no memory: a row's block table names the blocks of a pool that hold its tokens, position
+ * p in block p / block of the table.  Per step:
+ *   lsh_cache_advance    rows continue their parents' tables, blocks are taken for new tokens, every new token gets a slot
+ *   lsh_cache_write      for each layer: keys and values of the new tokens go to their slots
+ *   lsh_cache_attention  for each layer: queries over the rows' tokens
+ * One set of tables serves all layers; a layer has a pool. */
+
+typedef struct {
+    int32_t S, B;       /* as in lsh_step_params; rows R = S * B <= 2^20                               */
+    int32_t n_blocks;   /* blocks of a pool, 1 .. 2^24; n_blocks * block < 2^31                        */
+    int32_t block;      /* tokens of a block: 16, 32, 64 or 128                                        */
+    int32_t max_blocks; /* columns of the block tables, 1 .. 2^20                                      */
+    int32_t n_heads;    /* heads of keys and values, 1 .. 65535                                        */
+    int32_t head_dim;   /* values of a head: a multiple of 16, 16 .. 256                               */
+} lsh_cache_params;
+
+/* Device memory of a layer, caller-owned, k and v at multiples of 16 bytes.  A code is an OCP e4m3 number, a value is
+ * code * scale.
+ *   k        [n_blocks, n_heads, head_dim / 16, block, 16] codes: 16 of a token's values, then the next token's
+ *   v        [n_blocks, n_heads, block / 16, head_dim, 16] codes: a value of 16 tokens, then the next value
+ *   k_scale, v_scale   fp32 [n_blocks, n_heads] */
+typedef struct {
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;
+    float* v_scale;
+} lsh_cache_pool;
+
+/* Where the values of row r, token t, head h begin: r * row + t * token + h * head elements of `dtype` behind the array's
+ * address.  A head's values lie side by side. */
+typedef struct {
+    int32_t dtype;
+    int64_t row, token, head;
+} lsh_rows;
+
+/* Bytes of workspace lsh_cache_advance needs (0 on invalid arguments). */
+size_t lsh_cache_workspace_bytes(const lsh_cache_params* c);
+
+/* The tables after a step.  Row r = s*B + b continues the tokens of row s*B + parents[r] (a parent outside 0 .. B-1: none) and
+ * gets n_new[r] tokens more.
+ *   T                 most new tokens of a row in this call
+ *   parents_dev       int32 [S, B] (out_beam of a selection), or NULL: every row continues itself
+ *   n_new_dev         int32 [R], each 0 .. T, or NULL: T for rows with a parent, 0 for rows without
+ *   tables_in_dev, lengths_in_dev     int32 [R, max_blocks] and [R]; only the entries that a row's length needs are read
+ *   tables_out_dev, lengths_out_dev   the same afterwards, entries behind the row's last block -1; not the input arrays
+ *   slots_dev         int32 [R, T]: block * (tokens of a block) + place of every new token, -1 behind the row's last
+ *   copy_from_dev     int32 [R]: -1, or a row that writes on a block that another row continues too has a block of its own
+ *                     instead, which lsh_cache_write begins as a copy of this one
+ *   shared_dev        int32 [S], or NULL: how many leading blocks, whole ones, all rows of the sentence that have tokens
+ *                     have in common
+ *   status_dev        int32 [2]: blocks missing in the pool; rows that ask for more than T or their table holds.  If one of
+ *                     them is not 0, no row gets new tokens (slots and copy_from -1); rows have their parents' tables.
+ * Free are the blocks that no row continues with and no copy begins from: rows that end need no release.  Free blocks are
+ * taken lowest first, by rows in order.
+ * Blocks of different sentences must be different.  Asynchronous on the stream, allocates nothing. */
+lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t* parents_dev, const int32_t* n_new_dev,
+                             const int32_t* tables_in_dev, const int32_t* lengths_in_dev, int32_t* tables_out_dev,
+                             int32_t* lengths_out_dev, int32_t* slots_dev, int32_t* copy_from_dev, int32_t* shared_dev,
+                             int32_t* status_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Keys and values of new tokens (fp32, bf16 or fp16; both of one type) into a layer's pool.
+ *   slots_dev      int32 [R, T] as lsh_cache_advance leaves them: a row's tokens have consecutive positions, -1 behind the
+ *                  last.  Slots that no block of the pool has, and what follows a gap, are left out.
+ *   copy_from_dev  int32 [R], or NULL: the block that the row's first block begins as a copy of
+ * A block's scale (of each head, of keys and of values) is the smallest power of two, 2^-126 at least, with which its largest
+ * finite value is at most 448, 0 for a block of zeros, and never less than its earlier tokens'; codes are rounded to nearest
+ * even, NaN and infinities become the code NaN.  Where the scale grows, the block's earlier codes are rounded once more.
+ * What lies behind the new tokens in a block stays.  No two rows may have slots in one block. */
+lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool, int32_t T, const void* k_dev, const lsh_rows* k_rows,
+                           const void* v_dev, const lsh_rows* v_rows, const int32_t* slots_dev,
+                           const int32_t* copy_from_dev, void* hip_stream);
+
+typedef struct {
+    int32_t T;          /* queries of a row: its last tokens                                           */
+    int32_t n_heads;    /* heads of queries, a multiple of the cache's: head h reads head
+                           h / (n_heads / cache heads) of it                                           */
+    int32_t causal;     /* 1: a token sees the positions up to its own; 0: all of the row              */
+    int32_t window;     /* > 0 (causal only): ... and of those the last `window`                       */
+    float scale;        /* > 0; of the products, usually 1 / sqrt(head_dim)                            */
+} lsh_attention_params;
+
+/* Bytes of workspace lsh_cache_attention needs (0 on invalid arguments). */
+size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p);
+
+/* out = softmax(scale * q k^T over the positions a token sees) v.
+ *   q_dev        [R, T, n_heads, head_dim] with pitches q_rows; out_dev the same with out_rows, of the same type
+ *   tables_dev, lengths_dev   as lsh_cache_advance leaves them (a row's new tokens count); blocks outside the pool are not seen
+ *   n_new_dev    int32 [R], or NULL: T.  Token t < n of a row is at position lengths[r] - n + t; what stands in out and lse
+ *                behind a row's n-th token stays
+ *   shared_dev   int32 [S] as lsh_cache_advance leaves them, or NULL: these leading blocks are read once for all beams
+ *   lse_dev      fp32 [R, T, n_heads], or NULL: log sum exp of the scaled products
+ * A token that sees nothing gets zeros and an lse of -inf.  What a token does not see does not reach its result, a NaN neither.
+ * Products and sums are fp32 (queries of 16 bits: the probabilities are rounded to bf16 for bf16, kept to 16 bits for fp16).
+ * Asynchronous on the stream, allocates nothing; the same inputs give the same outputs bit for bit. */
+lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
+                               const lsh_rows* q_rows, const int32_t* tables_dev, const int32_t* lengths_dev,
+                               const int32_t* n_new_dev, const int32_t* shared_dev, void* workspace_dev,
+                               size_t workspace_bytes, void* out_dev, const lsh_rows* out_rows, float* lse_dev,
+                               void* hip_stream);
 
 /* ---- inspection (synchronous device-to-host copies; never on the timed path) ---------------- */
 

@@ -10,7 +10,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "liblshbeam.so")
 
-LSH_F32, LSH_BF16 = 0, 1
+LSH_F32, LSH_BF16, LSH_F16 = 0, 1, 2
 NUM_KERNELS = 5
 
 # every symbol include/lshbeam.h declares
@@ -22,6 +22,8 @@ EXPORTED_SYMBOLS = (
     "lsh_status_string", "lsh_step_is_fused", "lsh_debug_build_info", "lsh_beam_advance",
     "lsh_beam_backtrace", "lsh_set_option", "lsh_get_option", "lsh_decode_step_static",
     "lsh_static_scratch_bytes", "lsh_debug_counts", "lsh_release_kept",
+    "lsh_select_workspace_bytes", "lsh_beam_select", "lsh_cache_workspace_bytes", "lsh_cache_advance", "lsh_cache_write",
+    "lsh_attention_workspace_bytes", "lsh_cache_attention",
 )
 
 OPTION_AUTO = -1
@@ -50,6 +52,29 @@ class BeamParams(ctypes.Structure):
 class StepParams(ctypes.Structure):
     _fields_ = [("S", ctypes.c_int32), ("B", ctypes.c_int32), ("T", ctypes.c_int32),
                 ("threshold", ctypes.c_int32), ("full_vocab", ctypes.c_int32)]
+
+
+class SelectParams(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int32), ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("ld", ctypes.c_int64), ("allowed_ld", ctypes.c_int64)]
+
+
+class CacheParams(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int32), ("B", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class AttentionParams(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class _PoolPointers(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("row", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 _lib = None
@@ -108,6 +133,18 @@ def load_library():
     lib.lsh_step_is_fused.argtypes = [vp, ctypes.POINTER(StepParams)]
     lib.lsh_kernel_name.argtypes = [i32]
     lib.lsh_kernel_name.restype = ctypes.c_char_p
+    lib.lsh_select_workspace_bytes.argtypes = [ctypes.POINTER(SelectParams)]
+    lib.lsh_select_workspace_bytes.restype = sz
+    lib.lsh_beam_select.argtypes = [ctypes.POINTER(SelectParams), vp, vp, vp, vp, sz, vp, vp, vp, vp, vp]
+    lib.lsh_cache_workspace_bytes.argtypes = [ctypes.POINTER(CacheParams)]
+    lib.lsh_cache_workspace_bytes.restype = sz
+    lib.lsh_cache_advance.argtypes = [ctypes.POINTER(CacheParams), i32] + [vp] * 11 + [sz, vp]
+    rows = ctypes.POINTER(_Rows)
+    lib.lsh_cache_write.argtypes = [ctypes.POINTER(CacheParams), ctypes.POINTER(_PoolPointers), i32, vp, rows, vp, rows, vp, vp, vp]
+    lib.lsh_attention_workspace_bytes.argtypes = [ctypes.POINTER(CacheParams), ctypes.POINTER(AttentionParams)]
+    lib.lsh_attention_workspace_bytes.restype = sz
+    lib.lsh_cache_attention.argtypes = [ctypes.POINTER(CacheParams), ctypes.POINTER(_PoolPointers), ctypes.POINTER(AttentionParams), vp,
+                                        rows, vp, vp, vp, vp, vp, sz, vp, rows, vp, vp]
     lib.lsh_status_string.argtypes = [ctypes.c_int]
     lib.lsh_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -485,3 +522,169 @@ def beam_backtrace(hist: BeamHistory, n_steps: int, stream=None):
                                              tokens.data_ptr(), length.data_ptr(), score.data_ptr(),
                                              _stream_ptr(stream)), "lsh_beam_backtrace")
     return tokens, length, score
+
+
+# ---- selection from the caller's logits, and a paged cache in 8 bits -----------------------------
+
+_types = None
+
+
+def _lsh_dtype(x, name) -> int:
+    """lsh_dtype of a tensor of logits, keys, values or queries."""
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: LSH_F32, torch.bfloat16: LSH_BF16, torch.float16: LSH_F16}
+    t = _types.get(x.dtype)
+    if t is None:
+        raise ValueError(f"{name}: dtype {x.dtype} not in {tuple(_types)}")
+    return t
+
+
+def _ints(x, name, shape, optional=False):
+    """Device address of a contiguous int32 tensor of this shape (any, if None)."""
+    import torch
+    if x is None and optional:
+        return None
+    _require_cuda(x, name, (torch.int32,))
+    if shape is not None and x.numel() != shape:
+        raise ValueError(f"{name} must have {shape} elements, has {x.numel()}")
+    return x.data_ptr()
+
+
+def _floats(x, name, n):
+    import torch
+    _require_cuda(x, name, (torch.float32,))
+    if x.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, has {x.numel()}")
+    return x.data_ptr()
+
+
+def _same_device(first, *others):
+    """All on the current device: the library launches there, and has no handle that says where it was made."""
+    import torch
+    at = first.get_device()
+    if at != torch.cuda.current_device() or any(x is not None and x.get_device() != at for x in others):
+        raise ValueError("all tensors must be on the current device")
+
+
+def select_params(S: int, B: int, V: int, N: Optional[int] = None) -> SelectParams:
+    """N: results per sentence, B of them unless given."""
+    return SelectParams(S, B, B if N is None else N, V, LSH_F32, V, 0)
+
+
+def select_workspace_bytes(sp: SelectParams) -> int:
+    return int(load_library().lsh_select_workspace_bytes(ctypes.byref(sp)))
+
+
+def beam_select(sp: SelectParams, logits, beam_scores, workspace, out_beam, out_word, out_score, allowed=None, lse=None,
+                stream=None):
+    """lsh_beam_select: asynchronous on `stream` (default: torch's current stream).  logits: [S*B, V], float32, bfloat16 or
+    float16, unit stride in a row; allowed: int32 bits [S*B, >= ceil(V / 32)], or one row of them for all."""
+    R, n = sp.S * sp.B, sp.S * sp.N
+    if not logits.is_cuda or logits.dim() != 2 or tuple(logits.shape) != (R, sp.V) or (sp.V > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a device tensor [S*B, V] with contiguous rows")
+    _same_device(logits, beam_scores, workspace, out_beam, out_word, out_score, allowed, lse)
+    ld = logits.stride(0) if R > 1 else sp.V
+    mask, mask_ld = None, 0
+    if allowed is not None:
+        import torch
+        words = (sp.V + 31) // 32
+        if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.shape[0] not in (1, R) or allowed.shape[1] < words or (
+                allowed.shape[1] > 1 and allowed.stride(1) != 1):
+            raise ValueError("allowed must be int32 [S*B or 1, >= ceil(V / 32)] with contiguous rows")
+        mask, mask_ld = allowed.data_ptr(), allowed.stride(0) if allowed.shape[0] > 1 else 0
+    p = SelectParams(sp.S, sp.B, sp.N, sp.V, _lsh_dtype(logits, "logits"), ld, mask_ld)
+    _check(load_library().lsh_beam_select(
+        ctypes.byref(p), logits.data_ptr(), _floats(beam_scores, "beam_scores", R), mask, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _ints(out_beam, "out_beam", n), _ints(out_word, "out_word", n),
+        _floats(out_score, "out_score", n), None if lse is None else _floats(lse, "lse", R), _stream_ptr(stream)), "lsh_beam_select")
+
+
+def cache_params(S: int, B: int, n_blocks: int, block: int, max_blocks: int, n_heads: int, head_dim: int) -> CacheParams:
+    return CacheParams(S, B, n_blocks, block, max_blocks, n_heads, head_dim)
+
+
+class CachePool:
+    """Caller-owned device memory of one layer of a cache (torch is only the allocator): codes as uint8 k [n_blocks, heads,
+    head_dim / 16, block, 16] and v [n_blocks, heads, block / 16, head_dim, 16], scales as float32 [n_blocks, heads].  Tensors
+    that are handed in are kept and used as they are."""
+
+    def __init__(self, cp: CacheParams, k=None, v=None, k_scale=None, v_scale=None):
+        import torch
+        shapes = ((cp.n_blocks, cp.n_heads, cp.head_dim // 16, cp.block, 16), (cp.n_blocks, cp.n_heads, cp.block // 16, cp.head_dim, 16),
+                  (cp.n_blocks, cp.n_heads), (cp.n_blocks, cp.n_heads))
+        given = []
+        for x, shape, name in zip((k, v, k_scale, v_scale), shapes, ("k", "v", "k_scale", "v_scale")):
+            dtype = torch.uint8 if name in ("k", "v") else torch.float32
+            if x is None:
+                x = torch.zeros(shape, dtype=dtype, device="cuda")
+            _require_cuda(x, name, (dtype,))
+            if tuple(x.shape) != shape:
+                raise ValueError(f"{name} must be {shape}, is {tuple(x.shape)}")
+            given.append(x)
+        self.k, self.v, self.k_scale, self.v_scale = given
+        self._shape = (cp.n_blocks, cp.block, cp.n_heads, cp.head_dim)
+        self._pointers = _PoolPointers(*[x.data_ptr() for x in given])
+
+    def _of(self, cp: CacheParams):
+        if (cp.n_blocks, cp.block, cp.n_heads, cp.head_dim) != self._shape:
+            raise ValueError("the pool was made for other cache parameters")
+        return ctypes.byref(self._pointers)
+
+
+def cache_workspace_bytes(cp: CacheParams) -> int:
+    return int(load_library().lsh_cache_workspace_bytes(ctypes.byref(cp)))
+
+
+def cache_advance(cp: CacheParams, T: int, tables_in, lengths_in, tables_out, lengths_out, slots, copy_from, shared, status, workspace,
+                  parents=None, n_new=None, stream=None):
+    """lsh_cache_advance: all arrays int32; shared, parents and n_new may be None."""
+    R = cp.S * cp.B
+    _same_device(tables_in, lengths_in, tables_out, lengths_out, slots, copy_from, shared, status, workspace, parents, n_new)
+    _check(load_library().lsh_cache_advance(
+        ctypes.byref(cp), T, _ints(parents, "parents", R, True), _ints(n_new, "n_new", R, True),
+        _ints(tables_in, "tables_in", R * cp.max_blocks), _ints(lengths_in, "lengths_in", R),
+        _ints(tables_out, "tables_out", R * cp.max_blocks), _ints(lengths_out, "lengths_out", R), _ints(slots, "slots", R * T),
+        _ints(copy_from, "copy_from", R), _ints(shared, "shared", cp.S, True), _ints(status, "status", 2), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "lsh_cache_advance")
+
+
+def _rows(x, name, shape):
+    """lsh_rows of a tensor [R, T, heads, head_dim] with any pitches."""
+    if not x.is_cuda or tuple(x.shape) != shape or x.stride(3) != 1:
+        raise ValueError(f"{name} must be a device tensor {shape} with contiguous heads")
+    return _Rows(_lsh_dtype(x, name), x.stride(0), x.stride(1), x.stride(2))
+
+
+def cache_write(cp: CacheParams, pool: CachePool, k, v, slots, copy_from=None, stream=None):
+    """lsh_cache_write: k, v [S*B, T, n_heads, head_dim] (views into a fused projection, say), slots int32 [S*B, T]."""
+    R, T = cp.S * cp.B, int(k.shape[1]) if k.dim() == 4 else 0
+    shape = (R, T, cp.n_heads, cp.head_dim)
+    _same_device(k, v, slots, copy_from, pool.k)
+    kr, vr = _rows(k, "k", shape), _rows(v, "v", shape)
+    _check(load_library().lsh_cache_write(
+        ctypes.byref(cp), pool._of(cp), T, k.data_ptr(), ctypes.byref(kr), v.data_ptr(), ctypes.byref(vr), _ints(slots, "slots", R * T),
+        _ints(copy_from, "copy_from", R, True), _stream_ptr(stream)), "lsh_cache_write")
+
+
+def attention_params(T: int, n_heads: int, scale: float, causal: bool = True, window: int = 0) -> AttentionParams:
+    return AttentionParams(T, n_heads, 1 if causal else 0, window, scale)
+
+
+def attention_workspace_bytes(cp: CacheParams, ap: AttentionParams) -> int:
+    return int(load_library().lsh_attention_workspace_bytes(ctypes.byref(cp), ctypes.byref(ap)))
+
+
+def cache_attention(cp: CacheParams, ap: AttentionParams, pool: CachePool, q, tables, lengths, workspace, out, shared=None, n_new=None,
+                    lse=None, stream=None):
+    """lsh_cache_attention: q, out [S*B, T, n_heads, head_dim] of one type, lse float32 [S*B, T, n_heads] or None."""
+    R = cp.S * cp.B
+    shape = (R, ap.T, ap.n_heads, cp.head_dim)
+    _same_device(q, out, tables, lengths, workspace, shared, n_new, lse, pool.k)
+    qr, orow = _rows(q, "q", shape), _rows(out, "out", shape)
+    _check(load_library().lsh_cache_attention(
+        ctypes.byref(cp), pool._of(cp), ctypes.byref(ap), q.data_ptr(), ctypes.byref(qr), _ints(tables, "tables", R * cp.max_blocks),
+        _ints(lengths, "lengths", R), _ints(n_new, "n_new", R, True), _ints(shared, "shared", cp.S, True), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), out.data_ptr(), ctypes.byref(orow),
+        None if lse is None else _floats(lse, "lse", R * ap.T * ap.n_heads), _stream_ptr(stream)), "lsh_cache_attention")

@@ -6,7 +6,8 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "lshbeam.hip")
+SRC = os.path.join(HERE, "csrc", "lshbeam.hip")              # the decode step and the tables it looks up
+DECODER_SRC = os.path.join(HERE, "csrc", "lshdecoder.hip")   # what stands around a decoder with a cache
 LIB = os.path.join(HERE, "liblshbeam.so")
 
 HIPCC_FLAGS = [
@@ -26,7 +27,7 @@ def sources():
 def build(verbose: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", tmp, SRC]
+    cmd = [hipcc] + HIPCC_FLAGS + ["-o", tmp, SRC, DECODER_SRC]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

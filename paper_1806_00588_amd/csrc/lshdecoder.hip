@@ -1,0 +1,219 @@
+// C ABI of what stands around a decoder that makes its own logits and keeps a paged cache (see include/lshbeam.h): selection
+// from dense logits, block tables, cache writes, attention.  Host side: argument validation, the choice of kernels, launches.
+// A translation unit of its own: its kernels are a code object of their own, so the places of the decode step's kernels in
+// theirs (short kernels' times go by them) stay as they are.
+#ifdef LSHBEAM_TRACE   // (the phase timestamps belong to the decode step's kernels)
+#undef LSHBEAM_TRACE
+#endif
+#include "../../include/lshbeam.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "beam_select.h"
+#include "cache_attention.h"
+#include "cache_tables.h"
+#include "cache_write.h"
+
+using namespace lshbeam;
+
+namespace {
+
+constexpr int64_t kMaxRows = 1 << 20;
+constexpr int64_t kMaxGrid = (1 << 24) - 1;   // workgroups of 256 threads: fewer than 2^32 threads
+constexpr int kMaxWords = 1 << 24, kMaxBeams = 256;
+constexpr int kMaxBlocks = 1 << 24, kMaxColumns = 1 << 20;
+
+size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+lsh_status launched() { return hipGetLastError() == hipSuccess ? LSH_OK : LSH_ERR_HIP; }
+
+template <typename F> void for_type(int32_t dtype, F f) {   // f(std::integral_constant<int, kType...>)
+    if (dtype == LSH_F32) f(std::integral_constant<int, kTypeF32>());
+    else if (dtype == LSH_BF16) f(std::integral_constant<int, kTypeBf16>());
+    else f(std::integral_constant<int, kTypeF16>());
+}
+bool type_ok(int32_t dtype) { return dtype == LSH_F32 || dtype == LSH_BF16 || dtype == LSH_F16; }
+size_t type_bytes(int32_t dtype) { return dtype == LSH_F32 ? 4 : 2; }
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// ---- selection ----------------------------------------------------------------------------------
+
+bool select_ok(const lsh_select_params* p) {
+    return p && p->S >= 1 && p->B >= 1 && p->B <= kMaxBeams && p->N >= 1 && p->N <= kMaxBeams && p->V >= 1 && p->V <= kMaxWords &&
+           (int64_t)p->S * p->B <= kMaxRows && (int64_t)p->S * p->N <= kMaxRows;
+}
+int64_t row_pieces(const lsh_select_params* p) { return ceil_div(p->V, kSelPiece); }
+bool select_is_small(const lsh_select_params* p) { return p->B * row_pieces(p) <= kSelSmall; }
+
+size_t select_bytes(const lsh_select_params* p, size_t* tiles_bytes) {
+    const size_t R = (size_t)p->S * p->B;
+    *tiles_bytes = round_up(R * (size_t)ceil_div(p->V, kSelTile) * sizeof(float));
+    return *tiles_bytes + round_up(R * (size_t)ceil_div(row_pieces(p), kSelBatch) * sizeof(SelPart));
+}
+
+// ---- cache --------------------------------------------------------------------------------------
+
+bool cache_ok(const lsh_cache_params* c) {
+    return c && c->S >= 1 && c->B >= 1 && c->B <= kMaxBeams && (int64_t)c->S * c->B <= kMaxRows && c->n_blocks >= 1 && c->n_blocks <= kMaxBlocks &&
+           (c->block == 16 || c->block == 32 || c->block == 64 || c->block == 128) && (int64_t)c->n_blocks * c->block <= INT32_MAX &&
+           c->max_blocks >= 1 && c->max_blocks <= kMaxColumns && c->n_heads >= 1 && c->n_heads <= 65535 && c->head_dim >= 16 &&
+           c->head_dim <= 256 && c->head_dim % 16 == 0;
+}
+bool pool_ok(const lsh_cache_pool* p) {
+    return p && p->k && p->v && p->k_scale && p->v_scale && aligned(p->k, 16) && aligned(p->v, 16);
+}
+bool pitch_ok(const lsh_rows* x, int32_t head_dim) {
+    return x && type_ok(x->dtype) && x->row >= 0 && x->token >= 0 && x->head >= 0 && head_dim > 0;
+}
+
+struct TablesRoom { size_t plan, base, free_ids, used, bytes; };
+TablesRoom tables_room(const lsh_cache_params* c) {
+    const size_t R = (size_t)c->S * c->B;
+    TablesRoom w{};
+    w.base = round_up(R * sizeof(RowPlan));
+    w.free_ids = w.base + round_up(R * sizeof(int32_t));
+    w.used = w.free_ids + round_up((size_t)c->n_blocks * sizeof(int32_t));
+    w.bytes = w.used + round_up((size_t)c->n_blocks);
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lsh_select_workspace_bytes(const lsh_select_params* p) {
+    size_t tiles = 0;
+    return select_ok(p) ? select_bytes(p, &tiles) : 0;
+}
+
+lsh_status lsh_beam_select(const lsh_select_params* p, const void* logits_dev, const float* beam_scores_dev,
+                           const uint32_t* allowed_dev, void* workspace_dev, size_t workspace_bytes, int32_t* out_beam_dev,
+                           int32_t* out_word_dev, float* out_score_dev, float* out_lse_dev, void* hip_stream) {
+    if (!select_ok(p) || !type_ok(p->dtype) || p->ld < p->V || !logits_dev || !beam_scores_dev || !out_beam_dev || !out_word_dev ||
+        !out_score_dev || !aligned(logits_dev, type_bytes(p->dtype)))
+        return LSH_ERR_INVALID_ARG;
+    if (allowed_dev && p->allowed_ld != 0 && p->allowed_ld < (p->V + 31) / 32) return LSH_ERR_INVALID_ARG;
+    const bool small = select_is_small(p);
+    size_t tiles_bytes = 0;
+    if (!workspace_dev || !aligned(workspace_dev, 256)) return LSH_ERR_INVALID_ARG;
+    if (workspace_bytes < select_bytes(p, &tiles_bytes)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    const int64_t R = (int64_t)p->S * p->B, pieces = row_pieces(p);
+    SelArgs a{};
+    a.x = logits_dev; a.ld = p->ld;
+    a.allowed = reinterpret_cast<const uint8_t*>(allowed_dev); a.allowed_pitch = 4 * p->allowed_ld;
+    a.scores = beam_scores_dev;
+    a.V = p->V; a.B = p->B; a.N = p->N;
+    a.tiles = (int)ceil_div(p->V, kSelTile);
+    a.tile_max = static_cast<float*>(workspace_dev);
+    a.part = reinterpret_cast<SelPart*>(static_cast<char*>(workspace_dev) + tiles_bytes);
+    a.out_beam = out_beam_dev; a.out_word = out_word_dev; a.out_score = out_score_dev; a.out_lse = out_lse_dev;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (small) {
+        for_type(p->dtype, [&](auto type) {
+            hipLaunchKernelGGL(k_select_small<decltype(type)::value>, dim3((unsigned)p->S), dim3(kSelThreads), 0, st, a);
+        });
+        return launched();
+    }
+    // a wave takes four pieces, more where there are more waves than the chip holds at a time
+    a.pieces = kSelBatch;
+    while (a.pieces < 4 * kSelBatch && R * ceil_div(pieces, 2 * a.pieces) >= 256 * 32) a.pieces *= 2;
+    a.parts = (int)ceil_div(pieces, a.pieces);
+    const int64_t grid = R * ceil_div(a.parts, 4);
+    if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    for_type(p->dtype, [&](auto type) {
+        hipLaunchKernelGGL(k_select_tiles<decltype(type)::value>, dim3((unsigned)grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_select_words<decltype(type)::value>, dim3((unsigned)p->S), dim3(kSelThreads), 0, st, a);
+    });
+    return launched();
+}
+
+size_t lsh_cache_workspace_bytes(const lsh_cache_params* c) { return cache_ok(c) ? tables_room(c).bytes : 0; }
+
+lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t* parents_dev, const int32_t* n_new_dev,
+                             const int32_t* tables_in_dev, const int32_t* lengths_in_dev, int32_t* tables_out_dev,
+                             int32_t* lengths_out_dev, int32_t* slots_dev, int32_t* copy_from_dev, int32_t* shared_dev,
+                             int32_t* status_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (!cache_ok(c) || T < 1 || !tables_in_dev || !lengths_in_dev || !tables_out_dev || !lengths_out_dev || !slots_dev || !copy_from_dev ||
+        !status_dev || tables_in_dev == tables_out_dev || lengths_in_dev == lengths_out_dev || !workspace_dev || !aligned(workspace_dev, 256))
+        return LSH_ERR_INVALID_ARG;
+    const TablesRoom w = tables_room(c);
+    if (workspace_bytes < w.bytes) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    TablesArgs a{};
+    a.S = c->S; a.B = c->B; a.T = T; a.n_blocks = c->n_blocks; a.block = c->block; a.width = c->max_blocks;
+    a.parents = parents_dev; a.n_new = n_new_dev; a.tables_in = tables_in_dev; a.lengths_in = lengths_in_dev;
+    a.tables_out = tables_out_dev; a.lengths_out = lengths_out_dev; a.slots = slots_dev; a.copy_from = copy_from_dev;
+    a.shared = shared_dev; a.status = status_dev;
+    char* room = static_cast<char*>(workspace_dev);
+    a.plan = reinterpret_cast<RowPlan*>(room);
+    a.base = reinterpret_cast<int32_t*>(room + w.base);
+    a.free_ids = reinterpret_cast<int32_t*>(room + w.free_ids);
+    a.used = reinterpret_cast<uint8_t*>(room + w.used);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const unsigned R = (unsigned)c->S * (unsigned)c->B;
+    hipLaunchKernelGGL(k_tables_clear, dim3((unsigned)ceil_div(c->n_blocks, 16 * 256)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_tables_rows, dim3(R), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_tables_take, dim3(1), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(k_tables_finish, dim3(R), dim3(256), 0, st, a);
+    return launched();
+}
+
+lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool, int32_t T, const void* k_dev, const lsh_rows* k_rows,
+                           const void* v_dev, const lsh_rows* v_rows, const int32_t* slots_dev, const int32_t* copy_from_dev, void* hip_stream) {
+    if (!cache_ok(c) || !pool_ok(pool) || T < 1 || !k_dev || !v_dev || !slots_dev || !pitch_ok(k_rows, c->head_dim) ||
+        !pitch_ok(v_rows, c->head_dim) || k_rows->dtype != v_rows->dtype || !aligned(k_dev, type_bytes(k_rows->dtype)) ||
+        !aligned(v_dev, type_bytes(v_rows->dtype)))
+        return LSH_ERR_INVALID_ARG;
+    WriteArgs a{};
+    a.T = T; a.n_blocks = c->n_blocks; a.block = c->block; a.heads = c->n_heads; a.D = c->head_dim;
+    a.per_row = (int)(((int64_t)T + c->block - 2) / c->block + 1);
+    a.k = k_dev; a.v = v_dev;
+    a.kp = RowsPitch{k_rows->row, k_rows->token, k_rows->head};
+    a.vp = RowsPitch{v_rows->row, v_rows->token, v_rows->head};
+    a.slots = slots_dev; a.copy_from = copy_from_dev;
+    a.codes_k = pool->k; a.codes_v = pool->v; a.scale_k = pool->k_scale; a.scale_v = pool->v_scale;
+    const int64_t grid = (int64_t)c->S * c->B * a.per_row;
+    if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    for_type(k_rows->dtype, [&](auto type) {
+        hipLaunchKernelGGL(k_cache_write<decltype(type)::value>, dim3((unsigned)grid, (unsigned)c->n_heads), dim3(256), 0,
+                           (hipStream_t)hip_stream, a);
+    });
+    return launched();
+}
+
+size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p) {
+    return cache_ok(c) && p && p->T >= 1 && p->n_heads >= 1 && p->n_heads % c->n_heads == 0 ? 256 : 0;
+}
+
+lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
+                               const lsh_rows* q_rows, const int32_t* tables_dev, const int32_t* lengths_dev, const int32_t* n_new_dev,
+                               const int32_t* shared_dev, void* workspace_dev, size_t workspace_bytes, void* out_dev,
+                               const lsh_rows* out_rows, float* lse_dev, void* hip_stream) {
+    if (!cache_ok(c) || !pool_ok(pool) || !p || p->T < 1 || p->n_heads < 1 || p->n_heads > 65535 || p->n_heads % c->n_heads != 0 ||
+        p->window < 0 || (p->window > 0 && !p->causal) || !(p->scale > 0.f && p->scale < INFINITY) || !q_dev || !tables_dev || !lengths_dev ||
+        !out_dev || !pitch_ok(q_rows, c->head_dim) || !pitch_ok(out_rows, c->head_dim) || q_rows->dtype != out_rows->dtype ||
+        !aligned(q_dev, type_bytes(q_rows->dtype)) || !aligned(out_dev, type_bytes(out_rows->dtype)) || !workspace_dev ||
+        !aligned(workspace_dev, 256))
+        return LSH_ERR_INVALID_ARG;
+    if (workspace_bytes < lsh_attention_workspace_bytes(c, p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    AttnArgs a{};
+    a.S = c->S; a.B = c->B; a.T = p->T; a.q_heads = p->n_heads; a.heads = c->n_heads; a.D = c->head_dim;
+    a.n_blocks = c->n_blocks; a.block = c->block; a.width = c->max_blocks;
+    a.causal = p->causal != 0; a.window = p->window; a.scale = p->scale;
+    a.q = q_dev; a.qp = RowsPitch{q_rows->row, q_rows->token, q_rows->head};
+    a.codes_k = pool->k; a.codes_v = pool->v; a.scale_k = pool->k_scale; a.scale_v = pool->v_scale;
+    a.tables = tables_dev; a.lengths = lengths_dev; a.n_new = n_new_dev; a.shared = shared_dev;
+    a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
+    a.lse = lse_dev;
+    const int64_t grid = (int64_t)c->S * c->B * p->T;
+    if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    for_type(q_rows->dtype, [&](auto type) {
+        hipLaunchKernelGGL(k_attention<decltype(type)::value>, dim3((unsigned)grid, (unsigned)p->n_heads), dim3(256), 0, (hipStream_t)hip_stream, a);
+    });
+    return launched();
+}
+
+}  // extern "C"

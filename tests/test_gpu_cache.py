@@ -1,0 +1,424 @@
+"""lsh_cache_write and lsh_cache_attention against oracle/decoder.py.
+
+Written codes and scales are whole decisions: equal bit for bit (a NaN's sign aside).  Attention, before its first run: a product of D
+terms in fp32 errs by (D + 2) 2^-24 times the sum of its terms' sizes; the probabilities by twice that and 2^-20 for exponentials and
+scales; n of them are added, weights of 2^-24 each; then each is rounded to what the matrix instructions take, at most 2^-8 (bf16
+queries), 2^-15 (fp16) or 2^-22 (fp32) of it; and the result is rounded to its own type, half a step: fp16's steps are 2^-24 below
+2^-14, so half of one is 2^-25 whatever the result.  All but that relative to the sum of p |v|."""
+import numpy as np
+import pytest
+
+import oracle.decoder as plain
+from gpu_harness import to_dev
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": "float32", "bf16": "bfloat16", "f16": "float16"}
+ROUNDING = {"f32": (2.0 ** -22, 2.0 ** -24), "bf16": (2.0 ** -8, 2.0 ** -8), "f16": (2.0 ** -15, 2.0 ** -11)}
+
+
+def ints(x):
+    return None if x is None else to_dev(np.ascontiguousarray(x, dtype=np.int32))
+
+
+def random_pool(rng, n_blocks, heads, block, D, size=1.0, nan=0.0):
+    k, v = (rng.integers(0, 256, (n_blocks, heads, block, D)).astype(np.uint8) for _ in range(2))
+    for x in (k, v):
+        x[x & 127 == 127] = 5
+        x[rng.random(x.shape) < nan] = 127
+    # a bell of values rather than all codes alike: halve exponents at random
+    for x in (k, v):
+        low = (rng.random(x.shape) < 0.7) & (x & 127 != 127)
+        x[low] = x[low] & 0xBF
+    scales = [(2.0 ** rng.integers(-8, -3, (n_blocks, heads))) * size for _ in range(2)]
+    return plain.Pool(k, v, *scales)
+
+
+def to_pool(cp, ref):
+    import torch
+    from paper_1806_00588_amd import binding
+    k, v = ref.layout()
+    return binding.CachePool(cp, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), to_dev(ref.k_scale.astype(np.float32)),
+                             to_dev(ref.v_scale.astype(np.float32)))
+
+
+def from_pool(pool):
+    return plain.Pool.from_layout(*[x.cpu().numpy() for x in (pool.k, pool.v, pool.k_scale, pool.v_scale)])
+
+
+def assert_same_pool(got, want):
+    for name in ("k", "v"):
+        a, b = getattr(got, name), getattr(want, name)
+        a, b = np.where(a & 127 == 127, 127, a), np.where(b & 127 == 127, 127, b)
+        assert np.array_equal(a, b), (name, np.argwhere(a != b)[:5])
+        assert np.array_equal(getattr(got, name + "_scale"), getattr(want, name + "_scale")), name
+
+
+# ---- write --------------------------------------------------------------------------------------
+
+def slots_of(rng, old, new, T, block, n_blocks, taken=()):
+    """Slots [R, T] of rows of `old` tokens that get `new`, in blocks of their own."""
+    R = len(old)
+    ids = iter([int(i) for i in rng.permutation(n_blocks) if i not in taken])
+    out = np.full((R, T), -1)
+    for r in range(R):
+        b = None
+        for i in range(new[r]):
+            p = old[r] + i
+            if b is None or p % block == 0:
+                b = next(ids)
+            out[r, i] = b * block + p % block
+    return out
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D,block,heads,T", [(16, 16, 1, 1), (64, 16, 2, 1), (128, 16, 8, 3), (80, 32, 3, 50), (256, 64, 2, 7), (48, 128, 1, 200)])
+def test_write_matches_plain(D, block, heads, T, dtype):
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(D + block + T)
+    R = 6
+    n_blocks = R * (T // block + 2) + 4
+    old = rng.integers(0, 3 * block, R)
+    old[0], old[1] = 0, block - 1
+    new = rng.integers(0, T + 1, R)
+    new[:3] = T
+    new[3] = 0
+    ref = random_pool(rng, n_blocks, heads, block, D)
+    slots = slots_of(rng, old, new, T, block, n_blocks - 2, )
+    copies = np.full(R, -1)
+    copies[[1, 4]] = n_blocks - 1, n_blocks - 2
+    kv = (rng.standard_normal((R, T, 2, heads, D)) * np.exp(2 * rng.standard_normal((R, T, 2, heads, 1)))).astype(np.float32)
+    kv = torch.from_numpy(kv).to(getattr(torch, TYPES[dtype]))
+    cp = binding.cache_params(R, 1, n_blocks, block, 4, heads, D)
+    pool = to_pool(cp, ref)
+    kvd = kv.cuda()
+    binding.cache_write(cp, pool, kvd[:, :, 0], kvd[:, :, 1], ints(slots), ints(copies))
+    torch.cuda.synchronize()
+    plain.write(ref, kv[:, :, 0].double().numpy(), kv[:, :, 1].double().numpy(), slots, copies)
+    assert_same_pool(from_pool(pool), ref)
+
+
+def test_write_special_values():
+    """Zeros, values at the border of a scale, infinities and NaN, the smallest and the largest numbers; then a second token after each."""
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(1)
+    R, T, heads, D, block = 9, 2, 1, 32, 16
+    x = rng.standard_normal((R, T, 2, heads, D)).astype(np.float32)
+    x[0] = 0.0
+    x[1, 0] = 0.0
+    x[2, :, :, :, 3] = 448.0 * 4
+    x[2, :, :, :, 4:] = 1.0
+    x[3, :, :, :, 3] = np.nextafter(np.float32(448.0), np.float32(500))
+    x[4, 0, :, :, 5], x[4, 1, :, :, 6] = np.inf, np.nan
+    x[5] = np.nan
+    x[6, :] *= 1e-42
+    x[7, :, :, :, 0] = np.finfo(np.float32).max
+    x[8, 0] *= 1e-6
+    x[8, 1] *= 1e4
+    cp = binding.cache_params(R, 1, R, block, 4, heads, D)
+    ref = random_pool(rng, R, heads, block, D)
+    pool = to_pool(cp, ref)
+    slots = np.arange(R)[:, None] * block + np.array([0, 1])
+    xd = to_dev(x)
+    for t in (0, 1):                           # a call for each token, then both in one call on a third block
+        binding.cache_write(cp, pool, xd[:, t:t + 1, 0], xd[:, t:t + 1, 1], ints(slots[:, t:t + 1]))
+        plain.write(ref, x[:, t:t + 1, 0], x[:, t:t + 1, 1], slots[:, t:t + 1])
+    torch.cuda.synchronize()
+    assert_same_pool(from_pool(pool), ref)
+    ends = np.array([[16 * r + 13, 16 * r + 14] if r % 2 else [16 * r + 15, -1] for r in range(R)])
+    binding.cache_write(cp, pool, xd[:, :, 0], xd[:, :, 1], ints(ends))
+    plain.write(ref, x[:, :, 0], x[:, :, 1], ends)
+    torch.cuda.synchronize()
+    assert_same_pool(from_pool(pool), ref)
+
+
+def test_write_leaves_out_slots_outside_the_pool():
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(2)
+    cp = binding.cache_params(5, 1, 4, 16, 4, 2, 32)
+    ref = random_pool(rng, 4, 2, 16, 32)
+    pool = to_pool(cp, ref)
+    x = to_dev(rng.standard_normal((5, 3, 2, 32)).astype(np.float32))
+    slots = np.array([[64, 65, 66], [-1, 3, 4], [1 << 30, 1, 2], [-5, -5, -5], [5, 9, 10]])   # (5, then a gap: one token)
+    binding.cache_write(cp, pool, x, x, ints(slots), ints([99, -4, 1 << 30, 2, 1 << 29]))
+    torch.cuda.synchronize()
+    y = x.cpu().numpy()
+    plain.write(ref, y, y, np.array([[-1] * 3] * 4 + [[5, -1, -1]]))
+    assert_same_pool(from_pool(pool), ref)
+
+
+def test_write_offsets_past_32_bits():
+    """A pool of more than 4 GiB of codes, written and read at its end."""
+    import torch
+    from paper_1806_00588_amd import binding
+    n_blocks, heads, D, block = (1 << 32) // (4 * 128 * 128) + 9, 4, 128, 128
+    cp = binding.cache_params(2, 1, n_blocks, block, 2, heads, D)
+    pool = binding.CachePool(cp)
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((2, 130, heads, D)).astype(np.float32)
+    tables = np.array([[n_blocks - 1, n_blocks - 2], [0, n_blocks - 5]])
+    slots = np.concatenate([tables[:, :1] * block + np.arange(128), tables[:, 1:] * block + np.arange(2)], axis=1)
+    xd = to_dev(x)
+    binding.cache_write(cp, pool, xd, xd, ints(slots))
+    last = binding.CachePool(binding.cache_params(2, 1, 9, block, 2, heads, D), *[t[-9:] for t in (pool.k, pool.v, pool.k_scale, pool.v_scale)])
+    torch.cuda.synchronize()
+    ref = plain.Pool(np.zeros((10, heads, block, D), np.uint8), np.zeros((10, heads, block, D), np.uint8), np.zeros((10, heads)), np.zeros((10, heads)))
+    small = np.array([[8, 7], [9, 4]])
+    plain.write(ref, x, x, np.concatenate([small[:, :1] * block + np.arange(128), small[:, 1:] * block + np.arange(2)], axis=1))
+    got = from_pool(last)
+    assert_same_pool(got, plain.Pool(ref.k[:9], ref.v[:9], ref.k_scale[:9], ref.v_scale[:9]))
+    check_attention(rng, cp, pool, ref, small, np.array([130, 129]), "f32", 1, heads, device_tables=tables)
+
+
+# ---- attention ----------------------------------------------------------------------------------
+
+def check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, q_heads, causal=True, window=0, n_new=None, shared=None, device_tables=None,
+                    scale=None, q=None, stream=None, pitched=False):
+    import torch
+    from paper_1806_00588_amd import binding
+    R, D = cp.S * cp.B, cp.head_dim
+    kind = getattr(torch, TYPES[dtype])
+    scale = 1 / np.sqrt(D) if scale is None else scale
+    if q is None:
+        q = rng.standard_normal((R, T, q_heads, D)) * 2
+    q = torch.from_numpy(np.asarray(q, dtype=np.float32)).to(kind)
+    ap = binding.attention_params(T, q_heads, float(np.float32(scale)), causal, window)
+    ws = torch.full((binding.attention_workspace_bytes(cp, ap),), 255, dtype=torch.uint8, device="cuda")
+    if pitched:
+        qd = torch.zeros(R, T, q_heads + 2, D + 3, dtype=kind, device="cuda")[:, :, 1:-1, 3:]
+        out = torch.full((R, T + 1, q_heads, 2 * D + 1), 9.0, dtype=kind, device="cuda")[:, 1:, :, 1:D + 1]
+        qd.copy_(q)
+    else:
+        qd, out = q.cuda(), torch.full((R, T, q_heads, D), 9.0, dtype=kind, device="cuda")
+    lse = torch.full((R, T, q_heads), 9.0, device="cuda")
+    td, ld, nd, sd = ints(tables if device_tables is None else device_tables), ints(lengths), ints(n_new), ints(shared)
+    torch.cuda.synchronize()
+    binding.cache_attention(cp, ap, pool, qd, td, ld, ws, out, shared=sd, n_new=nd, lse=lse, stream=stream)
+    torch.cuda.synchronize()
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    want, want_lse, size, reach = plain.attention(ref, q.double().numpy(), tables, lengths, float(np.float32(scale)), causal, window, n_new)
+    for r in range(R):                         # behind a row's tokens nothing is written
+        n = T if n_new is None else n_new[r]
+        assert np.all(got[r, n:] == 9.0) and np.all(got_lse[r, n:] == 9.0)
+        want[r, n:], want_lse[r, n:] = 9.0, 9.0
+    inside, last = ROUNDING[dtype]
+    product = (D + 2) * 2.0 ** -24 * reach
+    off = 2 * product + 2.0 ** -20 + int(max(lengths)) * 2.0 ** -24 + inside
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    bad = np.abs(got - want) > off[..., None] * size + np.maximum(last * np.abs(want), 2.0 ** -25 if dtype == "f16" else 1e-30)
+    assert not bad.any(), (np.argwhere(bad)[:4], np.abs(got - want)[bad][:4], want[bad][:4])
+    assert np.array_equal(np.isneginf(got_lse), np.isneginf(want_lse))
+    fin = np.isfinite(want_lse)
+    assert np.all(np.abs(got_lse[fin] - want_lse[fin]) <= (product + 2.0 ** -20 + int(max(lengths)) * 2.0 ** -24)[fin] + 2.0 ** -24 * np.abs(want_lse[fin]))
+    return out, lse
+
+
+def scene(rng, S, B, lengths, block, heads, D, common=None, nan=0.0, spare=3, width=None):
+    """Params, pool, reference pool, tables; rows of a sentence share their first `common` tokens' whole blocks."""
+    from paper_1806_00588_amd import binding
+    lengths = np.asarray(lengths)
+    n = -(-lengths // block)
+    width = width or max(1, int(n.max())) + 1
+    ids = iter(rng.permutation(int(n.sum()) + spare).tolist())
+    tables = np.full((S * B, width), -1)
+    for s in range(S):
+        head = [next(ids) for _ in range((common[s] if common is not None else 0) // block)]
+        for b in range(B):
+            r = s * B + b
+            t = head[:n[r]] + [next(ids) for _ in range(n[r] - len(head))]
+            tables[r, :len(t)] = t
+    cp = binding.cache_params(S, B, int(n.sum()) + spare, block, width, heads, D)
+    ref = random_pool(rng, cp.n_blocks, heads, block, D, nan=nan)
+    return cp, to_pool(cp, ref), ref, tables, lengths
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D", [16, 48, 64, 80, 128, 192, 256])
+@pytest.mark.parametrize("block,heads,group", [(16, 2, 1), (32, 1, 4), (64, 2, 3), (128, 1, 20)])
+def test_attention_matches_plain(block, heads, group, D, dtype):
+    rng = np.random.default_rng(D + block)
+    cp, pool, ref, tables, lengths = scene(rng, 7, 1, [0, 1, 15, 16, 17, 130, 300], block, heads, D)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, heads * group)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T,group,window,causal", [(2, 1, 0, True), (5, 3, 0, True), (16, 1, 0, True), (17, 4, 0, True), (70, 2, 0, True), (3, 2, 1, True),
+                                                   (9, 4, 20, True), (40, 1, 100, True), (6, 2, 0, False), (33, 8, 0, False)])
+def test_several_tokens(T, group, window, causal, dtype):
+    """Tokens see their own and earlier positions, a window of them, or all; rows shorter than T have tokens before their first position,
+    which see nothing."""
+    rng = np.random.default_rng(T)
+    cp, pool, ref, tables, lengths = scene(rng, 6, 1, [0, 1, T, 63, 64 + T, 200], 16, 2, 64)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, 2 * group, causal, window)
+    n_new = np.minimum(lengths, rng.integers(0, T + 1, 6))
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, 2 * group, causal, window, n_new=n_new)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,B,group,T", [(1, 4, 1, 1), (2, 12, 4, 1), (3, 5, 3, 2), (1, 40, 2, 1), (2, 3, 8, 9), (1, 2, 32, 1)])
+def test_beams_that_share_blocks(S, B, group, T, dtype):
+    rng = np.random.default_rng(S + B)
+    common = [int(c) for c in rng.integers(0, 40, S) * 16]
+    lengths = np.array([c + int(x) for c in common for x in rng.integers(0, 90, B)])
+    cp, pool, ref, tables, lengths = scene(rng, S, B, lengths, 16, 2, 64, common)
+    whole = np.array(common) // 16
+    for r in range(S * B):
+        whole[r // B] = min(whole[r // B], lengths[r] // 16)
+    for shared in (None, whole, whole // 2, np.zeros(S, dtype=int)):
+        check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, 2 * group, shared=shared)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, 2 * group, window=70, shared=whole)
+    dead = lengths.copy()                      # beams that have ended: no tokens, a table of nothing
+    dead[1::2] = 0
+    dead_tables = tables.copy()
+    dead_tables[1::2] = -1
+    check_attention(rng, cp, pool, ref, dead_tables, dead, dtype, T, 2 * group, shared=whole)
+    dead, dead_tables = lengths.copy(), tables.copy()
+    dead[::B], dead_tables[::B] = 0, -1        # the first of each sentence
+    check_attention(rng, cp, pool, ref, dead_tables, dead, dtype, T, 2 * group, shared=whole)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_long_rows(dtype):
+    rng = np.random.default_rng(4)
+    cp, pool, ref, tables, lengths = scene(rng, 3, 1, [5000, 1, 3333], 16, 2, 64)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, 8)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, 2, window=4000)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_of_any_pitch_and_start(dtype):
+    rng = np.random.default_rng(5)
+    cp, pool, ref, tables, lengths = scene(rng, 4, 1, [33, 1, 0, 90], 16, 3, 48)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, 3, 6, pitched=True)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T", [1, 6])
+def test_what_is_not_seen_does_not_reach_a_result(T, dtype):
+    """Blocks full of NaN behind a row's end, scales of NaN and infinity in blocks that no row has, and a NaN in a key and in a value
+    that some of a row's tokens see and others do not."""
+    rng = np.random.default_rng(6)
+    cp, pool, ref, tables, lengths = scene(rng, 4, 1, [40, 17, 100, 64], 16, 2, 64)
+    for r in range(4):
+        end = lengths[r] % 16
+        if end:
+            ref.k[tables[r, lengths[r] // 16], :, end:] = 127
+            ref.v[tables[r, lengths[r] // 16], :, end:] = 255
+    free = np.setdiff1d(np.arange(cp.n_blocks), tables)
+    ref.k[free], ref.v[free] = 127, 127
+    ref.k_scale[free], ref.v_scale[free] = np.nan, np.inf
+    if T > 1:                                  # the last positions, which only the last tokens see
+        ref.v[tables[0, 2], 0, 7, 9] = 127
+        ref.k[tables[2, 6], 1, 2, 3] = 255
+    check_attention(rng, cp, to_pool(cp, ref), ref, tables, lengths, dtype, T, 4)
+    check_attention(rng, cp, to_pool(cp, ref), ref, tables, lengths, dtype, T, 4, window=30)
+
+
+def test_a_nan_reaches_whoever_sees_it():
+    rng = np.random.default_rng(7)
+    cp, pool, ref, tables, lengths = scene(rng, 2, 3, [70] * 6, 16, 2, 64, [64, 64])
+    ref.v[tables[1, 1], 1, 3, 17] = 127        # a shared block: all beams of the first sentence, one head, one value
+    ref.k[tables[4, 4], 0, 2, 5] = 127         # a beam's own block: one row, one head, all values
+    for shared in (None, np.array([4, 4])):
+        out, lse = check_attention(rng, cp, to_pool(cp, ref), ref, tables, lengths, "bf16", 1, 4, shared=shared)
+        assert int(out.isnan().sum()) == 3 * 2 + 2 * 64
+    q = rng.standard_normal((6, 1, 4, 64))
+    q[2, 0, 1, 5] = np.nan
+    clean = random_pool(rng, cp.n_blocks, 2, 16, 64)
+    for shared in (None, np.array([4, 4])):
+        out, _ = check_attention(rng, cp, to_pool(cp, clean), clean, tables, lengths, "f32", 1, 4, shared=shared, q=q)
+        assert int(out.isnan().sum()) == 64
+
+
+def test_large_and_small_products():
+    """Products of thousands, of which one decides; and queries whose products are all but 0."""
+    rng = np.random.default_rng(8)
+    cp, pool, ref, tables, lengths = scene(rng, 3, 1, [200, 77, 5], 32, 1, 128)
+    check_attention(rng, cp, pool, ref, tables, lengths, "f32", 1, 4, scale=8.0)
+    check_attention(rng, cp, pool, ref, tables, lengths, "f32", 1, 4, scale=1e-30)
+    q = rng.standard_normal((3, 1, 4, 128)) * 1e-20
+    check_attention(rng, cp, pool, ref, tables, lengths, "f32", 1, 4, q=q)
+
+
+def test_blocks_outside_the_pool_are_not_seen():
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(9)
+    cp, pool, ref, tables, lengths = scene(rng, 2, 1, [48, 48], 16, 1, 32)
+    bad = tables.copy()
+    bad[0, 1], bad[1, 0], bad[1, 1], bad[1, 2] = 1 << 30, -1, -7, cp.n_blocks
+    q = rng.standard_normal((2, 1, 2, 32)).astype(np.float32)
+    ap = binding.attention_params(1, 2, 0.2)
+    out, lse = torch.full((2, 1, 2, 32), 9.0, device="cuda"), torch.full((2, 1, 2), 9.0, device="cuda")
+    ws = torch.empty(binding.attention_workspace_bytes(cp, ap), dtype=torch.uint8, device="cuda")
+    binding.cache_attention(cp, ap, pool, to_dev(q), ints(bad), ints([48, 48]), ws, out, lse=lse)
+    torch.cuda.synchronize()
+    want, want_lse, _, _ = plain.attention(ref, q[:1], np.array([[tables[0, 0], tables[0, 2]]]), [32], np.float64(np.float32(0.2)))
+    assert np.allclose(out.cpu().numpy()[0], want[0], rtol=1e-5, atol=1e-6) and np.allclose(lse.cpu().numpy()[0], want_lse[0], rtol=1e-5, atol=1e-6)
+    assert torch.all(out[1] == 0) and torch.all(torch.isneginf(lse[1]))
+    # lengths that no table holds, shared blocks that no row has
+    for lengths in ([1 << 30, -4], [64, 2]):
+        binding.cache_attention(cp, ap, pool, to_dev(q), ints(tables), ints(lengths), ws, out, shared=ints([1 << 20, -3]), lse=lse)
+        torch.cuda.synchronize()
+
+
+def test_streams_graphs_and_the_same_bits():
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(10)
+    cp, pool, ref, tables, lengths = scene(rng, 2, 6, [700 + i for i in range(12)], 16, 2, 64, [640, 512])
+    shared = np.array([40, 32])
+    side = torch.cuda.Stream()
+    q = rng.standard_normal((12, 1, 8, 64))
+    a, la = check_attention(rng, cp, pool, ref, tables, lengths, "bf16", 1, 8, shared=shared, q=q, stream=side)
+    b, lb = check_attention(rng, cp, pool, ref, tables, lengths, "bf16", 1, 8, shared=shared, q=q)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    ap = binding.attention_params(1, 8, float(np.float32(1 / np.sqrt(64))))
+    ws = torch.empty(binding.attention_workspace_bytes(cp, ap), dtype=torch.uint8, device="cuda")
+    qd, td, ld, sd = torch.from_numpy(q).bfloat16().cuda(), ints(tables), ints(lengths), ints(shared)
+    out, lse = torch.empty_like(a), torch.empty_like(la)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        binding.cache_attention(cp, ap, pool, qd, td, ld, ws, out, shared=sd, lse=lse)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        binding.cache_attention(cp, ap, pool, qd, td, ld, ws, out, shared=sd, lse=lse)
+    for k in range(4):
+        out.fill_(3.0), lse.fill_(3.0), ws.fill_(85 * k)
+        if k == 2:
+            ld.sub_(200)                       # shorter rows, fewer shared blocks
+            sd.copy_(ints([31, 31]))
+            a, la = check_attention(rng, cp, pool, ref, tables, lengths - 200, "bf16", 1, 8, shared=np.array([31, 31]), q=q)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(la, lse)
+
+
+def test_binding_refuses():
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(11)
+    cp, pool, ref, tables, lengths = scene(rng, 2, 1, [20, 30], 16, 2, 32)
+    ap = binding.attention_params(2, 4, 0.2)
+    ws = torch.empty(binding.attention_workspace_bytes(cp, ap), dtype=torch.uint8, device="cuda")
+    q = torch.zeros(2, 2, 4, 32, device="cuda")
+    ok = dict(q=q, tables=ints(tables), lengths=ints(lengths), workspace=ws, out=q.clone())
+    for bad in ({"q": q.double()}, {"q": q[:, :1]}, {"q": q.cpu()}, {"q": q.transpose(2, 3)}, {"out": q[:1].clone()}, {"tables": ints(tables[:1])},
+                {"lengths": ints([1])}, {"shared": ints([1])}, {"n_new": ints([1])}, {"lse": torch.zeros(2, 2, 3, device="cuda")},
+                {"lengths": ints(lengths).long()}):
+        with pytest.raises(ValueError):
+            binding.cache_attention(cp, ap, pool, **{**ok, **bad})
+    for bad in ({"out": q.half()}, {"workspace": ws[:-1]}):
+        with pytest.raises(binding.LshBeamError):
+            binding.cache_attention(cp, ap, pool, **{**ok, **bad})
+    with pytest.raises(ValueError):
+        binding.cache_attention(binding.cache_params(2, 1, cp.n_blocks, 32, cp.max_blocks, 2, 32), ap, pool, **ok)
+    k = torch.zeros(2, 1, 2, 32, device="cuda")
+    for bad in ((k, k[:1], ints([[0], [16]])), (k, k.cpu(), ints([[0], [16]])), (k.double(), k.double(), ints([[0], [16]])), (k, k, ints([0]))):
+        with pytest.raises(ValueError):
+            binding.cache_write(cp, pool, *bad)
+    with pytest.raises(ValueError):
+        binding.cache_write(cp, pool, k, k, ints([[0], [16]]), ints([1]))
