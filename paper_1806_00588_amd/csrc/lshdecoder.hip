@@ -81,6 +81,43 @@ TablesRoom tables_room(const lsh_cache_params* c) {
     return w;
 }
 
+bool attention_ok(const lsh_cache_params* c, const lsh_attention_params* p) {
+    return cache_ok(c) && p && p->T >= 1 && p->T <= kMaxRows && p->n_heads >= 1 && p->n_heads <= 65535 && p->n_heads % c->n_heads == 0;
+}
+
+// How a call of the attention is divided.
+struct AttnPlan {
+    int row_tiles;      // row tiles of 16 of a workgroup
+    int chunk;          // tiles of 64 tokens of a chunk, a multiple of four: as many for each wave
+    int common_groups, common_splits, own_groups, own_splits;
+    int64_t common_units, own_units;
+    size_t acc, bytes;  // where the parts' products begin in the workspace; its size
+};
+AttnPlan attention_plan(const lsh_cache_params* c, const lsh_attention_params* p, bool shared) {
+    AttnPlan w{};
+    const int64_t R = (int64_t)c->S * c->B, per_row = (int64_t)p->T * (p->n_heads / c->n_heads);
+    const bool common = shared && c->B > 1;
+    const int64_t rows = common ? c->B * per_row : per_row;
+    w.row_tiles = rows <= 16 ? 1 : rows <= 32 || c->head_dim > 128 ? 2 : 4;
+    int64_t tiles = ceil_div((int64_t)c->max_blocks * c->block, kAttnTile);   // at most; what a row has is known on the device only
+    if (p->window > 0) tiles = std::min(tiles, ceil_div((int64_t)p->window + p->T, kAttnTile) + 1);
+    w.own_groups = (int)ceil_div(per_row, 16 * w.row_tiles);
+    w.common_groups = common ? (int)ceil_div(rows, 16 * w.row_tiles) : 0;
+    const int64_t own = R * c->n_heads * w.own_groups, sets = common ? (int64_t)c->S * c->n_heads * w.common_groups : own;
+    // short chunks where there is little to do, longer ones (a workgroup's begin and end are worth about four tiles) where the chip
+    // is full; beams' own tokens are few, and whatever there is of them goes round the workgroups
+    w.chunk = sets * ceil_div(tiles, 4) <= 512 ? 4 : sets * ceil_div(tiles, 8) <= 1024 ? 8 : 16;
+    const int64_t splits = std::min(ceil_div(tiles, w.chunk), std::max<int64_t>(1, 4096 / sets));
+    w.common_splits = common ? (int)splits : 0;
+    w.own_splits = (int)(common ? std::min(splits, std::max<int64_t>(1, 1024 / own)) : splits);
+    w.common_units = common ? sets * splits : 0;
+    w.own_units = own * w.own_splits;
+    const size_t parts = (size_t)(w.common_splits + w.own_splits), at = (size_t)R * p->T * p->n_heads * (parts > 1 ? parts : 0);
+    w.acc = round_up(at * sizeof(float2));
+    w.bytes = std::max<size_t>(256, w.acc + round_up(at * c->head_dim * sizeof(float)));
+    return w;
+}
+
 }  // namespace
 
 extern "C" {
@@ -185,16 +222,16 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
 }
 
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p) {
-    return cache_ok(c) && p && p->T >= 1 && p->n_heads >= 1 && p->n_heads % c->n_heads == 0 ? 256 : 0;
+    if (!attention_ok(c, p)) return 0;
+    return std::max(attention_plan(c, p, false).bytes, attention_plan(c, p, true).bytes);
 }
 
 lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
                                const lsh_rows* q_rows, const int32_t* tables_dev, const int32_t* lengths_dev, const int32_t* n_new_dev,
                                const int32_t* shared_dev, void* workspace_dev, size_t workspace_bytes, void* out_dev,
                                const lsh_rows* out_rows, float* lse_dev, void* hip_stream) {
-    if (!cache_ok(c) || !pool_ok(pool) || !p || p->T < 1 || p->n_heads < 1 || p->n_heads > 65535 || p->n_heads % c->n_heads != 0 ||
-        p->window < 0 || (p->window > 0 && !p->causal) || !(p->scale > 0.f && p->scale < INFINITY) || !q_dev || !tables_dev || !lengths_dev ||
-        !out_dev || !pitch_ok(q_rows, c->head_dim) || !pitch_ok(out_rows, c->head_dim) || q_rows->dtype != out_rows->dtype ||
+    if (!attention_ok(c, p) || !pool_ok(pool) || p->window < 0 || (p->window > 0 && !p->causal) ||
+        !(p->scale > 0.f && p->scale < INFINITY) || !q_dev || !tables_dev || !lengths_dev || !out_dev || !pitch_ok(q_rows, c->head_dim) || !pitch_ok(out_rows, c->head_dim) || q_rows->dtype != out_rows->dtype ||
         !aligned(q_dev, type_bytes(q_rows->dtype)) || !aligned(out_dev, type_bytes(out_rows->dtype)) || !workspace_dev ||
         !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
@@ -208,10 +245,32 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
     a.tables = tables_dev; a.lengths = lengths_dev; a.n_new = n_new_dev; a.shared = shared_dev;
     a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
     a.lse = lse_dev;
-    const int64_t grid = (int64_t)c->S * c->B * p->T;
-    if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
+    a.chunk = plan.chunk;
+    a.common_groups = plan.common_groups; a.common_splits = plan.common_splits; a.common_units = (int)plan.common_units;
+    a.own_groups = plan.own_groups; a.own_splits = plan.own_splits;
+    a.parts = plan.common_splits + plan.own_splits;
+    a.ml = static_cast<float2*>(workspace_dev);
+    a.acc = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.acc);
+    const int64_t grid = plan.common_units + plan.own_units, rows = (int64_t)c->S * c->B * p->T * p->n_heads;
+    if (grid > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    const hipStream_t st = (hipStream_t)hip_stream;
     for_type(q_rows->dtype, [&](auto type) {
-        hipLaunchKernelGGL(k_attention<decltype(type)::value>, dim3((unsigned)grid, (unsigned)p->n_heads), dim3(256), 0, (hipStream_t)hip_stream, a);
+        constexpr int kType = decltype(type)::value;
+        auto run = [&](auto dp, auto mt) {
+            constexpr int kDp = decltype(dp)::value, kMt = decltype(mt)::value;
+            if (c->head_dim == kDp) hipLaunchKernelGGL((k_attention_tiles<kType, kDp, kMt, true>), dim3((unsigned)grid), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((k_attention_tiles<kType, kDp, kMt, false>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        };
+        auto run_rows = [&](auto dp) {
+            if (plan.row_tiles == 1) run(dp, std::integral_constant<int, 1>());
+            else if (plan.row_tiles == 2) run(dp, std::integral_constant<int, 2>());
+            else if constexpr (decltype(dp)::value <= 128) run(dp, std::integral_constant<int, 4>());
+        };
+        if (c->head_dim <= 64) run_rows(std::integral_constant<int, 64>());
+        else if (c->head_dim <= 128) run_rows(std::integral_constant<int, 128>());
+        else run_rows(std::integral_constant<int, 256>());
+        if (a.parts > 1) hipLaunchKernelGGL(k_attention_join<kType>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
     });
     return launched();
 }
