@@ -11,7 +11,7 @@ DECODER_SRC = os.path.join(HERE, "csrc", "lshdecoder.hip")   # what stands aroun
 LIB = os.path.join(HERE, "liblshbeam.so")
 
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     # keep the compiler from forming packed-fp32 VALU ops out of scalar float code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -25,13 +25,25 @@ def sources():
 
 
 def build(verbose: bool = True) -> str:
+    """The two translation units at the same time, then the library of both."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", tmp, SRC, DECODER_SRC]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    objects = [tmp + ".%d.o" % i for i in range(2)]
+    compiles = [[hipcc] + HIPCC_FLAGS + ["-c", "-o", o, src] for o, src in zip(objects, (SRC, DECODER_SRC))]
+    link = [hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp] + objects
+    try:
+        if verbose:
+            print("\n".join(" ".join(c) for c in compiles + [link]), flush=True)
+        running = [subprocess.Popen(c) for c in compiles]
+        failed = [c for c, p in zip(compiles, running) if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.check_call(link)
+        os.replace(tmp, LIB)
+    finally:
+        for path in objects + [tmp]:
+            if os.path.exists(path):
+                os.remove(path)
     return LIB
 
 

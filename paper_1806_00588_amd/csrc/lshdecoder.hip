@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "beam_select.h"
@@ -85,37 +86,68 @@ bool attention_ok(const lsh_cache_params* c, const lsh_attention_params* p) {
     return cache_ok(c) && p && p->T >= 1 && p->T <= kMaxRows && p->n_heads >= 1 && p->n_heads <= 65535 && p->n_heads % c->n_heads == 0;
 }
 
-// How a call of the attention is divided.
+// How a call of the attention is divided: a launch for all beams together (if the blocks that they have in common are given) and one
+// for each row by itself, which a third joins if there is more than one part of a row.
+struct AttnLaunch {
+    int row_tiles;      // 1: k_attention_few, else the waves of k_attention_rows
+    int chunk;          // tiles of 64 tokens
+    int groups, splits;
+    int64_t units;      // workgroups; 0: no such launch
+};
 struct AttnPlan {
-    int row_tiles;      // row tiles of 16 of a workgroup
-    int chunk;          // tiles of 64 tokens of a chunk, a multiple of four: as many for each wave
-    int common_groups, common_splits, own_groups, own_splits;
-    int64_t common_units, own_units;
+    AttnLaunch common, own;
     size_t acc, bytes;  // where the parts' products begin in the workspace; its size
 };
+// sets: pairs of a row set and a head; tiles: of a row at most -- what a row has is known on the device only, and a chunk behind its
+// last tile costs little.  Short chunks where there is little to do, longer ones where the chip is full: a workgroup's begin and end
+// are worth some tiles.
+AttnLaunch attention_launch(int64_t rows, int64_t sets, int64_t tiles, int64_t most_splits) {
+    AttnLaunch w{};
+    w.groups = (int)ceil_div(rows, 64);
+    w.row_tiles = (int)ceil_div(ceil_div(rows, w.groups), 16);
+    sets *= w.groups;
+    w.chunk = 4;
+    while (w.chunk < kMaxChunk && sets * ceil_div(tiles, w.chunk) > 128 * w.chunk + (w.row_tiles > 1 ? 768 : 0)) w.chunk *= 2;
+    w.splits = (int)std::min({ceil_div(tiles, w.chunk), std::max<int64_t>(1, 4096 / sets), most_splits});
+    w.units = sets * w.splits;
+    return w;
+}
 AttnPlan attention_plan(const lsh_cache_params* c, const lsh_attention_params* p, bool shared) {
     AttnPlan w{};
     const int64_t R = (int64_t)c->S * c->B, per_row = (int64_t)p->T * (p->n_heads / c->n_heads);
-    const bool common = shared && c->B > 1;
-    const int64_t rows = common ? c->B * per_row : per_row;
-    w.row_tiles = rows <= 16 ? 1 : rows <= 32 || c->head_dim > 128 ? 2 : 4;
-    int64_t tiles = ceil_div((int64_t)c->max_blocks * c->block, kAttnTile);   // at most; what a row has is known on the device only
+    int64_t tiles = ceil_div((int64_t)c->max_blocks * c->block, kAttnTile);
     if (p->window > 0) tiles = std::min(tiles, ceil_div((int64_t)p->window + p->T, kAttnTile) + 1);
-    w.own_groups = (int)ceil_div(per_row, 16 * w.row_tiles);
-    w.common_groups = common ? (int)ceil_div(rows, 16 * w.row_tiles) : 0;
-    const int64_t own = R * c->n_heads * w.own_groups, sets = common ? (int64_t)c->S * c->n_heads * w.common_groups : own;
-    // short chunks where there is little to do, longer ones (a workgroup's begin and end are worth about four tiles) where the chip
-    // is full; beams' own tokens are few, and whatever there is of them goes round the workgroups
-    w.chunk = sets * ceil_div(tiles, 4) <= 512 ? 4 : sets * ceil_div(tiles, 8) <= 1024 ? 8 : 16;
-    const int64_t splits = std::min(ceil_div(tiles, w.chunk), std::max<int64_t>(1, 4096 / sets));
-    w.common_splits = common ? (int)splits : 0;
-    w.own_splits = (int)(common ? std::min(splits, std::max<int64_t>(1, 1024 / own)) : splits);
-    w.common_units = common ? sets * splits : 0;
-    w.own_units = own * w.own_splits;
-    const size_t parts = (size_t)(w.common_splits + w.own_splits), at = (size_t)R * p->T * p->n_heads * (parts > 1 ? parts : 0);
+    const bool common = shared && c->B > 1;
+    if (common) w.common = attention_launch(c->B * per_row, (int64_t)c->S * c->n_heads, tiles, INT32_MAX);
+    // (beams' own tokens are few, and whatever there is of them goes round the workgroups)
+    w.own = attention_launch(per_row, R * c->n_heads, tiles, common ? std::max<int64_t>(1, 1024 / (R * c->n_heads)) : INT32_MAX);
+    const size_t parts = (size_t)(w.common.splits + w.own.splits), at = (size_t)R * p->T * p->n_heads * (parts > 1 ? parts : 0);
     w.acc = round_up(at * sizeof(float2));
     w.bytes = std::max<size_t>(256, w.acc + round_up(at * c->head_dim * sizeof(float)));
     return w;
+}
+
+// A launch with more than 64 KB of LDS; the limit is raised once per kernel and device.
+template <auto KERNEL, int LDS, typename ARGS> bool launch_lds(unsigned grid, unsigned threads, hipStream_t st, const ARGS& a) {
+    if constexpr (LDS > 64 * 1024) {
+        static std::atomic<uint64_t> done{0};   // a bit per device
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess) return false;
+        const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+        if (!(bit && (done.load(std::memory_order_acquire) & bit))) {
+            if (hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return false;
+            done.fetch_or(bit, std::memory_order_release);
+        }
+    }
+    hipLaunchKernelGGL(KERNEL, dim3(grid), dim3(threads), LDS, st, a);
+    return true;
+}
+template <int TYPE, int DP, bool EXACT> bool attend(const AttnArgs& a, const AttnLaunch& w, hipStream_t st) {
+    const unsigned grid = (unsigned)w.units;
+    if (w.row_tiles == 1) return launch_lds<k_attention_few<TYPE, DP, EXACT>, kFewLds<TYPE, DP>>(grid, 256, st, a);
+    if (w.row_tiles == 2) return launch_lds<k_attention_rows<TYPE, DP, 2, EXACT>, kRowsLds<TYPE, DP, 2>>(grid, 128, st, a);
+    if (w.row_tiles == 3) return launch_lds<k_attention_rows<TYPE, DP, 3, EXACT>, kRowsLds<TYPE, DP, 3>>(grid, 192, st, a);
+    return launch_lds<k_attention_rows<TYPE, DP, 4, EXACT>, kRowsLds<TYPE, DP, 4>>(grid, 256, st, a);
 }
 
 }  // namespace
@@ -223,7 +255,7 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
 
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p) {
     if (!attention_ok(c, p)) return 0;
-    return std::max(attention_plan(c, p, false).bytes, attention_plan(c, p, true).bytes);
+    return std::max(attention_plan(c, p, false).bytes, attention_plan(c, p, true).bytes);   // (who has a workspace may leave `shared` out)
 }
 
 lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
@@ -246,33 +278,34 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
     a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
     a.lse = lse_dev;
     const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
-    a.chunk = plan.chunk;
-    a.common_groups = plan.common_groups; a.common_splits = plan.common_splits; a.common_units = (int)plan.common_units;
-    a.own_groups = plan.own_groups; a.own_splits = plan.own_splits;
-    a.parts = plan.common_splits + plan.own_splits;
+    a.has_common = plan.common.units > 0;
+    a.parts = plan.common.splits + plan.own.splits;
     a.ml = static_cast<float2*>(workspace_dev);
     a.acc = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.acc);
-    const int64_t grid = plan.common_units + plan.own_units, rows = (int64_t)c->S * c->B * p->T * p->n_heads;
-    if (grid > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
+    if (plan.common.units > kMaxGrid || plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)hip_stream;
+    bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
-        auto run = [&](auto dp, auto mt) {
-            constexpr int kDp = decltype(dp)::value, kMt = decltype(mt)::value;
-            if (c->head_dim == kDp) hipLaunchKernelGGL((k_attention_tiles<kType, kDp, kMt, true>), dim3((unsigned)grid), dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((k_attention_tiles<kType, kDp, kMt, false>), dim3((unsigned)grid), dim3(256), 0, st, a);
-        };
-        auto run_rows = [&](auto dp) {
-            if (plan.row_tiles == 1) run(dp, std::integral_constant<int, 1>());
-            else if (plan.row_tiles == 2) run(dp, std::integral_constant<int, 2>());
-            else if constexpr (decltype(dp)::value <= 128) run(dp, std::integral_constant<int, 4>());
-        };
-        if (c->head_dim <= 64) run_rows(std::integral_constant<int, 64>());
-        else if (c->head_dim <= 128) run_rows(std::integral_constant<int, 128>());
-        else run_rows(std::integral_constant<int, 256>());
-        if (a.parts > 1) hipLaunchKernelGGL(k_attention_join<kType>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
+        for (int own = 0; own < 2; ++own) {
+            const AttnLaunch& w = own ? plan.own : plan.common;
+            if (w.units == 0) continue;
+            a.common = !own;
+            a.chunk = w.chunk; a.groups = w.groups; a.splits = w.splits;
+            a.part0 = own ? plan.common.splits : 0;
+            const int D = c->head_dim;
+            ok = ok && (D == 64    ? attend<kType, 64, true>(a, w, st)
+                        : D < 64   ? attend<kType, 64, false>(a, w, st)
+                        : D == 128 ? attend<kType, 128, true>(a, w, st)
+                        : D < 128  ? attend<kType, 128, false>(a, w, st)
+                        : D == 192 ? attend<kType, 192, true>(a, w, st)
+                        : D == 256 ? attend<kType, 256, true>(a, w, st)
+                                   : attend<kType, 256, false>(a, w, st));
+        }
+        if (ok && a.parts > 1) hipLaunchKernelGGL(k_attention_join<kType>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
     });
-    return launched();
+    return ok ? launched() : LSH_ERR_HIP;
 }
 
 }  // extern "C"
