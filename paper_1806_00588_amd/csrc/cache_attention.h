@@ -45,8 +45,8 @@ struct AttnArgs {
     // of a launch: all beams of a sentence over the blocks that they have in common, or each row over the rest of its own
     int common;
     int has_common;            // there is a launch of the first kind
-    int chunk;                 // tiles of a chunk
-    int groups, splits;        // groups of rows; workgroups along the tokens
+    int chunk;                 // tiles of a chunk at least
+    int sets, groups, splits;  // sentences or rows; groups of their rows; workgroups along the tokens
     int part0;                 // the first part that this launch writes
     int parts;                 // in all; 1: results are written at once
     float2* ml;                // workspace [R * T * q_heads, parts]: max of the products (times log2 e), sum of the exponentials; sum -1: done
@@ -123,133 +123,151 @@ __device__ __forceinline__ AttnRow attn_row(const AttnArgs& a, int s_or_r, int h
     const int g = a.q_heads / a.heads, per = a.T * g;
     AttnRow w{0, 0, 0, 0, 0, false};
     if (i >= (a.common ? a.B * per : per)) return w;
-    const int b = a.common ? i / per : 0, at = i - b * per;
+    const int b = a.common ? (int)((unsigned)i / (unsigned)per) : 0, at = i - b * per;
     w.r = a.common ? s_or_r * a.B + b : s_or_r;
-    w.t = at / g;
+    w.t = (int)((unsigned)at / (unsigned)g);
     w.head = h * g + at - w.t * g;
     const int n = row_new(a, w.r);
     w.valid = w.t < n;
-    if (w.valid) seen(a, row_length(a, w.r), n, w.t, &w.lo, &w.hi);
+    seen(a, row_length(a, w.r), n, w.t, &w.lo, &w.hi);
     return w;
 }
-// Tokens that the rows of sentence s have in common.
-__device__ __forceinline__ int common_tokens(const AttnArgs& a, int s) {
-    return a.has_common ? min(max(a.shared[s], 0), a.width) * a.block : 0;
-}
 
-// A workgroup's place and what is found out once for it.
-constexpr int kMaxChunk = 32;                        // tiles
-struct AttnShared {
-    AttnRow row[64];
-    int id[4 * kMaxChunk];                           // block of each 16 tokens of the chunk, -1: none that anybody here sees
-    float k_scale[4 * kMaxChunk], v_scale[4 * kMaxChunk];   // times scale * log2 e; as it is
-    int vlo, vhi, lo_most, hi_least, first_lo, table_row;
-};
+// A workgroup's place, and what is found out once for it: the same in all lanes.
 struct AttnPlace {
     int split, group, h, sr;                         // sr: sentence or row
-    int shared_tokens;
-    int tile0, tiles, chunks;                        // of the positions that any row sees here
+    int shared_tokens;                               // that the rows of the sentence have in common
+    int vlo, vhi;                                    // positions that any row sees here
+    int lo_most, hi_least;                           // ... and that all do
+    int tile0, tiles, chunk, chunks;                 // of the former; tiles of a chunk
+    int table_row;
     bool direct;                                     // nobody else has a part of these rows
 };
-
-// Rows, positions: by all threads, ends with a barrier.
-template <int ROWS> __device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a, AttnShared& sh) {
+__device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a) {
     AttnPlace p;
-    int u = blockIdx.x;
-    p.split = u % a.splits;
-    u /= a.splits;
-    p.group = u % a.groups;
-    u /= a.groups;
-    p.h = u % a.heads;
-    p.sr = u / a.heads;
-    const int s = a.common ? p.sr : p.sr / a.B;
-    p.shared_tokens = common_tokens(a, s);
-    const int from = a.common ? 0 : p.shared_tokens, to = a.common ? p.shared_tokens : INT32_MAX;
-    if (wave_id() == 0) {
-        const int i = lane_id();
-        AttnRow w{0, 0, 0, 0, 0, false};
-        if (i < ROWS) w = attn_row(a, p.sr, p.h, p.group * ROWS + i);
-        int first = w.valid && w.lo < w.hi ? w.lo : INT32_MAX;
-        w.lo = max(w.lo, from);
-        w.hi = min(w.hi, to);
-        const bool live = w.valid && w.lo < w.hi;
-        int vlo = live ? w.lo : INT32_MAX, vhi = live ? w.hi : 0;
-        // a row without a position here is worked on like the rest and left out at the end
-        if (!live) { w.lo = INT32_MIN; w.hi = INT32_MAX; }
-        int lo_most = w.lo, hi_least = w.hi, table_row = p.sr;
-        if (i < ROWS) sh.row[i] = w;
-        if (a.common) {                              // the sentence's first row with tokens
-            int b0 = INT32_MAX;
-            for (int b = i; b < a.B; b += kWave)
-                if (b0 == INT32_MAX && a.lengths[p.sr * a.B + b] > 0) b0 = b;
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) b0 = min(b0, __shfl_xor(b0, off, kWave));
-            table_row = p.sr * a.B + min(b0, a.B - 1);
-        }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            vlo = min(vlo, __shfl_xor(vlo, off, kWave));
-            vhi = max(vhi, __shfl_xor(vhi, off, kWave));
-            lo_most = max(lo_most, __shfl_xor(lo_most, off, kWave));
-            hi_least = min(hi_least, __shfl_xor(hi_least, off, kWave));
-            first = min(first, __shfl_xor(first, off, kWave));
-        }
-        if (i == 0) { sh.vlo = vlo; sh.vhi = vhi; sh.lo_most = lo_most; sh.hi_least = hi_least; sh.first_lo = first; sh.table_row = table_row; }
-    }
-    __syncthreads();
-    const int vhi = __builtin_amdgcn_readfirstlane(sh.vhi);
-    p.tile0 = vhi > 0 ? __builtin_amdgcn_readfirstlane(sh.vlo) / kAttnTile : 0;
-    p.tiles = vhi > 0 ? (vhi + kAttnTile - 1) / kAttnTile - p.tile0 : 0;
-    p.chunks = (p.tiles + a.chunk - 1) / a.chunk;
-    p.direct = a.parts == 1 || (!a.common && p.chunks <= 1 && __builtin_amdgcn_readfirstlane(sh.first_lo) >= p.shared_tokens);
+    // (heads first: workgroups go round the eight XCDs one by one, and chunks next to each other in that order -- which short rows do
+    // not have -- would leave some of them idle)
+    unsigned u = blockIdx.x;
+    p.h = u % (unsigned)a.heads;
+    u /= (unsigned)a.heads;
+    p.group = u % (unsigned)a.groups;
+    u /= (unsigned)a.groups;
+    p.sr = u % (unsigned)a.sets;
+    p.split = u / (unsigned)a.sets;
+    p.shared_tokens = 0;
+    if (a.has_common) p.shared_tokens = min(max(a.shared[a.common ? p.sr : p.sr / a.B], 0), a.width) * a.block;
+    p.table_row = a.common ? p.sr * a.B : p.sr;
     return p;
 }
 
-// Queries to LDS as operands [plane, row tile, kk, half, lane].
-template <int TYPE, int DP, int MT>
-__device__ __forceinline__ void stage_queries(const AttnArgs& a, const AttnShared& sh, uint4* to, int threads) {
-    using T = typename WordOf<TYPE>::type;
-    constexpr int NP = kPlanes<TYPE>, KK = DP / 64;
-    for (int e = threadIdx.x; e < 16 * MT * (DP / 8); e += threads) {
-        const int cd = e % (DP / 8), row = e / (DP / 8);
-        const AttnRow& w = sh.row[row];
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (w.valid && 8 * cd < a.D) {
-            const T* p = static_cast<const T*>(a.q) + w.r * a.qp.row + w.t * a.qp.token + w.head * a.qp.head + 8 * cd;
-            if constexpr (TYPE == kTypeF32) {
-                const Float4U u = *reinterpret_cast<const Float4U*>(p), v = *reinterpret_cast<const Float4U*>(p + 4);
-                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-            } else {
-                const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(p);
+constexpr int kLookup = 32;                          // tiles whose blocks are looked up at a time
+struct AttnShared {
+    AttnRow row[16];
+    int id[4 * kLookup];                             // block of each 16 tokens, -1: none that anybody here sees
+    float k_scale[4 * kLookup], v_scale[4 * kLookup];   // times scale * log2 e; as it is
+};
+
+// The rest of the place, by every wave for itself: w is its lane's row (the rows of 64 lanes hold those of the workgroup), whose
+// positions are cut to what belongs to this launch.
+__device__ __forceinline__ void find_positions(const AttnArgs& a, AttnPlace& p, AttnRow& w) {
+    int first = w.valid && w.lo < w.hi ? w.lo : INT32_MAX;
+    w.lo = max(w.lo, a.common ? 0 : p.shared_tokens);
+    w.hi = min(w.hi, a.common ? p.shared_tokens : INT32_MAX);
+    const bool live = w.valid && w.lo < w.hi;
+    int vlo = live ? w.lo : INT32_MAX, vhi = live ? w.hi : 0;
+    // a row without a position here is worked on like the rest and left out at the end
+    if (!live) { w.lo = INT32_MIN; w.hi = INT32_MAX; }
+    int lo_most = w.lo, hi_least = w.hi;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { x[2 * i] = word_f32<TYPE>((T)(v.w[i] & 0xffffu)); x[2 * i + 1] = word_f32<TYPE>((T)(v.w[i] >> 16)); }
-            }
-        }
-        uint4 planes[NP];
-        planes_of<NP>(x, planes);
-        const int piece = cd >> 1, kk = piece >> 2, lane = (piece & 3) * 16 + (row & 15);
+    for (int off = 32; off > 0; off >>= 1) {
+        vlo = min(vlo, __shfl_xor(vlo, off, kWave));
+        vhi = max(vhi, __shfl_xor(vhi, off, kWave));
+        lo_most = max(lo_most, __shfl_xor(lo_most, off, kWave));
+        hi_least = min(hi_least, __shfl_xor(hi_least, off, kWave));
+        first = min(first, __shfl_xor(first, off, kWave));
+    }
+    p.vlo = __builtin_amdgcn_readfirstlane(vlo);
+    p.vhi = __builtin_amdgcn_readfirstlane(vhi);
+    p.lo_most = __builtin_amdgcn_readfirstlane(lo_most);
+    p.hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+    p.tile0 = p.vhi > 0 ? p.vlo / kAttnTile : 0;
+    p.tiles = p.vhi > 0 ? (p.vhi + kAttnTile - 1) / kAttnTile - p.tile0 : 0;
+    p.chunk = max(a.chunk, (p.tiles + a.splits - 1) / a.splits);
+    p.chunks = (p.tiles + p.chunk - 1) / p.chunk;
+    p.direct = a.parts == 1 || (!a.common && p.chunks <= 1 && __builtin_amdgcn_readfirstlane(first) >= p.shared_tokens);
+    if (a.common) {                                  // the table of the sentence's first row with tokens
+        int b0 = INT32_MAX;
+        for (int b = lane_id(); b < a.B; b += kWave)
+            if (b0 == INT32_MAX && a.lengths[p.sr * a.B + b] > 0) b0 = b;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) to[(((p * MT + (row >> 4)) * KK + kk) * 2 + (cd & 1)) * 64 + lane] = planes[p];
+        for (int off = 32; off > 0; off >>= 1) b0 = min(b0, __shfl_xor(b0, off, kWave));
+        p.table_row = p.sr * a.B + min(__builtin_amdgcn_readfirstlane(b0), a.B - 1);
     }
 }
 
-// Blocks and scales of chunk `chunk`'s tokens, 16 at a time: thread i the i-th of them.
-__device__ __forceinline__ void load_chunk(const AttnArgs& a, AttnShared& sh, const AttnPlace& p, int chunk) {
+// A table entry for the 16 tokens from `pos` on, any row's if there is none.
+__device__ __forceinline__ int32_t table_entry(const AttnArgs& a, int table_row, int64_t pos) {
+    return a.tables[(int64_t)table_row * a.width + min(pos >> __builtin_ctz(a.block), (int64_t)a.width - 1)];
+}
+// Blocks and scales of n tiles (kLookup at most) from `tile` on, 16 tokens at a time: thread i the i-th of them.  `entry` is its table entry.
+__device__ __forceinline__ void put_lookup(const AttnArgs& a, AttnShared& sh, const AttnPlace& p, int64_t tile, int n, int32_t entry) {
     const int i = threadIdx.x;
-    if (i >= 4 * a.chunk) return;
-    const int64_t pos = ((int64_t)p.tile0 + (int64_t)chunk * a.chunk) * kAttnTile + 16 * i;
-    int32_t id = -1;
-    if (pos < sh.vhi && pos + 15 >= sh.vlo && pos / a.block < a.width) {
-        id = a.tables[(int64_t)sh.table_row * a.width + pos / a.block];
-        id = id < a.n_blocks ? max(id, -1) : -1;
-    }
+    if (i >= 4 * n) return;
+    const int64_t pos = tile * kAttnTile + 16 * i;
+    const int32_t id = pos < p.vhi && pos + 15 >= p.vlo && entry >= 0 && entry < a.n_blocks && pos < (int64_t)a.width * a.block ? entry : -1;
     const int64_t at = (int64_t)max(id, 0) * a.heads + p.h;
     sh.id[i] = id;
     sh.k_scale[i] = id >= 0 ? a.scale_k[at] * (a.scale * 1.44269504f) : 0.f;
     sh.v_scale[i] = id >= 0 ? a.scale_v[at] : 0.f;
 }
 
-// A wave's sums for one row tile: lane (n, c) has values 16 dt + 4 c + j of row n, its maximum, and of its sum what its tokens give.
+// Queries: asked for (whatever the row's tokens: they are there), then put to LDS as operands [plane, row tile, kk, half, lane].
+template <int TYPE, int DP, int MT, int THREADS> struct Queries {
+    using T = typename WordOf<TYPE>::type;
+    static constexpr int NP = kPlanes<TYPE>, KK = DP / 64, ALL = 16 * MT * (DP / 8), OWN = (ALL + THREADS - 1) / THREADS;
+    struct Eight { uint32_t w[TYPE == kTypeF32 ? 8 : 4]; };
+    Eight x[OWN];
+    __device__ __forceinline__ void ask(const AttnArgs& a, const AttnPlace& p) {
+        const int g = a.q_heads / a.heads, per = a.T * g, rows = a.common ? a.B * per : per;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const int e = threadIdx.x + j * THREADS, cd = e % (DP / 8), i = p.group * 16 * MT + e / (DP / 8);
+            x[j] = Eight{};
+            if (e >= ALL || i >= rows || 8 * cd >= a.D) continue;
+            const int b = a.common ? (int)((unsigned)i / (unsigned)per) : 0, at = i - b * per, t = (int)((unsigned)at / (unsigned)g);
+            const int r = a.common ? p.sr * a.B + b : p.sr;
+            const T* from = static_cast<const T*>(a.q) + r * a.qp.row + t * a.qp.token + (p.h * g + at - t * g) * a.qp.head + 8 * cd;
+            const Chunk16U<T> u = *reinterpret_cast<const Chunk16U<T>*>(from);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[j].w[q] = u.w[q];
+            if constexpr (TYPE == kTypeF32) {
+                const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(from + 4);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[j].w[4 + q] = v.w[q];
+            }
+        }
+    }
+    __device__ __forceinline__ void put(uint4* to) const {
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const int e = threadIdx.x + j * THREADS, cd = e % (DP / 8), row = e / (DP / 8);
+            if (e >= ALL) continue;
+            float f[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if constexpr (TYPE == kTypeF32) f[q] = __uint_as_float(x[j].w[q]);
+                else f[q] = word_f32<TYPE>((T)(x[j].w[q >> 1] >> (16 * (q & 1)) & 0xffffu));
+            }
+            uint4 planes[NP];
+            planes_of<NP>(f, planes);
+            const int piece = cd >> 1, kk = piece >> 2, lane = (piece & 3) * 16 + (row & 15);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) to[(((p * MT + (row >> 4)) * KK + kk) * 2 + (cd & 1)) * 64 + lane] = planes[p];
+        }
+    }
+};
+
+// A wave's sums for 16 rows: lane (n, c) has values 16 dt + 4 c + j of row n, its maximum, and of its sum what its tokens give.
 template <int DP> struct RowSums {
     float m = -INFINITY, l = 0.f;
     f32x4 acc[DP / 16];
@@ -259,13 +277,14 @@ template <int DP> struct RowSums {
     }
 };
 
-// One tile: products with the keys (k(kk, i): 16 codes of a token), then `between()`, softmax, products with the values
-// (v(dt): a value's codes of 16 tokens).  rel: the tile's number in the chunk, pos its first token.
-template <int TYPE, int DP, int MT, bool EXACT, typename K, typename V, typename F>
-__device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnShared& sh, const uint4* queries, int row_tile, int rel, int pos,
-                                            int lo, int hi, RowSums<DP>& to, K k, V v, F between) {
+// One tile: products of the queries (q(plane, kk, half): an operand) with the keys (k(kk, i): 16 codes of a token), then `between()`,
+// softmax, products with the values (v(dt): a value's codes of 16 tokens).  rel: the tile's number among those looked up, pos its
+// first token.
+template <int TYPE, int DP, bool EXACT, typename Q, typename K, typename V, typename F>
+__device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnPlace& p, const AttnShared& sh, int rel, int pos,
+                                            int lo, int hi, RowSums<DP>& to, Q q, K k, V v, F between) {
     constexpr int NP = kPlanes<TYPE>, KK = DP / 64, DT = DP / 16;
-    const int ln = lane_id(), c = ln >> 4, pieces = a.D >> 4;
+    const int c = lane_id() >> 4, pieces = a.D >> 4;
     f32x4 sc[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -281,11 +300,12 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnShared&
 #pragma unroll
                 for (int i = 0; i < 4; ++i) key[i] = half ? codes_to_operand(w[i].z, w[i].w) : codes_to_operand(w[i].x, w[i].y);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const bf16x8 q = __builtin_bit_cast(bf16x8, queries[(((p * MT + row_tile) * KK + kk) * 2 + half) * 64 + ln]);
+                for (int pl = 0; pl < NP; ++pl) {
+                    const bf16x8 query = __builtin_bit_cast(bf16x8, q(pl, kk, half));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[i], q, sc[i], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[i], query, sc[i], 0, 0, 0);
                 }
+                if constexpr (DP > 64) __builtin_amdgcn_sched_barrier(0);   // (or all codes are widened before they are used, and the registers do not last)
             }
         }
     }
@@ -293,15 +313,15 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnShared&
     const bool has = sh.id[4 * rel + c] >= 0;
     const float k_scale = sh.k_scale[4 * rel + c], v_scale = sh.v_scale[4 * rel + c];
     // which tokens the rows see: all of a tile but at the ends
-    const bool whole = __builtin_amdgcn_readfirstlane(pos >= sh.lo_most && pos + kAttnTile <= sh.hi_least && __ballot(!has) == 0);
+    const bool whole = __builtin_amdgcn_readfirstlane(pos >= p.lo_most && pos + kAttnTile <= p.hi_least && __ballot(!has) == 0);
     const int first = pos + 16 * c;
     float x[16], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sc[i >> 2][i & 3] * k_scale;
-    if (!whole) {
-        const int vhi = sh.vhi;
+    if (!whole) {   // the row sees tokens from .. end - 1 of the lane's
+        const int from = max(lo - first, 0), end = has ? min(hi, p.vhi) - first : 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = has && first + i >= lo && first + i < hi && first + i < vhi ? x[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) x[i] = i >= from && i < end ? x[i] : -INFINITY;
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
@@ -332,53 +352,57 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnShared&
         for (int i = 0; i < 8; ++i) y[i] = x[8 * half + i];
         planes_of<NP>(y, prob[half]);
     }
+    if constexpr (DP > 64) __builtin_amdgcn_sched_barrier(0);
     if (whole) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             if (EXACT || dt < pieces) {
-                const uint4 w = v(dt);
-                const bf16x8 v0 = codes_to_operand(w.x, w.y), v1 = codes_to_operand(w.z, w.w);
+                const uint4 both = v(dt);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, __builtin_bit_cast(bf16x8, prob[0][p]), to.acc[dt], 0, 0, 0);
-                    to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, __builtin_bit_cast(bf16x8, prob[1][p]), to.acc[dt], 0, 0, 0);
+                for (int half = 0; half < 2; ++half) {
+                    const bf16x8 value = half ? codes_to_operand(both.z, both.w) : codes_to_operand(both.x, both.y);
+#pragma unroll
+                    for (int pl = 0; pl < NP; ++pl)
+                        to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, __builtin_bit_cast(bf16x8, prob[half][pl]), to.acc[dt], 0, 0, 0);
                 }
+                if constexpr (DP > 64) { if (dt & 1) __builtin_amdgcn_sched_barrier(0); }
             }
         }
         return;
     }
     // values that no row sees count as 0, whatever lies there, and a NaN among the others counts for the rows that see it
-    const int vlo = sh.vlo, vhi = sh.vhi;
-    uint32_t keep[4];
+    uint32_t keep[2][2];
     bf16x8 sees[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const int t = first + i;
-        const uint32_t byte = has && t >= vlo && t < vhi ? 0xffu << (8 * (i & 3)) : 0u;
-        keep[i >> 2] = i & 3 ? keep[i >> 2] | byte : byte;
-        sees[i >> 3][i & 7] = t >= lo && t < hi ? (__bf16)1.f : (__bf16)0.f;
+        const uint32_t byte = has && first + i >= p.vlo && first + i < p.vhi ? 0xffu << (8 * (i & 3)) : 0u;
+        uint32_t& at = keep[i >> 3][i >> 2 & 1];
+        at = i & 3 ? at | byte : byte;
+        sees[i >> 3][i & 7] = first + i >= lo && first + i < hi ? (__bf16)1.f : (__bf16)0.f;
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
         if (EXACT || dt < pieces) {
-            uint4 w = v(dt);
-            w = make_uint4(w.x & keep[0], w.y & keep[1], w.z & keep[2], w.w & keep[3]);
-            const uint4 bad = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
-            if (__ballot((bad.x | bad.y | bad.z | bad.w) != 0)) {   // the code 1.0 (0x38) in the place of each NaN
-                f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-                hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_operand(bad.x & 0x38383838u, bad.y & 0x38383838u), sees[0], hits, 0, 0, 0);
-                hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_operand(bad.z & 0x38383838u, bad.w & 0x38383838u), sees[1], hits, 0, 0, 0);
+            const uint4 both = v(dt);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) to.acc[dt][j] = hits[j] > 0.f ? __builtin_nanf("") : to.acc[dt][j];
-                w = make_uint4(w.x & ~bad.x, w.y & ~bad.y, w.z & ~bad.z, w.w & ~bad.w);
-            }
-            const bf16x8 v0 = codes_to_operand(w.x, w.y), v1 = codes_to_operand(w.z, w.w);
+            for (int half = 0; half < 2; ++half) {
+                uint2 w = half ? make_uint2(both.z, both.w) : make_uint2(both.x, both.y);
+                w = make_uint2(w.x & keep[half][0], w.y & keep[half][1]);
+                const uint2 bad = make_uint2(nan_bytes(w.x), nan_bytes(w.y));
+                if (__ballot((bad.x | bad.y) != 0)) {   // the code 1.0 (0x38) in the place of each NaN
+                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_operand(bad.x & 0x38383838u, bad.y & 0x38383838u), sees[half], hits, 0, 0, 0);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, __builtin_bit_cast(bf16x8, prob[0][p]), to.acc[dt], 0, 0, 0);
-                to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, __builtin_bit_cast(bf16x8, prob[1][p]), to.acc[dt], 0, 0, 0);
+                    for (int j = 0; j < 4; ++j) to.acc[dt][j] = hits[j] > 0.f ? __builtin_nanf("") : to.acc[dt][j];
+                    w = make_uint2(w.x & ~bad.x, w.y & ~bad.y);
+                }
+                const bf16x8 value = codes_to_operand(w.x, w.y);
+#pragma unroll
+                for (int pl = 0; pl < NP; ++pl)
+                    to.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, __builtin_bit_cast(bf16x8, prob[half][pl]), to.acc[dt], 0, 0, 0);
             }
         }
+        if constexpr (DP > 64) { if (dt & 1) __builtin_amdgcn_sched_barrier(0); }
     }
 }
 
@@ -401,9 +425,13 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const AttnPlace& p, c
     }
 }
 
-template <int TYPE, int DP> constexpr int kFewLds = (4 * 16 * (DP + 4) * 4 > kPlanes<TYPE> * DP * 32 ? 4 * 16 * (DP + 4) * 4 : kPlanes<TYPE> * DP * 32);
+template <int TYPE, int DP, int MT> constexpr int kQueriesLds = kPlanes<TYPE> * MT * DP * 32;
+template <int DP, int SUMS> constexpr int kSumsLds = SUMS * 16 * (DP + 4) * 4;
+constexpr int larger(int a, int b) { return a > b ? a : b; }
 
-// grid = (sentences or rows) * heads * groups * splits workgroups of four waves; D <= DP, EXACT: D == DP.
+template <int TYPE, int DP> constexpr int kFewLds = larger(kQueriesLds<TYPE, DP, 1>, kSumsLds<DP, 4>);
+
+// grid = heads * groups * sets * splits workgroups of four waves; D <= DP, EXACT: D == DP.
 template <int TYPE, int DP, bool EXACT>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArgs a) {
     constexpr int KK = DP / 64, DT = DP / 16, PITCH = DP + 4;
@@ -411,17 +439,29 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
     __shared__ AttnShared sh;
     __shared__ float wave_m[4][16], wave_l[4][16];
     const int ln = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), n16 = ln & 15, c = ln >> 4, pieces = a.D >> 4;
-    const AttnPlace p = attn_place<16>(a, sh);
+    AttnPlace p = attn_place(a);
+    Queries<TYPE, DP, 1, 256> queries;
+    queries.ask(a, p);
+    // without a window the first tile is known before the lengths are
+    const int64_t tile_guess = p.shared_tokens / kAttnTile * (a.common ? 0 : 1) + (int64_t)p.split * a.chunk;
+    const int table_guess = p.table_row;
+    int32_t entry = table_entry(a, p.table_row, tile_guess * kAttnTile + 16 * threadIdx.x);
+    AttnRow row = attn_row(a, p.sr, p.h, p.group * 16 + n16);
+    find_positions(a, p, row);
+    if (threadIdx.x < 16) sh.row[threadIdx.x] = row;
+    const int lo = row.lo, hi = row.hi;
     RowSums<DP> sums;
     const bool some = p.split < p.chunks;
-    if (some) stage_queries<TYPE, DP, 1>(a, sh, lds, 256);
-    const int lo = sh.row[n16].lo, hi = sh.row[n16].hi;
+    if (some) queries.put(lds);
     const int64_t head_bytes = (int64_t)a.block * a.D;
-    for (int chunk = p.split; chunk < p.chunks; chunk += a.splits) {
-        if (chunk != p.split) __syncthreads();
-        load_chunk(a, sh, p, chunk);
+    const int last = min(p.tiles, (p.split + 1) * p.chunk);
+    for (int rel0 = p.split * p.chunk; rel0 < last; rel0 += kLookup) {
+        const int n = min(kLookup, last - rel0);
+        if (rel0 != p.split * p.chunk) __syncthreads();
+        if (p.tile0 + rel0 != tile_guess || p.table_row != table_guess)
+            entry = table_entry(a, p.table_row, ((int64_t)p.tile0 + rel0) * kAttnTile + 16 * threadIdx.x);
+        put_lookup(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
         __syncthreads();
-        const int rel0 = chunk * a.chunk, n = min(a.chunk, p.tiles - rel0);
         uint4 kw[KK][4], vw[DT];
         auto load_k = [&](int rel) {
             const int group = n16 >> 2, in_block = ((p.tile0 + rel0 + rel) * kAttnTile + 16 * group) & (a.block - 1);
@@ -443,13 +483,15 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
                 for (int dt = 0; dt < DT; ++dt)
                     if (EXACT || dt < pieces) vw[dt] = *reinterpret_cast<const uint4*>(at + dt * 256);
             }
-            attend_tile<TYPE, DP, 1, EXACT>(a, sh, lds, 0, rel, (p.tile0 + rel0 + rel) * kAttnTile, lo, hi, sums,
-                                            [&](int kk, int i) { return kw[kk][i]; }, [&](int dt) { return vw[dt]; },
+            attend_tile<TYPE, DP, EXACT>(a, p, sh, rel, (p.tile0 + rel0 + rel) * kAttnTile, lo, hi, sums,
+                                            [&](int pl, int kk, int half) { return lds[((pl * KK + kk) * 2 + half) * 64 + ln]; },
+                                            [&](int kk, int i) { return kw[kk][i]; },
+                                            [&](int dt) { return vw[dt]; },
                                             [&] { if (rel + 4 < n) load_k(rel + 4); });
         }
     }
     // the four waves' results together
-    const bool live = sh.row[n16].lo != INT32_MIN;
+    const bool live = lo != INT32_MIN;
     sums.l += __shfl_xor(sums.l, 16, kWave);
     sums.l += __shfl_xor(sums.l, 32, kWave);
     if (c == 0) { wave_m[wv][n16] = live ? sums.m : -INFINITY; wave_l[wv][n16] = live ? sums.l : 0.f; }
@@ -463,45 +505,68 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
     }
     const int quads = a.D >> 2;
     for (int e = threadIdx.x; e < 16 * quads; e += 256) {
-        const int row = e / quads, d = 4 * (e - row * quads);
-        if (!sh.row[row].valid) continue;
-        const float top = fmaxf(fmaxf(wave_m[0][row], wave_m[1][row]), fmaxf(wave_m[2][row], wave_m[3][row]));
+        const int at = (int)((unsigned)e / (unsigned)quads), d = 4 * (e - at * quads);
+        if (!sh.row[at].valid) continue;
+        const float top = fmaxf(fmaxf(wave_m[0][at], wave_m[1][at]), fmaxf(wave_m[2][at], wave_m[3][at]));
         float sum = 0.f;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float m = wave_m[w][row], l = wave_l[w][row];
+            const float m = wave_m[w][at], l = wave_l[w][at];
             if (l == 0.f) continue;                      // (nothing, or not this row)
             const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 1.f;   // (no maximum: nothing but NaN, which stays)
             sum += l * f;
-            v += *reinterpret_cast<const f32x4*>(red + (w * 16 + row) * PITCH + d) * f;
+            v += *reinterpret_cast<const f32x4*>(red + (w * 16 + at) * PITCH + d) * f;
         }
-        put_row<TYPE>(a, p, sh.row[row], d, v, top, sum);
+        put_row<TYPE>(a, p, sh.row[at], d, v, top, sum);
     }
 }
 
 template <int DP> constexpr int kRowsStages = DP > 128 ? 2 : 3;
-template <int TYPE, int DP, int MT> constexpr int kRowsLds = kRowsStages<DP> * DP * 128 + kPlanes<TYPE> * MT * DP * 32;
+template <int TYPE, int DP, int MT> constexpr int kRowsLds = kRowsStages<DP> * DP * 128 + kQueriesLds<TYPE, DP, MT>;
 
-// The same grid, MT waves: wave w has rows 16 w .. 16 w + 15 of the group.
+// The same grid, MT waves: wave w has rows 16 w .. 16 w + 15 of the group.  Bound by how many workgroups a CU holds and by what each of
+// them does one thing after the other (about 1.3 us a tile): 16 sentences of 12 beams over 8000 common tokens of 8 heads, D = 128, bf16, 264 MB
+// in 80 us.  Measured and not kept: two waves per 16 rows, each for half the tokens (108 us); queries in registers and a third
+// workgroup on a CU (81); all rows in each wave and tiles in registers as above (some 500 registers, which do not last).
 template <int TYPE, int DP, int MT, bool EXACT>
 __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
-    constexpr int DT = DP / 16, STAGES = kRowsStages<DP>, TILE = 2 * DT * 64;   // uint4 of a tile: keys [kk, i, lane], values [dt, lane]
-    constexpr int LOADS = (2 * DT + MT - 1) / MT;                               // of a wave for a tile, 1 KB each
-    extern __shared__ uint4 lds[];
+    constexpr int KK = DP / 64, DT = DP / 16, STAGES = kRowsStages<DP>, TILE = 2 * DT * 64;   // uint4 of a tile: keys [kk, i, lane], values [dt, lane]
+    constexpr int LOADS = (2 * DT + MT - 1) / MT;                                             // of a wave for a tile, 1 KB each
+    extern __shared__ uint4 lds[];                       // tiles [stage, TILE], queries as operands
     uint4* queries = lds + STAGES * TILE;
     __shared__ AttnShared sh;
     const int ln = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), n16 = ln & 15, c = ln >> 4, pieces = a.D >> 4;
-    const AttnPlace p = attn_place<16 * MT>(a, sh);
+    AttnPlace p = attn_place(a);
     RowSums<DP> sums;
-    if (p.split < p.chunks) stage_queries<TYPE, DP, MT>(a, sh, queries, 64 * MT);
-    const AttnRow row = sh.row[16 * wv + n16];
+    const int64_t tile_guess = p.shared_tokens / kAttnTile * (a.common ? 0 : 1) + (int64_t)p.split * a.chunk;
+    const int table_guess = p.table_row;
+    int32_t entry;
+    AttnRow row;
+    {
+        Queries<TYPE, DP, MT, 64 * MT> q;
+        q.ask(a, p);
+        entry = table_entry(a, p.table_row, tile_guess * kAttnTile + 16 * threadIdx.x);
+        row = attn_row(a, p.sr, p.h, ln < 16 * MT ? p.group * 16 * MT + ln : INT32_MAX);
+        find_positions(a, p, row);
+        const int from = 16 * wv + n16;                  // the lane's own row of those
+        row.r = __shfl(row.r, from, kWave);
+        row.t = __shfl(row.t, from, kWave);
+        row.head = __shfl(row.head, from, kWave);
+        row.lo = __shfl(row.lo, from, kWave);
+        row.hi = __shfl(row.hi, from, kWave);
+        row.valid = __shfl((int)row.valid, from, kWave) != 0;
+        if (p.split < p.chunks) q.put(queries);
+    }
     const int64_t head_bytes = (int64_t)a.block * a.D;
-    for (int chunk = p.split; chunk < p.chunks; chunk += a.splits) {
-        if (chunk != p.split) __syncthreads();
-        load_chunk(a, sh, p, chunk);
+    const int last = min(p.tiles, (p.split + 1) * p.chunk);
+    for (int rel0 = p.split * p.chunk; rel0 < last; rel0 += kLookup) {
+        const int n = min(kLookup, last - rel0);
+        if (rel0 != p.split * p.chunk) __syncthreads();
+        if (p.tile0 + rel0 != tile_guess || p.table_row != table_guess)
+            entry = table_entry(a, p.table_row, ((int64_t)p.tile0 + rel0) * kAttnTile + 16 * threadIdx.x);
+        put_lookup(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
         __syncthreads();
-        const int rel0 = chunk * a.chunk, n = min(a.chunk, p.tiles - rel0);
         // every wave asks for LOADS kilobytes of a tile, the last of them twice where they do not come out even
         auto ask = [&](int rel) {
             const int group = n16 >> 2, base = (p.tile0 + rel0 + rel) * kAttnTile;
@@ -531,21 +596,23 @@ __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
             lds_barrier();
             if (rel + STAGES - 1 < n) ask(rel + STAGES - 1);
             const uint4* stage = lds + (rel % STAGES) * TILE;
-            attend_tile<TYPE, DP, MT, EXACT>(a, sh, queries, wv, rel, (p.tile0 + rel0 + rel) * kAttnTile, row.lo, row.hi, sums,
-                                             [&](int kk, int i) {
-                                                 const uint4 w = stage[(kk * 4 + i) * 64 + ln];
-                                                 return EXACT || c + 4 * kk < pieces ? w : make_uint4(0, 0, 0, 0);
-                                             },
-                                             [&](int dt) { return stage[(DT + dt) * 64 + ln]; }, [] {});
+            attend_tile<TYPE, DP, EXACT>(a, p, sh, rel, (p.tile0 + rel0 + rel) * kAttnTile, row.lo, row.hi, sums,
+                                         [&](int pl, int kk, int half) { return queries[(((pl * MT + wv) * KK + kk) * 2 + half) * 64 + ln]; },
+                                         [&](int kk, int i) {
+                                             const uint4 w = stage[(kk * 4 + i) * 64 + ln];
+                                             return EXACT || c + 4 * kk < pieces ? w : make_uint4(0, 0, 0, 0);
+                                         },
+                                         [&](int dt) { return stage[(DT + dt) * 64 + ln]; }, [] {});
         }
     }
     if (!row.valid) return;
     const bool live = row.lo != INT32_MIN;
-    sums.l += __shfl_xor(sums.l, 16, kWave);
-    sums.l += __shfl_xor(sums.l, 32, kWave);
+    float l = sums.l;
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-        if (EXACT || dt < pieces) put_row<TYPE>(a, p, row, dt * 16 + 4 * c, sums.acc[dt], live ? sums.m : -INFINITY, live ? sums.l : 0.f);
+        if (EXACT || dt < pieces) put_row<TYPE>(a, p, row, dt * 16 + 4 * c, sums.acc[dt], live ? sums.m : -INFINITY, live ? l : 0.f);
 }
 
 // A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.
@@ -570,11 +637,11 @@ __global__ void __launch_bounds__(256) k_attention_join(AttnArgs a) {
         sum = sum * was + wave_sum_f32(p.y * f);
         v *= was;
         const int n = min(a.parts - i0, kWave);
-        for (int j = 0; j < n; j += 4 * sides) {
-            f32x4 x[4];
-            float g[4];
+        for (int j = 0; j < n; j += 8 * sides) {
+            f32x4 x[8];
+            float g[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 8; ++q) {
                 const int part = j + q * sides + side;
                 g[q] = __shfl(f, min(part, kWave - 1), kWave);
                 const bool some = part < n && g[q] != 0.f && d < a.D;   // (a NaN is some)
@@ -582,7 +649,7 @@ __global__ void __launch_bounds__(256) k_attention_join(AttnArgs a) {
                 if (some) x[q] = *reinterpret_cast<const f32x4*>(acc + (int64_t)(i0 + part) * a.D);
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 8; ++q) {
                 const bool some = j + q * sides + side < n && g[q] != 0.f;
                 v += some ? x[q] * g[q] : f32x4{0.f, 0.f, 0.f, 0.f};
             }

@@ -90,7 +90,7 @@ bool attention_ok(const lsh_cache_params* c, const lsh_attention_params* p) {
 // for each row by itself, which a third joins if there is more than one part of a row.
 struct AttnLaunch {
     int row_tiles;      // 1: k_attention_few, else the waves of k_attention_rows
-    int chunk;          // tiles of 64 tokens
+    int chunk;          // tiles of 64 tokens at least
     int groups, splits;
     int64_t units;      // workgroups; 0: no such launch
 };
@@ -99,16 +99,15 @@ struct AttnPlan {
     size_t acc, bytes;  // where the parts' products begin in the workspace; its size
 };
 // sets: pairs of a row set and a head; tiles: of a row at most -- what a row has is known on the device only, and a chunk behind its
-// last tile costs little.  Short chunks where there is little to do, longer ones where the chip is full: a workgroup's begin and end
-// are worth some tiles.
+// last tile costs little.  A chunk has four tiles at least (eight of k_attention_rows: what a workgroup's begin and end are worth),
+// more where a row would have more chunks than workgroups.
 AttnLaunch attention_launch(int64_t rows, int64_t sets, int64_t tiles, int64_t most_splits) {
     AttnLaunch w{};
     w.groups = (int)ceil_div(rows, 64);
     w.row_tiles = (int)ceil_div(ceil_div(rows, w.groups), 16);
     sets *= w.groups;
-    w.chunk = 4;
-    while (w.chunk < kMaxChunk && sets * ceil_div(tiles, w.chunk) > 128 * w.chunk + (w.row_tiles > 1 ? 768 : 0)) w.chunk *= 2;
-    w.splits = (int)std::min({ceil_div(tiles, w.chunk), std::max<int64_t>(1, 4096 / sets), most_splits});
+    w.chunk = w.row_tiles > 1 ? 8 : 4;
+    w.splits = (int)std::min({ceil_div(tiles, w.chunk), std::max<int64_t>(1, (w.row_tiles > 1 ? 1024 : 2048) / sets), most_splits});
     w.units = sets * w.splits;
     return w;
 }
@@ -117,10 +116,11 @@ AttnPlan attention_plan(const lsh_cache_params* c, const lsh_attention_params* p
     const int64_t R = (int64_t)c->S * c->B, per_row = (int64_t)p->T * (p->n_heads / c->n_heads);
     int64_t tiles = ceil_div((int64_t)c->max_blocks * c->block, kAttnTile);
     if (p->window > 0) tiles = std::min(tiles, ceil_div((int64_t)p->window + p->T, kAttnTile) + 1);
-    const bool common = shared && c->B > 1;
+    // beams together where it saves reading more than two launches more cost: 32 MB
+    const bool common = shared && c->B > 1 && R * c->n_heads * tiles * kAttnTile * 2 * c->head_dim > (int64_t)32 << 20;
     if (common) w.common = attention_launch(c->B * per_row, (int64_t)c->S * c->n_heads, tiles, INT32_MAX);
     // (beams' own tokens are few, and whatever there is of them goes round the workgroups)
-    w.own = attention_launch(per_row, R * c->n_heads, tiles, common ? std::max<int64_t>(1, 1024 / (R * c->n_heads)) : INT32_MAX);
+    w.own = attention_launch(per_row, R * c->n_heads, tiles, common ? std::max<int64_t>(1, 512 / (R * c->n_heads)) : INT32_MAX);
     const size_t parts = (size_t)(w.common.splits + w.own.splits), at = (size_t)R * p->T * p->n_heads * (parts > 1 ? parts : 0);
     w.acc = round_up(at * sizeof(float2));
     w.bytes = std::max<size_t>(256, w.acc + round_up(at * c->head_dim * sizeof(float)));
@@ -292,6 +292,7 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
             const AttnLaunch& w = own ? plan.own : plan.common;
             if (w.units == 0) continue;
             a.common = !own;
+            a.sets = own ? c->S * c->B : c->S;
             a.chunk = w.chunk; a.groups = w.groups; a.splits = w.splits;
             a.part0 = own ? plan.common.splits : 0;
             const int D = c->head_dim;

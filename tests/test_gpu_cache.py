@@ -256,13 +256,18 @@ def test_several_tokens(T, group, window, causal, dtype):
     check_attention(rng, cp, pool, ref, tables, lengths, dtype, T, 2 * group, causal, window, n_new=n_new)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("S,B,group,T", [(1, 4, 1, 1), (2, 12, 4, 1), (3, 5, 3, 2), (1, 40, 2, 1), (2, 3, 8, 9), (1, 2, 32, 1)])
-def test_beams_that_share_blocks(S, B, group, T, dtype):
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("S,B,group,T,width", [(1, 4, 1, 1, None), (1, 4, 1, 1, 8000), (2, 12, 4, 1, 8000), (3, 5, 3, 2, 4000), (1, 40, 2, 1, 1000),
+                                               (2, 3, 8, 9, 8000), (1, 2, 32, 1, 16000), (2, 2, 2, 1, 9000)])
+def test_beams_that_share_blocks(S, B, group, T, width, dtype):
+    """Beams go together where the tables have room for so many tokens that it pays (their width, not what the rows have)."""
     rng = np.random.default_rng(S + B)
     common = [int(c) for c in rng.integers(0, 40, S) * 16]
     lengths = np.array([c + int(x) for c in common for x in rng.integers(0, 90, B)])
-    cp, pool, ref, tables, lengths = scene(rng, S, B, lengths, 16, 2, 64, common)
+    cp, pool, ref, tables, lengths = scene(rng, S, B, lengths, 16, 2, 64, common, width=width)
+    from paper_1806_00588_amd import binding
+    two = binding.attention_workspace_bytes(cp, binding.attention_params(T, 2 * group, 1.0))
+    assert two > 256 or width is None          # (a workspace for the parts of both launches)
     whole = np.array(common) // 16
     for r in range(S * B):
         whole[r // B] = min(whole[r // B], lengths[r] // 16)
@@ -277,6 +282,15 @@ def test_beams_that_share_blocks(S, B, group, T, dtype):
     dead, dead_tables = lengths.copy(), tables.copy()
     dead[::B], dead_tables[::B] = 0, -1        # the first of each sentence
     check_attention(rng, cp, pool, ref, dead_tables, dead, dtype, T, 2 * group, shared=whole)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_beams_over_a_long_prompt(dtype):
+    """More tiles than are looked up at a time, in both launches; D as the kernels have it and not."""
+    rng = np.random.default_rng(3)
+    for D, group in ((64, 1), (128, 6), (80, 6), (256, 6), (192, 2)):
+        cp, pool, ref, tables, lengths = scene(rng, 1, 4, [6400 + 100 * i for i in range(4)], 32, 1, D, [2400], width=9000)
+        check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, group, shared=np.array([75]))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
@@ -318,7 +332,7 @@ def test_what_is_not_seen_does_not_reach_a_result(T, dtype):
 
 def test_a_nan_reaches_whoever_sees_it():
     rng = np.random.default_rng(7)
-    cp, pool, ref, tables, lengths = scene(rng, 2, 3, [70] * 6, 16, 2, 64, [64, 64])
+    cp, pool, ref, tables, lengths = scene(rng, 2, 3, [70] * 6, 16, 2, 64, [64, 64], width=4000)
     ref.v[tables[1, 1], 1, 3, 17] = 127        # a shared block: all beams of the first sentence, one head, one value
     ref.k[tables[4, 4], 0, 2, 5] = 127         # a beam's own block: one row, one head, all values
     for shared in (None, np.array([4, 4])):
@@ -368,7 +382,7 @@ def test_streams_graphs_and_the_same_bits():
     import torch
     from paper_1806_00588_amd import binding
     rng = np.random.default_rng(10)
-    cp, pool, ref, tables, lengths = scene(rng, 2, 6, [700 + i for i in range(12)], 16, 2, 64, [640, 512])
+    cp, pool, ref, tables, lengths = scene(rng, 2, 6, [700 + i for i in range(12)], 16, 2, 64, [640, 512], width=2000)
     shared = np.array([40, 32])
     side = torch.cuda.Stream()
     q = rng.standard_normal((12, 1, 8, 64))
