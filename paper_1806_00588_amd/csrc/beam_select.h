@@ -61,35 +61,55 @@ template <int TYPE> __device__ __forceinline__ float word_f32(typename WordOf<TY
     else return __half2float(__ushort_as_half(v));
 }
 
-// Logits of words w .. w + 7 of a row (w < V; -inf behind the row's end and where the word is not allowed).  Rows may begin at any element.
-template <int TYPE>
-__device__ __forceinline__ void load_words(const SelArgs& a, int64_t r, int w, float (&x)[kSelWords]) {
+// Logits of words w .. w + 7 of a row as they lie in memory, and which of them count: those inside the row that are allowed.  Rows
+// may begin at any element.
+template <int TYPE> struct Words {
     using T = typename WordOf<TYPE>::type;
-    const T* p = static_cast<const T*>(a.x) + r * a.ld + w;
-    if (w + kSelWords <= a.V) {
-        if constexpr (TYPE == kTypeF32) {
+    uint32_t w[TYPE == kTypeF32 ? 8 : 4];
+    uint32_t bits;
+    __device__ __forceinline__ void load(const SelArgs& a, int64_t r, int at) {
+        bits = 0;
+        if (at >= a.V) return;
+        const T* p = static_cast<const T*>(a.x) + r * a.ld + at;
+        bits = 0xffu;
+        if (a.allowed) bits = a.allowed[r * a.allowed_pitch + (at >> 3)];
+        if (at + kSelWords <= a.V) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const Float4U v = *reinterpret_cast<const Float4U*>(p + 4 * i);
-                x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+            for (int h = 0; h < (TYPE == kTypeF32 ? 2 : 1); ++h) {
+                const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(p + 4 * h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[4 * h + i] = v.w[i];
             }
         } else {
-            const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(p);
+            bits &= 0xffu >> (at + kSelWords - a.V);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = word_f32<TYPE>((T)(v.w[i] & 0xffffu));
-                x[2 * i + 1] = word_f32<TYPE>((T)(v.w[i] >> 16));
+            for (int i = 0; i < kSelWords; ++i) {
+                const uint32_t v = at + i < a.V ? (uint32_t)word_bits(p[i]) : 0u;
+                if constexpr (TYPE == kTypeF32) w[i] = v;
+                else w[i >> 1] = i & 1 ? w[i >> 1] | v << 16 : v;
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kSelWords; ++i) x[i] = w + i < a.V ? word_f32<TYPE>(p[i]) : -INFINITY;
     }
-    if (a.allowed) {
-        const uint32_t bits = a.allowed[r * a.allowed_pitch + (w >> 3)];
+    static __device__ __forceinline__ uint32_t word_bits(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ uint32_t word_bits(uint16_t v) { return v; }
+    // ... as fp32, -inf where they do not count
+    __device__ __forceinline__ void get(float (&x)[kSelWords]) const {
 #pragma unroll
-        for (int i = 0; i < kSelWords; ++i) x[i] = (bits >> i & 1u) ? x[i] : -INFINITY;
+        for (int i = 0; i < kSelWords; ++i) {
+            if constexpr (TYPE == kTypeF32) x[i] = __uint_as_float(w[i]);
+            else x[i] = word_f32<TYPE>((T)(w[i >> 1] >> (16 * (i & 1)) & 0xffffu));
+        }
+        if (bits != 0xffu) {
+#pragma unroll
+            for (int i = 0; i < kSelWords; ++i) x[i] = bits >> i & 1u ? x[i] : -INFINITY;
+        }
     }
+};
+template <int TYPE>
+__device__ __forceinline__ void load_words(const SelArgs& a, int64_t r, int at, float (&x)[kSelWords]) {
+    Words<TYPE> w;
+    w.load(a, r, at);
+    w.get(x);
 }
 
 __device__ __forceinline__ float max_of(const float (&x)[kSelWords]) {   // (a NaN is not the largest; it shows in the sum)
@@ -114,31 +134,35 @@ template <int TYPE>
 __global__ void __launch_bounds__(256) k_select_tiles(SelArgs a) {
     const int per_row = (a.parts + 3) >> 2;
     const int64_t r = blockIdx.x / per_row;
-    const int part = (blockIdx.x - (int)r * per_row) * 4 + wave_id();
+    const int part = (blockIdx.x - (int)r * per_row) * 4 + __builtin_amdgcn_readfirstlane(wave_id());
     if (part >= a.parts) return;
     const int ln = lane_id();
     const int n_pieces = (a.V + kSelPiece - 1) / kSelPiece;
     const int end = min(n_pieces, (part + 1) * a.pieces);
     float m = -INFINITY;
     double sum = 0.0;
+    Words<TYPE> next[kSelBatch];
+    auto ask = [&](int p) {
+#pragma unroll
+        for (int i = 0; i < kSelBatch; ++i)
+            if (p + i < end) next[i].load(a, r, (p + i) * kSelPiece + ln * kSelWords);
+    };
+    ask(part * a.pieces);
     for (int p = part * a.pieces; p < end; p += kSelBatch) {
-        float x[kSelBatch][kSelWords], top[kSelBatch];
+        Words<TYPE> now_[kSelBatch];
 #pragma unroll
-        for (int i = 0; i < kSelBatch; ++i) {
-            const int w = (p + i) * kSelPiece + ln * kSelWords;
-            if (p + i < end && w < a.V) load_words<TYPE>(a, r, w, x[i]);
-            else {
-#pragma unroll
-                for (int j = 0; j < kSelWords; ++j) x[i][j] = -INFINITY;
-            }
-        }
+        for (int i = 0; i < kSelBatch; ++i) now_[i] = next[i];
+        ask(p + kSelBatch);              // (while these are worked on)
         float now = m;
 #pragma unroll
         for (int i = 0; i < kSelBatch; ++i) {
-            top[i] = row16_max(max_of(x[i]));
-            now = fmaxf(now, top[i]);
+            if (p + i >= end) continue;
+            float x[kSelWords];
+            now_[i].get(x);
+            const float top = row16_max(max_of(x));
+            now = fmaxf(now, top);
             const int t = (p + i) * 4 + (ln >> 4);
-            if ((ln & 15) == 0 && p + i < end && t < a.tiles) a.tile_max[r * a.tiles + t] = top[i];
+            if ((ln & 15) == 0 && t < a.tiles) a.tile_max[r * a.tiles + t] = top;
         }
         now = wave_max_f32(now);
         if (now > m) {
@@ -146,7 +170,12 @@ __global__ void __launch_bounds__(256) k_select_tiles(SelArgs a) {
             m = now;
         }
 #pragma unroll
-        for (int i = 0; i < kSelBatch; ++i) sum += (double)sum_exp(x[i], m);
+        for (int i = 0; i < kSelBatch; ++i) {
+            if (p + i >= end) continue;
+            float x[kSelWords];
+            now_[i].get(x);
+            sum += (double)sum_exp(x, m);
+        }
     }
     sum = wave_sum_f64(sum);
     if (ln == 0) a.part[r * a.parts + part] = SelPart{sum, m, 0.f};
@@ -170,11 +199,13 @@ __device__ __forceinline__ uint32_t pair_of(int beam, int word) { return (uint32
 struct SelShared {
     double off[256];                    // of each beam: score - log of the sum of exp(x - top), ...
     float top[256];                     // ... its largest logit
+    float rough[256];                   // off in 32 bits
     uint64_t key[kSelListed];
     uint32_t pair[kSelListed];
     uint32_t tile[kSelListed];
     uint32_t hist[256];
     uint32_t wsum[kSelThreads / kWave + 1];
+    float wave_best[kSelThreads / kWave];
     uint32_t n_tiles, n_words, digit, need, above;
 };
 
@@ -216,6 +247,45 @@ __device__ __forceinline__ uint64_t nth_of_threads(SelShared& sh, uint64_t key, 
     return prefix;
 }
 
+// The score in 32 bits, -inf where there is none.  It errs by 2^-23 of the largest of its parts.
+__device__ __forceinline__ float rough_score(const SelShared& sh, int b, float x) {
+    const float f = sh.rough[b] + (x - sh.top[b]);
+    return fabsf(f) < INFINITY ? f : -INFINITY;
+}
+
+// Which scores can be among the N best, given that each thread knows the rough score of a word of its own (-inf: none): at least N of
+// the threads' scores are let in, and few more.  Scores are told apart by their distance from the best, in sixteenths; one sixteenth
+// more than needed is let in, which is far more than rough scores err by as long as the best is below 2^15 (no row's off is above
+// the best, so that what is let in has no large parts).  Where it is not, or the N-th is 16 and more away, `none` says so.
+// All threads call it; it ends with a barrier.
+struct SelLimit {
+    float best, width;
+    bool none;
+    __device__ __forceinline__ bool lets(float f) const { return (best - f) * 16.f < width; }
+};
+__device__ __forceinline__ SelLimit limit_of_threads(SelShared& sh, float f, int N) {
+    const float top = wave_max_f32(f);
+    if (lane_id() == 0) sh.wave_best[wave_id()] = top;
+    if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
+    __syncthreads();
+    SelLimit to{row16_max(sh.wave_best[lane_id() & 15]), 0.f, true};
+    const float d = (to.best - f) * 16.f;
+    if (d < 256.f) atomicAdd(&sh.hist[(int)d], 1u);   // (-inf - -inf is NaN: not counted)
+    __syncthreads();
+    // lane l of every wave: bins 4 l .. 4 l + 3
+    const uint32_t* h = sh.hist + 4 * lane_id();
+    const uint32_t c0 = h[0], c1 = h[1], c2 = h[2], c3 = h[3], incl = wave_incl_scan(c0 + c1 + c2 + c3), before = incl - (c0 + c1 + c2 + c3);
+    const uint64_t here = __ballot(before < (uint32_t)N && incl >= (uint32_t)N);
+    if (here && fabsf(to.best) < 32768.f) {
+        int b = 4 * lane_id();
+        if (before + c0 < (uint32_t)N) { ++b; if (before + c0 + c1 < (uint32_t)N) { ++b; if (before + c0 + c1 + c2 < (uint32_t)N) ++b; } }
+        to.width = (float)((int)wave_read_lane((uint32_t)b, __builtin_ctzll(here)) + 2);
+        to.none = false;
+    }
+    __syncthreads();
+    return to;
+}
+
 // The row's lse from its parts, by a wave; also its offset in shared memory.
 __device__ __forceinline__ void row_offset(const SelArgs& a, SelShared& sh, int64_t r, int b, const SelPart* part, int parts) {
     const int ln = lane_id();
@@ -232,24 +302,46 @@ __device__ __forceinline__ void row_offset(const SelArgs& a, SelShared& sh, int6
         const double lg = log(sum);      // (of nothing: -inf)
         sh.off[b] = (double)a.scores[r] - lg;
         sh.top[b] = m;
+        sh.rough[b] = (float)sh.off[b];
         if (a.out_lse) a.out_lse[r] = (float)(m > -INFINITY ? (double)m + lg : lg);
     }
 }
 
-// The N best of sh.key / sh.pair [n], n <= kSelListed, to the outputs of sentence s; empty places behind them.
+// The N best of sh.key / sh.pair [n], n <= kSelListed, to the outputs of sentence s; empty places behind them.  A word's rank is how
+// many are before it: lane j of every wave holds words j and j + 64, a ballot for each word that the wave ranks (a thread for each word
+// and a loop over the others waited for LDS in every turn).
 __device__ __forceinline__ void rank_words(const SelArgs& a, SelShared& sh, int s, int n) {
-    for (int e = threadIdx.x; e < n; e += kSelThreads) {
-        const uint64_t k = sh.key[e];
-        const uint32_t p = sh.pair[e];
-        int rank = 0;
-        for (int o = 0; o < n; ++o) rank += sh.key[o] > k || (sh.key[o] == k && sh.pair[o] < p);
-        if (rank < a.N) {
-            const size_t at = (size_t)s * a.N + rank;
-            a.out_beam[at] = (int32_t)(p >> 24);
-            a.out_word[at] = (int32_t)(p & 0xffffffu);
-            a.out_score[at] = key_score(k);
-        }
+    const int ln = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    constexpr int kWaves = kSelThreads / kWave;
+    uint64_t k[2];
+    uint32_t p[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const bool in = ln + kWave * h < n;
+        k[h] = in ? sh.key[ln + kWave * h] : 0;
+        p[h] = in ? sh.pair[ln + kWave * h] : 0xffffffffu;
     }
+    auto rank_one = [&](uint64_t key, uint32_t pair) {
+        int rank = __popcll(__ballot(k[0] > key || (k[0] == key && p[0] < pair)));
+        if (n > kWave) rank += __popcll(__ballot(k[1] > key || (k[1] == key && p[1] < pair)));
+        for (int o = 2 * kWave; o < n; o += kWave) {
+            const bool in = o + ln < n;
+            const uint64_t ko = in ? sh.key[o + ln] : 0;
+            const uint32_t po = in ? sh.pair[o + ln] : 0xffffffffu;
+            rank += __popcll(__ballot(ko > key || (ko == key && po < pair)));
+        }
+        if (ln == 0 && rank < a.N) {
+            const size_t at = (size_t)s * a.N + rank;
+            a.out_beam[at] = (int32_t)(pair >> 24);
+            a.out_word[at] = (int32_t)(pair & 0xffffffu);
+            a.out_score[at] = key_score(key);
+        }
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        for (int e = wv; e < kWave && e + kWave * h < n; e += kWaves)
+            rank_one((uint64_t)wave_read_lane((uint32_t)(k[h] >> 32), e) << 32 | wave_read_lane((uint32_t)k[h], e), wave_read_lane(p[h], e));
+    for (int e = 2 * kWave + wv; e < n; e += kWaves) rank_one(sh.key[e], sh.pair[e]);
     for (int i = n + threadIdx.x; i < a.N; i += kSelThreads) {
         const size_t at = (size_t)s * a.N + i;
         a.out_beam[at] = -1;
@@ -263,7 +355,7 @@ __device__ __forceinline__ void rank_words(const SelArgs& a, SelShared& sh, int 
 // beam and word as far as there is room.
 template <int TYPE>
 __device__ __forceinline__ void select_all_words(const SelArgs& a, SelShared& sh, int s) {
-    const int wv = wave_id(), ln = lane_id();
+    const int wv = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
     const int pieces = (a.V + kSelPiece - 1) / kSelPiece, units = a.B * pieces;
     uint64_t prefix = 0;
     uint32_t need = (uint32_t)a.N;
@@ -334,26 +426,74 @@ __device__ __forceinline__ void select_all_words(const SelArgs& a, SelShared& sh
 template <int TYPE>
 __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
     __shared__ SelShared sh;
-    const int s = blockIdx.x, wv = wave_id(), ln = lane_id();
+    const int s = blockIdx.x, wv = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
     const int64_t r0 = (int64_t)s * a.B;
+    // wave w takes 64 tiles of a row at a time, unit w, w + 16, ..., sixteen of them under way together; the first sixteen it keeps
+    constexpr int kHeld = 16, kWaves = kSelThreads / kWave;
+    const int runs = (a.tiles + kWave - 1) / kWave, units = a.B * runs;
+    const float* top = a.tile_max + r0 * a.tiles;
+    auto ask = [&](int u0, float (&x)[kHeld]) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int u = u0 + i * kWaves;
+            x[i] = -INFINITY;
+            if (u >= units) continue;
+            const int b = (int)((unsigned)u / (unsigned)runs), t = (u - b * runs) * kWave + ln;
+            if (t < a.tiles) x[i] = top[(int64_t)b * a.tiles + t];
+        }
+    };
+    float held[kHeld];
+    ask(wv, held);
     if (threadIdx.x == 0) sh.n_tiles = sh.n_words = 0;
-    for (int b = wv; b < a.B; b += kSelThreads / kWave) row_offset(a, sh, r0 + b, b, a.part + (r0 + b) * a.parts, a.parts);
+    for (int b = wv; b < a.B; b += kWaves) row_offset(a, sh, r0 + b, b, a.part + (r0 + b) * a.parts, a.parts);
     __syncthreads();
     // the threads' best tiles: N distinct tiles reach the N-th of them, and no word below can be among the N best
-    const int tiles = a.B * a.tiles;
-    const float* top = a.tile_max + r0 * a.tiles;
-    uint64_t best = 0;
-    for (int i = threadIdx.x; i < tiles; i += kSelThreads) {
-        const uint64_t k = score_key(score_of(sh, i / a.tiles, top[i]));
-        best = k > best ? k : best;
-    }
-    const uint64_t least = nth_of_threads(sh, best, a.N);
-    for (int i = threadIdx.x; i < tiles; i += kSelThreads) {
-        const uint64_t k = score_key(score_of(sh, i / a.tiles, top[i]));
-        if (k >= least) {
-            const uint32_t to = atomicAdd(&sh.n_tiles, 1u);
-            if (to < kSelListed) sh.tile[to] = (uint32_t)i;
+    float best = -INFINITY;
+    auto score = [&](int u0, float (&x)[kHeld]) {   // in the place of the maxima
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int u = u0 + i * kWaves;
+            if (u >= units) continue;
+            x[i] = rough_score(sh, (int)((unsigned)u / (unsigned)runs), x[i]);
+            best = fmaxf(best, x[i]);
         }
+    };
+    score(wv, held);
+    for (int u0 = wv + kWaves * kHeld; u0 < units; u0 += kWaves * kHeld) {
+        float x[kHeld];
+        ask(u0, x);
+        score(u0, x);
+    }
+    const SelLimit limit = limit_of_threads(sh, best, a.N);
+    auto list = [&](int u) {             // (a lane of the wave's unit u)
+        const int b = (int)((unsigned)u / (unsigned)runs), t = (u - b * runs) * kWave + ln;
+        if (t >= a.tiles) return;
+        const uint32_t to = atomicAdd(&sh.n_tiles, 1u);
+        if (to < kSelListed) sh.tile[to] = (uint32_t)(b * a.tiles + t);
+    };
+    uint64_t least = 1;
+    if (!limit.none) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (limit.lets(held[i]) && wv + i * kWaves < units) list(wv + i * kWaves);
+        for (int u0 = wv + kHeld * kWaves; u0 < units; u0 += kHeld * kWaves) {
+            float x[kHeld];
+            ask(u0, x);
+            score(u0, x);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (limit.lets(x[i]) && u0 + i * kWaves < units) list(u0 + i * kWaves);
+        }
+    } else {                             // scores far apart, huge, or fewer than N: the same by keys
+        uint64_t key = 0;
+        auto key_of = [&](int u) {
+            const int b = (int)((unsigned)u / (unsigned)runs), t = (u - b * runs) * kWave + ln;
+            return t < a.tiles ? score_key(score_of(sh, b, top[(int64_t)b * a.tiles + t])) : 0;
+        };
+        for (int u = wv; u < units; u += kWaves) { const uint64_t k = key_of(u); key = k > key ? k : key; }
+        least = nth_of_threads(sh, key, a.N);
+        for (int u = wv; u < units; u += kWaves)
+            if (key_of(u) >= least) list(u);
     }
     __syncthreads();
     const int n = (int)sh.n_tiles;
@@ -365,6 +505,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
             load_words<TYPE>(a, r0 + b, w, x);
 #pragma unroll
             for (int j = 0; j < kSelWords; ++j) {
+                if (!limit.none && !limit.lets(rough_score(sh, b, x[j]))) continue;
                 const uint64_t k = score_key(score_of(sh, b, x[j]));
                 if (k >= least) {
                     const uint32_t to = atomicAdd(&sh.n_words, 1u);
@@ -384,7 +525,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select_small(SelArgs a) {
     __shared__ SelShared sh;
     __shared__ SelPart part[kSelSmall];
     constexpr int kOwn = kSelSmall / (kSelThreads / kWave);   // pieces of a wave
-    const int s = blockIdx.x, wv = wave_id(), ln = lane_id();
+    const int s = blockIdx.x, wv = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
     const int64_t r0 = (int64_t)s * a.B;
     const int pieces = (a.V + kSelPiece - 1) / kSelPiece, units = a.B * pieces;
     float x[kOwn][kSelWords];
@@ -410,21 +551,34 @@ __global__ void __launch_bounds__(kSelThreads) k_select_small(SelArgs a) {
     __syncthreads();
     for (int b = wv; b < a.B; b += kSelThreads / kWave) row_offset(a, sh, r0 + b, b, part + b * pieces, pieces);
     __syncthreads();
-    uint64_t best = 0;
+    float lane_best[kOwn], best = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         const int u = wv + i * (kSelThreads / kWave);
-        const uint64_t k = u < units ? score_key(score_of(sh, u / pieces, max_of(x[i]))) : 0;
-        best = k > best ? k : best;
+        lane_best[i] = u < units ? rough_score(sh, u / pieces, max_of(x[i])) : -INFINITY;
+        best = fmaxf(best, lane_best[i]);
     }
-    const uint64_t least = nth_of_threads(sh, best, a.N);
+    const SelLimit limit = limit_of_threads(sh, best, a.N);
+    uint64_t least = 1;
+    if (limit.none) {
+        uint64_t key = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int u = wv + i * (kSelThreads / kWave);
+            const uint64_t k = u < units ? score_key(score_of(sh, u / pieces, max_of(x[i]))) : 0;
+            key = k > key ? k : key;
+        }
+        least = nth_of_threads(sh, key, a.N);
+    }
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         const int u = wv + i * (kSelThreads / kWave), b = min(u / pieces, a.B - 1);
         const int w = (u - b * pieces) * kSelPiece + ln * kSelWords;
+        if (u >= units || (!limit.none && !limit.lets(lane_best[i]))) continue;   // (the lane's others are no better)
 #pragma unroll
         for (int j = 0; j < kSelWords; ++j) {
-            const uint64_t k = u < units ? score_key(score_of(sh, b, x[i][j])) : 0;
+            if (!limit.none && !limit.lets(rough_score(sh, b, x[i][j]))) continue;
+            const uint64_t k = score_key(score_of(sh, b, x[i][j]));
             if (k >= least) {
                 const uint32_t to = atomicAdd(&sh.n_words, 1u);
                 if (to < kSelListed) { sh.key[to] = k; sh.pair[to] = pair_of(b, w + j); }

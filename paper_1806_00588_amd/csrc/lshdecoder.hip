@@ -50,10 +50,19 @@ bool select_ok(const lsh_select_params* p) {
 int64_t row_pieces(const lsh_select_params* p) { return ceil_div(p->V, kSelPiece); }
 bool select_is_small(const lsh_select_params* p) { return p->B * row_pieces(p) <= kSelSmall; }
 
+// Pieces of a wave of k_select_tiles: one as long as there are few waves, four (its loads are under way together) with many, more where
+// there are far more waves than the chip holds.
+int wave_pieces(const lsh_select_params* p) {
+    const int64_t R = (int64_t)p->S * p->B, all = row_pieces(p);
+    int n = 1;
+    while (n < kSelBatch && R * ceil_div(all, n) > 2048) n *= 2;
+    while (n >= kSelBatch && n < 2 * kSelBatch && R * ceil_div(all, 2 * n) >= 256 * 32) n *= 2;
+    return n;
+}
 size_t select_bytes(const lsh_select_params* p, size_t* tiles_bytes) {
     const size_t R = (size_t)p->S * p->B;
     *tiles_bytes = round_up(R * (size_t)ceil_div(p->V, kSelTile) * sizeof(float));
-    return *tiles_bytes + round_up(R * (size_t)ceil_div(row_pieces(p), kSelBatch) * sizeof(SelPart));
+    return *tiles_bytes + round_up(R * (size_t)ceil_div(row_pieces(p), wave_pieces(p)) * sizeof(SelPart));
 }
 
 // ---- cache --------------------------------------------------------------------------------------
@@ -187,9 +196,7 @@ lsh_status lsh_beam_select(const lsh_select_params* p, const void* logits_dev, c
         });
         return launched();
     }
-    // a wave takes four pieces, more where there are more waves than the chip holds at a time
-    a.pieces = kSelBatch;
-    while (a.pieces < 4 * kSelBatch && R * ceil_div(pieces, 2 * a.pieces) >= 256 * 32) a.pieces *= 2;
+    a.pieces = wave_pieces(p);
     a.parts = (int)ceil_div(pieces, a.pieces);
     const int64_t grid = R * ceil_div(a.parts, 4);
     if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;

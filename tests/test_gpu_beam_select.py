@@ -140,6 +140,19 @@ def test_ties_go_to_the_lowest_beam_and_word(B, V, N, value):
     assert np.all(gb[0, n:] == -1)
 
 
+@pytest.mark.parametrize("B,V,N", [(3, 900, 20), (4, 30000, 50), (1, 5000, 256)])
+def test_scores_far_apart_and_huge(B, V, N):
+    """The N-th best hundreds behind the best; beam scores of thousands and millions, some beams far behind the others."""
+    rng = np.random.default_rng(V)
+    x = (rng.standard_normal((2 * B, V)) * 300).astype(np.float32)
+    for low in (0.0, -30000.0, -40000.0, -3e6, -1e30):
+        bs = (low * (1 + 1e-3 * rng.random(2 * B)) - rng.random(2 * B)).astype(np.float32)
+        check(run(to_dev(x), to_dev(bs), 2, B, N), x.astype(np.float64), bs, 2, B, N)
+    bs = np.float32([0.0, -20.0, -4000.0, -1e7] * B)[:2 * B]
+    y = (rng.standard_normal((2 * B, V)) * 0.01).astype(np.float32)
+    check(run(to_dev(y), to_dev(bs), 2, B, N), y.astype(np.float64), bs, 2, B, N)
+
+
 def test_few_distinct_values():
     """Logits of eight values: thousands of words share a score, and where the N-th best lies many have to be left out."""
     rng = np.random.default_rng(3)
