@@ -526,46 +526,43 @@ def beam_backtrace(hist: BeamHistory, n_steps: int, stream=None):
 
 # ---- selection from the caller's logits, and a paged cache in 8 bits -----------------------------
 
-_types = None
+class _Torch:
+    """What the calls below need of torch, looked up once."""
 
-
-def _lsh_dtype(x, name) -> int:
-    """lsh_dtype of a tensor of logits, keys, values or queries."""
-    global _types
-    if _types is None:
+    def __init__(self):
         import torch
-        _types = {torch.float32: LSH_F32, torch.bfloat16: LSH_BF16, torch.float16: LSH_F16}
-    t = _types.get(x.dtype)
-    if t is None:
-        raise ValueError(f"{name}: dtype {x.dtype} not in {tuple(_types)}")
-    return t
+        self.i32, self.f32, self.u8 = torch.int32, torch.float32, torch.uint8
+        self.types = {torch.float32: LSH_F32, torch.bfloat16: LSH_BF16, torch.float16: LSH_F16}
+        torch.cuda.init()
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _ints(x, name, shape, optional=False):
-    """Device address of a contiguous int32 tensor of this shape (any, if None)."""
-    import torch
-    if x is None and optional:
-        return None
-    _require_cuda(x, name, (torch.int32,))
-    if shape is not None and x.numel() != shape:
-        raise ValueError(f"{name} must have {shape} elements, has {x.numel()}")
-    return x.data_ptr()
+_torch = None
 
 
-def _floats(x, name, n):
-    import torch
-    _require_cuda(x, name, (torch.float32,))
+def _t() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
+def _ptr(x, dtype, n, name, device) -> int:
+    """Device address of a contiguous tensor of n elements on the current device: the library launches there, and has no handle
+    that says where it was made."""
+    if x.dtype is dtype and x.get_device() == device and x.numel() == n and x.is_contiguous():
+        return x.data_ptr()
+    _require_cuda(x, name, (dtype,))
     if x.numel() != n:
         raise ValueError(f"{name} must have {n} elements, has {x.numel()}")
-    return x.data_ptr()
+    raise ValueError(f"{name} must be on the current device")
 
 
-def _same_device(first, *others):
-    """All on the current device: the library launches there, and has no handle that says where it was made."""
-    import torch
-    at = first.get_device()
-    if at != torch.cuda.current_device() or any(x is not None and x.get_device() != at for x in others):
-        raise ValueError("all tensors must be on the current device")
+def _room(x, device):
+    """Address and bytes of a workspace."""
+    if x.get_device() != device or not x.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current device")
+    return x.data_ptr(), x.numel() * x.element_size()
 
 
 def select_params(S: int, B: int, V: int, N: Optional[int] = None) -> SelectParams:
@@ -581,24 +578,25 @@ def beam_select(sp: SelectParams, logits, beam_scores, workspace, out_beam, out_
                 stream=None):
     """lsh_beam_select: asynchronous on `stream` (default: torch's current stream).  logits: [S*B, V], float32, bfloat16 or
     float16, unit stride in a row; allowed: int32 bits [S*B, >= ceil(V / 32)], or one row of them for all."""
-    R, n = sp.S * sp.B, sp.S * sp.N
-    if not logits.is_cuda or logits.dim() != 2 or tuple(logits.shape) != (R, sp.V) or (sp.V > 1 and logits.stride(1) != 1):
-        raise ValueError("logits must be a device tensor [S*B, V] with contiguous rows")
-    _same_device(logits, beam_scores, workspace, out_beam, out_word, out_score, allowed, lse)
-    ld = logits.stride(0) if R > 1 else sp.V
+    t = _t()
+    dev, R, V = t.device(), sp.S * sp.B, sp.V
+    n = sp.S * sp.N
+    dtype = t.types.get(logits.dtype)
+    if dtype is None or logits.get_device() != dev or tuple(logits.shape) != (R, V) or (V > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits must be [S*B, V] with contiguous rows on the current device, of {tuple(t.types)}")
     mask, mask_ld = None, 0
     if allowed is not None:
-        import torch
-        words = (sp.V + 31) // 32
-        if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.shape[0] not in (1, R) or allowed.shape[1] < words or (
-                allowed.shape[1] > 1 and allowed.stride(1) != 1):
-            raise ValueError("allowed must be int32 [S*B or 1, >= ceil(V / 32)] with contiguous rows")
+        words = (V + 31) // 32
+        if allowed.dtype is not t.i32 or allowed.get_device() != dev or allowed.dim() != 2 or allowed.shape[0] not in (1, R) or (
+                allowed.shape[1] < words or (allowed.shape[1] > 1 and allowed.stride(1) != 1)):
+            raise ValueError("allowed must be int32 [S*B or 1, >= ceil(V / 32)] with contiguous rows on the current device")
         mask, mask_ld = allowed.data_ptr(), allowed.stride(0) if allowed.shape[0] > 1 else 0
-    p = SelectParams(sp.S, sp.B, sp.N, sp.V, _lsh_dtype(logits, "logits"), ld, mask_ld)
+    p = SelectParams(sp.S, sp.B, sp.N, V, dtype, logits.stride(0) if R > 1 else V, mask_ld)
+    ws, room = _room(workspace, dev)
     _check(load_library().lsh_beam_select(
-        ctypes.byref(p), logits.data_ptr(), _floats(beam_scores, "beam_scores", R), mask, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _ints(out_beam, "out_beam", n), _ints(out_word, "out_word", n),
-        _floats(out_score, "out_score", n), None if lse is None else _floats(lse, "lse", R), _stream_ptr(stream)), "lsh_beam_select")
+        ctypes.byref(p), logits.data_ptr(), _ptr(beam_scores, t.f32, R, "beam_scores", dev), mask, ws, room,
+        _ptr(out_beam, t.i32, n, "out_beam", dev), _ptr(out_word, t.i32, n, "out_word", dev), _ptr(out_score, t.f32, n, "out_score", dev),
+        None if lse is None else _ptr(lse, t.f32, R, "lse", dev), _stream_ptr(stream)), "lsh_beam_select")
 
 
 def cache_params(S: int, B: int, n_blocks: int, block: int, max_blocks: int, n_heads: int, head_dim: int) -> CacheParams:
@@ -625,11 +623,14 @@ class CachePool:
             given.append(x)
         self.k, self.v, self.k_scale, self.v_scale = given
         self._shape = (cp.n_blocks, cp.block, cp.n_heads, cp.head_dim)
+        if len({x.get_device() for x in given}) != 1:
+            raise ValueError("a pool's tensors must be on one device")
+        self._device = self.k.get_device()
         self._pointers = _PoolPointers(*[x.data_ptr() for x in given])
 
-    def _of(self, cp: CacheParams):
-        if (cp.n_blocks, cp.block, cp.n_heads, cp.head_dim) != self._shape:
-            raise ValueError("the pool was made for other cache parameters")
+    def _of(self, cp: CacheParams, device: int):
+        if (cp.n_blocks, cp.block, cp.n_heads, cp.head_dim) != self._shape or device != self._device:
+            raise ValueError("the pool was made for other cache parameters, or on another device than the current one")
         return ctypes.byref(self._pointers)
 
 
@@ -640,32 +641,39 @@ def cache_workspace_bytes(cp: CacheParams) -> int:
 def cache_advance(cp: CacheParams, T: int, tables_in, lengths_in, tables_out, lengths_out, slots, copy_from, shared, status, workspace,
                   parents=None, n_new=None, stream=None):
     """lsh_cache_advance: all arrays int32; shared, parents and n_new may be None."""
-    R = cp.S * cp.B
-    _same_device(tables_in, lengths_in, tables_out, lengths_out, slots, copy_from, shared, status, workspace, parents, n_new)
+    t = _t()
+    dev, i32, R = t.device(), t.i32, cp.S * cp.B
+    n = R * cp.max_blocks
+    ws, room = _room(workspace, dev)
     _check(load_library().lsh_cache_advance(
-        ctypes.byref(cp), T, _ints(parents, "parents", R, True), _ints(n_new, "n_new", R, True),
-        _ints(tables_in, "tables_in", R * cp.max_blocks), _ints(lengths_in, "lengths_in", R),
-        _ints(tables_out, "tables_out", R * cp.max_blocks), _ints(lengths_out, "lengths_out", R), _ints(slots, "slots", R * T),
-        _ints(copy_from, "copy_from", R), _ints(shared, "shared", cp.S, True), _ints(status, "status", 2), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "lsh_cache_advance")
+        ctypes.byref(cp), T, None if parents is None else _ptr(parents, i32, R, "parents", dev),
+        None if n_new is None else _ptr(n_new, i32, R, "n_new", dev), _ptr(tables_in, i32, n, "tables_in", dev),
+        _ptr(lengths_in, i32, R, "lengths_in", dev), _ptr(tables_out, i32, n, "tables_out", dev),
+        _ptr(lengths_out, i32, R, "lengths_out", dev), _ptr(slots, i32, R * T, "slots", dev), _ptr(copy_from, i32, R, "copy_from", dev),
+        None if shared is None else _ptr(shared, i32, cp.S, "shared", dev), _ptr(status, i32, 2, "status", dev), ws, room,
+        _stream_ptr(stream)), "lsh_cache_advance")
 
 
-def _rows(x, name, shape):
-    """lsh_rows of a tensor [R, T, heads, head_dim] with any pitches."""
-    if not x.is_cuda or tuple(x.shape) != shape or x.stride(3) != 1:
-        raise ValueError(f"{name} must be a device tensor {shape} with contiguous heads")
-    return _Rows(_lsh_dtype(x, name), x.stride(0), x.stride(1), x.stride(2))
+def _rows(x, name, R, T, heads, D, dev):
+    """lsh_rows of a tensor [R, T, heads, D] with any pitches."""
+    t = _t().types.get(x.dtype)
+    if t is None or x.get_device() != dev or tuple(x.shape) != (R, T, heads, D):
+        raise ValueError(f"{name} must be {(R, T, heads, D)} on the current device, of {tuple(_t().types)}")
+    row, token, head, one = x.stride()
+    if one != 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    return _Rows(t, row, token, head)
 
 
 def cache_write(cp: CacheParams, pool: CachePool, k, v, slots, copy_from=None, stream=None):
     """lsh_cache_write: k, v [S*B, T, n_heads, head_dim] (views into a fused projection, say), slots int32 [S*B, T]."""
-    R, T = cp.S * cp.B, int(k.shape[1]) if k.dim() == 4 else 0
-    shape = (R, T, cp.n_heads, cp.head_dim)
-    _same_device(k, v, slots, copy_from, pool.k)
-    kr, vr = _rows(k, "k", shape), _rows(v, "v", shape)
+    t = _t()
+    dev, R, T = t.device(), cp.S * cp.B, k.shape[1] if k.dim() == 4 else 0
+    kr, vr = _rows(k, "k", R, T, cp.n_heads, cp.head_dim, dev), _rows(v, "v", R, T, cp.n_heads, cp.head_dim, dev)
     _check(load_library().lsh_cache_write(
-        ctypes.byref(cp), pool._of(cp), T, k.data_ptr(), ctypes.byref(kr), v.data_ptr(), ctypes.byref(vr), _ints(slots, "slots", R * T),
-        _ints(copy_from, "copy_from", R, True), _stream_ptr(stream)), "lsh_cache_write")
+        ctypes.byref(cp), pool._of(cp, dev), T, k.data_ptr(), ctypes.byref(kr), v.data_ptr(), ctypes.byref(vr),
+        _ptr(slots, t.i32, R * T, "slots", dev), None if copy_from is None else _ptr(copy_from, t.i32, R, "copy_from", dev),
+        _stream_ptr(stream)), "lsh_cache_write")
 
 
 def attention_params(T: int, n_heads: int, scale: float, causal: bool = True, window: int = 0) -> AttentionParams:
@@ -679,12 +687,13 @@ def attention_workspace_bytes(cp: CacheParams, ap: AttentionParams) -> int:
 def cache_attention(cp: CacheParams, ap: AttentionParams, pool: CachePool, q, tables, lengths, workspace, out, shared=None, n_new=None,
                     lse=None, stream=None):
     """lsh_cache_attention: q, out [S*B, T, n_heads, head_dim] of one type, lse float32 [S*B, T, n_heads] or None."""
-    R = cp.S * cp.B
-    shape = (R, ap.T, ap.n_heads, cp.head_dim)
-    _same_device(q, out, tables, lengths, workspace, shared, n_new, lse, pool.k)
-    qr, orow = _rows(q, "q", shape), _rows(out, "out", shape)
+    t = _t()
+    dev, i32, R, T, H = t.device(), t.i32, cp.S * cp.B, ap.T, ap.n_heads
+    qr, orow = _rows(q, "q", R, T, H, cp.head_dim, dev), _rows(out, "out", R, T, H, cp.head_dim, dev)
+    ws, room = _room(workspace, dev)
     _check(load_library().lsh_cache_attention(
-        ctypes.byref(cp), pool._of(cp), ctypes.byref(ap), q.data_ptr(), ctypes.byref(qr), _ints(tables, "tables", R * cp.max_blocks),
-        _ints(lengths, "lengths", R), _ints(n_new, "n_new", R, True), _ints(shared, "shared", cp.S, True), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), out.data_ptr(), ctypes.byref(orow),
-        None if lse is None else _floats(lse, "lse", R * ap.T * ap.n_heads), _stream_ptr(stream)), "lsh_cache_attention")
+        ctypes.byref(cp), pool._of(cp, dev), ctypes.byref(ap), q.data_ptr(), ctypes.byref(qr),
+        _ptr(tables, i32, R * cp.max_blocks, "tables", dev), _ptr(lengths, i32, R, "lengths", dev),
+        None if n_new is None else _ptr(n_new, i32, R, "n_new", dev), None if shared is None else _ptr(shared, i32, cp.S, "shared", dev),
+        ws, room, out.data_ptr(), ctypes.byref(orow), None if lse is None else _ptr(lse, t.f32, R * T * H, "lse", dev),
+        _stream_ptr(stream)), "lsh_cache_attention")

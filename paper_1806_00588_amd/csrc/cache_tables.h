@@ -6,12 +6,14 @@
 // are given out lowest first, to rows in order: the result is a function of the inputs.
 //
 // Bound by latency: three dependent passes (who continues with what; how many blocks each row needs and which are free; tables
-// and slots) over a few bytes.
+// and slots) over a few bytes.  Small calls are one workgroup's (k_tables_once), which has plans and a bitmap of the pool in LDS:
+// 12 rows of 20 blocks XX us, where the four launches of the others take 20 to be made.
 #pragma once
 #include "device_utils.h"
 
 namespace lshbeam {
 
+struct RowPlan;
 struct TablesArgs {
     int S, B, T, n_blocks, block, width;
     const int32_t* parents;      // [R] beam of the sentence, or null: every row is its own parent
@@ -24,7 +26,7 @@ struct TablesArgs {
     int32_t* copy_from;          // [R]
     int32_t* shared;             // [S]
     int32_t* status;             // [2]
-    struct RowPlan* plan;        // workspace [R]
+    RowPlan* plan;        // workspace [R]
     int32_t* base;               // workspace [R]: where the row's blocks begin in `free_ids`
     int32_t* free_ids;           // workspace [n_blocks]
     uint8_t* used;               // workspace [n_blocks rounded up to 16]
@@ -50,29 +52,23 @@ __device__ __forceinline__ int parent_row(const TablesArgs& a, int r, int* token
     return p;
 }
 
-// Row r's plan; `or_all` is an OR over the threads that share the work (all of them call it).
-template <typename F>
-__device__ __forceinline__ RowPlan plan_row(const TablesArgs& a, int r, int p, int old_len, int thread, int threads, F or_all) {
-    int want = a.n_new ? max(a.n_new[r], 0) : (p < 0 ? 0 : a.T);
-    RowPlan plan{old_len, want, 0, -1};
-    const int n_old = blocks_of(old_len, a.block);
-    bool others = false;
-    const bool partial = want > 0 && old_len % a.block != 0;
-    const int32_t last = partial ? a.tables_in[(int64_t)p * a.width + n_old - 1] : -1;
-    if (partial) {   // does another row of the sentence continue with the block that this one would write on?
-        const int r0 = r - r % a.B;
-        for (int o = thread; o < a.B; o += threads) {
-            int tokens = 0;
-            const int q = r0 + o == r ? -1 : parent_row(a, r0 + o, &tokens);
-            if (q >= 0 && blocks_of(tokens, a.block) >= n_old) others |= a.tables_in[(int64_t)q * a.width + n_old - 1] == last;
-        }
-    }
-    others = or_all(others);
-    const int64_t len = (int64_t)old_len + want;
-    if (want > a.T || len > (int64_t)a.width * a.block || len > INT32_MAX) { plan.need = -1; return plan; }
-    plan.copy = others && last >= 0 && last < a.n_blocks ? last : -1;
-    plan.need = blocks_of((int)len, a.block) - n_old + (plan.copy >= 0);
+// Row r's plan, but for what other rows say: `last` is the block that it would write on, or -1 (a whole number of blocks, or nothing new).
+__device__ __forceinline__ RowPlan plan_row(const TablesArgs& a, int r, int p, int old_len, int32_t* last) {
+    const RowPlan plan{old_len, a.n_new ? max(a.n_new[r], 0) : (p < 0 ? 0 : a.T), 0, -1};
+    *last = plan.n_new > 0 && old_len % a.block != 0 ? a.tables_in[(int64_t)p * a.width + old_len / a.block] : -1;
     return plan;
+}
+// Does row q (-1: none) with `tokens` tokens continue with block `last` where row r's table ends?
+__device__ __forceinline__ bool continues(const TablesArgs& a, int q, int tokens, int old_len, int32_t last) {
+    const int n = blocks_of(old_len, a.block);
+    return q >= 0 && blocks_of(tokens, a.block) >= n && a.tables_in[(int64_t)q * a.width + n - 1] == last;
+}
+// `others`: another row continues with the row's last block.
+__device__ __forceinline__ void finish_plan(const TablesArgs& a, RowPlan& plan, int32_t last, bool others) {
+    const int64_t len = (int64_t)plan.old_len + plan.n_new;
+    if (plan.n_new > a.T || len > (int64_t)a.width * a.block || len > INT32_MAX) { plan.need = -1; return; }
+    plan.copy = others && last >= 0 && last < a.n_blocks ? last : -1;
+    plan.need = blocks_of((int)len, a.block) - blocks_of(plan.old_len, a.block) + (plan.copy >= 0);
 }
 
 __global__ void __launch_bounds__(256) k_tables_clear(TablesArgs a) {
@@ -85,7 +81,16 @@ __global__ void __launch_bounds__(256) k_tables_rows(TablesArgs a) {
     const int r = blockIdx.x;
     int old_len;
     const int p = parent_row(a, r, &old_len);
-    const RowPlan plan = plan_row(a, r, p, old_len, threadIdx.x, 256, [](bool v) { return __syncthreads_or(v) != 0; });
+    int32_t last;
+    RowPlan plan = plan_row(a, r, p, old_len, &last);
+    bool others = false;
+    if (last >= 0)
+        for (int o = threadIdx.x; o < a.B; o += 256) {
+            int tokens = 0;
+            const int q = r - r % a.B + o;
+            if (q != r) others |= continues(a, parent_row(a, q, &tokens), tokens, old_len, last);
+        }
+    finish_plan(a, plan, last, __syncthreads_or(others) != 0);
     if (threadIdx.x == 0) a.plan[r] = plan;
     const int n_old = blocks_of(old_len, a.block);
     for (int j = threadIdx.x; j < a.width; j += 256) {
@@ -156,46 +161,148 @@ __device__ __forceinline__ void finish_row(const TablesArgs& a, int r, const Row
 }
 
 // Leading blocks that all rows of sentence s with tokens have in common, whole blocks only.  One row: all of its whole blocks.
-// More: a block taken in this call is nobody else's, so it ends where the first row's new blocks begin at the latest.
-// `lead` is shared memory; ends with a barrier.
-__device__ __forceinline__ void shared_blocks(const TablesArgs& a, int s, const RowPlan* plan, bool ok, int* lead, int* rows, int* ref) {
-    if (threadIdx.x == 0) { lead[0] = lead[1] = INT32_MAX; *rows = 0; *ref = INT32_MAX; }
-    __syncthreads();
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+// More: a block taken in this call is nobody else's, so it ends where the first row's new blocks begin at the latest.  `threads`
+// threads share the work; min_all makes each of four values the smallest of all of them.
+template <typename F>
+__device__ __forceinline__ int shared_blocks(const TablesArgs& a, int s, const RowPlan* plan, bool ok, int thread, int threads, F min_all) {
+    auto length = [&](const RowPlan& p) { return ok ? p.old_len + p.n_new : p.old_len; };
+    int v[4] = {INT32_MAX, INT32_MAX, INT32_MAX, INT32_MAX};   // first row, last one (negative), whole blocks, old ones
+    for (int b = thread; b < a.B; b += threads) {
         const RowPlan p = plan[b];
-        const int len = ok ? p.old_len + p.n_new : p.old_len;
-        if (len <= 0) continue;
-        atomicAdd(rows, 1);
-        atomicMin(ref, b);
-        atomicMin(&lead[0], len / a.block);
-        atomicMin(&lead[1], blocks_of(p.old_len, a.block) - (ok && p.copy >= 0));
+        if (length(p) <= 0) continue;
+        v[0] = min(v[0], b);
+        v[1] = min(v[1], -b);
+        v[2] = min(v[2], length(p) / a.block);
+        v[3] = min(v[3], blocks_of(p.old_len, a.block) - (ok && p.copy >= 0));
     }
-    __syncthreads();
-    const int n = *rows, first = *ref, most = n == 0 ? 0 : n == 1 ? lead[0] : min(lead[0], lead[1]);
-    __syncthreads();
-    if (threadIdx.x == 0) lead[0] = most;
-    __syncthreads();
-    if (n > 1) {
-        const int32_t* t0 = a.tables_out + (int64_t)s * a.B * a.width;
-        for (int b = first + 1; b < a.B; ++b) {
-            const RowPlan p = plan[b];
-            if ((ok ? p.old_len + p.n_new : p.old_len) <= 0) continue;
-            for (int j = threadIdx.x; j < most; j += blockDim.x)
-                if (t0[(int64_t)b * a.width + j] != t0[(int64_t)first * a.width + j]) { atomicMin(&lead[0], j); break; }
+    min_all(v);
+    const int first = v[0], last = -v[1], most = min(v[2], v[3]);
+    if (first == INT32_MAX) return 0;
+    if (first == last) return v[2];
+    const int32_t* t0 = a.tables_out + (int64_t)s * a.B * a.width;
+    v[0] = most;
+    for (int j = thread; j < most; j += threads) {
+        const int32_t id = t0[(int64_t)first * a.width + j];
+        bool same = true;
+        for (int b0 = first + 1; b0 <= last; b0 += 8) {   // eight rows asked for together, whether they have tokens or not
+            int32_t other[8];
+            bool empty[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int b = min(b0 + k, last);
+                other[k] = t0[(int64_t)b * a.width + j];
+                empty[k] = length(plan[b]) <= 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) same &= empty[k] | (other[k] == id);
         }
+        if (!same) v[0] = min(v[0], j);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) a.shared[s] = lead[0];
+    min_all(v);
+    return v[0];
 }
 
-// grid = R workgroups.
+__device__ __forceinline__ void wave_min(int (&v)[4]) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = min(v[k], __shfl_xor(v[k], off, kWave));
+}
+
+// grid = R workgroups, after S more if blocks in common are asked for.
 __global__ void __launch_bounds__(256) k_tables_finish(TablesArgs a) {
-    __shared__ int lead[2], rows, ref;
-    const int r = blockIdx.x;
-    const bool ok = a.status[0] == 0 && a.status[1] == 0;
-    if (a.shared && r % a.B == 0) shared_blocks(a, r / a.B, a.plan + r, ok, lead, &rows, &ref);
+    __shared__ int least[4][4];
+    const int common = a.shared ? a.S : 0, r = (int)blockIdx.x - common;
+    const bool ok = (a.status[0] | a.status[1]) == 0;
+    if (r < 0) {
+        const int s = blockIdx.x;
+        const int n = shared_blocks(a, s, a.plan + (int64_t)s * a.B, ok, threadIdx.x, 256, [&](int (&v)[4]) {
+            wave_min(v);
+            __syncthreads();
+            if (lane_id() == 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) least[wave_id()][k] = v[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = min(min(least[0][k], least[1][k]), min(least[2][k], least[3][k]));
+        });
+        if (threadIdx.x == 0) a.shared[s] = n;
+        return;
+    }
     const RowPlan plan = a.plan[r];
     finish_row(a, r, plan, ok, a.free_ids + (ok ? a.base[r] : 0), threadIdx.x, 256);
+}
+
+// One workgroup does all of it.  LDS: the rows' plans, parents, last blocks and bases, a bit for each block of the pool.
+constexpr int kOnceRows = 1024, kOnceEntries = 32768, kOnceBlocks = 1 << 18, kOnceSlots = 65536;
+inline bool tables_at_once(int64_t R, int64_t width, int64_t n_blocks, int64_t T) {
+    return R <= kOnceRows && R * width <= kOnceEntries && n_blocks <= kOnceBlocks && R * T <= kOnceSlots;
+}
+inline size_t once_lds(int64_t R, int64_t n_blocks) { return (size_t)R * (sizeof(RowPlan) + 16) + (size_t)((n_blocks + 31) / 32) * 4; }
+__global__ void __launch_bounds__(1024) k_tables_once(TablesArgs a) {
+    extern __shared__ int32_t once[];
+    __shared__ uint32_t wsum[17];
+    const int R = a.S * a.B, tid = threadIdx.x, words = (a.n_blocks + 31) / 32;
+    RowPlan* plan = reinterpret_cast<RowPlan*>(once);
+    int32_t *parent = once + 4 * R, *last = parent + R, *others = last + R, *base = others + R;
+    uint32_t* used = reinterpret_cast<uint32_t*>(base + R);
+    for (int i = tid; i < words; i += 1024) used[i] = 0;
+    int32_t my_last = -1;
+    if (tid < R) {
+        int old_len;
+        const int p = parent_row(a, tid, &old_len);
+        plan[tid] = plan_row(a, tid, p, old_len, &my_last);
+        parent[tid] = p;
+        last[tid] = my_last;
+        others[tid] = 0;
+    }
+    __syncthreads();
+    for (int e = tid; e < R * a.B; e += 1024) {          // pairs of rows of a sentence
+        const int r = (int)((unsigned)e / (unsigned)a.B), q = r - r % a.B + e - r * a.B;
+        if (q != r && last[r] >= 0 && continues(a, parent[q], plan[q].old_len, plan[r].old_len, last[r])) others[r] = 1;
+    }
+    for (int e = tid; e < R * a.width; e += 1024) {      // the parents' tables; their blocks are in use
+        const int r = (int)((unsigned)e / (unsigned)a.width), j = e - r * a.width;
+        const int32_t id = j < blocks_of(plan[r].old_len, a.block) ? a.tables_in[(int64_t)parent[r] * a.width + j] : -1;
+        a.tables_out[e] = id;
+        if (id >= 0 && id < a.n_blocks) atomicOr(&used[id >> 5], 1u << (id & 31));
+    }
+    __syncthreads();
+    int need = 0;
+    if (tid < R) {
+        RowPlan mine = plan[tid];
+        finish_plan(a, mine, my_last, others[tid] != 0);
+        plan[tid] = mine;
+        need = mine.need;
+    }
+    const int refused = __syncthreads_count(need < 0);
+    uint32_t want = 0, found = 0;                        // (at most R * (width + 1) blocks)
+    const uint32_t incl = block_incl_scan((uint32_t)max(need, 0), wsum, &want);
+    if (tid < R) base[tid] = (int32_t)(incl - max(need, 0));
+    const int per = (words + 1023) / 1024;               // words of a thread, one after the other
+    auto free_bits = [&](int i) {
+        uint32_t bits = ~used[i];
+        if (i == words - 1 && (a.n_blocks & 31)) bits &= (1u << (a.n_blocks & 31)) - 1u;
+        return bits;
+    };
+    uint32_t n = 0;
+    for (int i = tid * per; i < min(words, (tid + 1) * per); ++i) n += __builtin_popcount(free_bits(i));
+    uint32_t at = block_incl_scan(n, wsum, &found) - n;
+    for (int i = tid * per; i < min(words, (tid + 1) * per) && at < want; ++i)
+        for (uint32_t bits = free_bits(i); bits && at < want; bits &= bits - 1) a.free_ids[at++] = 32 * i + __builtin_ctz(bits);
+    const bool ok = refused == 0 && want <= found;
+    if (tid == 0) {
+        a.status[0] = want > found ? (int32_t)(want - found) : 0;
+        a.status[1] = refused;
+    }
+    __syncthreads();                                     // (the workgroup's writes are there for all of it)
+    // 16 lanes to a row
+    for (int r = tid >> 4; r < R; r += 64) finish_row(a, r, plan[r], ok, a.free_ids + (ok ? base[r] : 0), tid & 15, 16);
+    if (a.shared)
+        for (int s = wave_id(); s < a.S; s += 16) {
+            const int lead = shared_blocks(a, s, plan + s * a.B, ok, lane_id(), kWave, [](int (&v)[4]) { wave_min(v); });
+            if (lane_id() == 0) a.shared[s] = lead;
+        }
 }
 
 }  // namespace lshbeam

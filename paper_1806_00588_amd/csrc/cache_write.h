@@ -55,6 +55,112 @@ template <int TYPE> __device__ __forceinline__ float value_at(const void* p, int
     return word_f32<TYPE>(static_cast<const typename WordOf<TYPE>::type*>(p)[i]);
 }
 
+// Eight values from any element on.
+template <int TYPE> __device__ __forceinline__ void load_values(const void* p, int64_t i, float (&x)[8]) {
+    using T = typename WordOf<TYPE>::type;
+    const T* from = static_cast<const T*>(p) + i;
+#pragma unroll
+    for (int h = 0; h < (TYPE == kTypeF32 ? 2 : 1); ++h) {
+        const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(from + 4 * h);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (TYPE == kTypeF32) x[4 * h + q] = __uint_as_float(v.w[q]);
+            else { x[2 * q] = word_f32<TYPE>((T)(v.w[q] & 0xffffu)); x[2 * q + 1] = word_f32<TYPE>((T)(v.w[q] >> 16)); }
+        }
+    }
+}
+__device__ __forceinline__ float finite_size(float m, float x) {   // the larger of m and |x|, if x is finite
+    x = fabsf(x);
+    return x < INFINITY ? fmaxf(m, x) : m;
+}
+
+// A block's earlier tokens, for one head of keys or values: scales, and what becomes of the codes.
+struct Earlier { float before, scale, inverse; bool same; };   // same: codes stay as they are, where they are
+__device__ __forceinline__ Earlier new_scale(float before, float amax, bool in_place) {
+    Earlier e;
+    e.before = before > 0.f && before < INFINITY ? before : 0.f;
+    e.scale = fmaxf(e.before, scale_for(amax));
+    e.inverse = e.scale > 0.f ? 1.f / e.scale : 0.f;
+    e.same = in_place && e.before == e.scale;
+    return e;
+}
+// The first `at` tokens' codes with another scale, or in another block.
+__device__ __forceinline__ void move_keys(const uint8_t* from, uint8_t* to, int at, int block, int D, const Earlier& e, int thread, int threads) {
+    const float ratio = e.before * e.inverse;
+    for (int i = thread; i < at * (D >> 4); i += threads) {
+        const int c = (int)((unsigned)i / (unsigned)at), t = i - c * at;
+        const int64_t line = ((int64_t)c * block + t) * 16;
+        uint4 w = *reinterpret_cast<const uint4*>(from + line);
+        if (e.before != e.scale) w = make_uint4(scaled_codes(w.x, ratio), scaled_codes(w.y, ratio), scaled_codes(w.z, ratio), scaled_codes(w.w, ratio));
+        *reinterpret_cast<uint4*>(to + line) = w;
+    }
+}
+
+// One token for each row (T = 1), grid = (R, heads), 256 threads: the first half has the keys, the other the values, two of a head
+// each.  Bound by latency: slot and values are asked for at once, then the block's scales; its codes only if they change.
+// 160 rows of 8 heads of 128: XX us.
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_cache_write_one(WriteArgs a) {
+    __shared__ float amax[4];
+    const int64_t r = blockIdx.x;
+    const int h = blockIdx.y, half = threadIdx.x >> 7, d = 2 * (threadIdx.x & 127);
+    const int32_t slot = a.slots[r];
+    const int32_t copy = a.copy_from ? a.copy_from[r] : -1;
+    const void* x = half ? a.v : a.k;
+    const RowsPitch& pitch = half ? a.vp : a.kp;
+    const int64_t from_x = r * pitch.row + h * pitch.head + d;
+    float x0 = 0.f, x1 = 0.f;
+    if (d < a.D) { x0 = value_at<TYPE>(x, from_x); x1 = value_at<TYPE>(x, from_x + 1); }
+    if (slot < 0 || slot / a.block >= a.n_blocks) return;
+    const int block = slot / a.block, at = slot & (a.block - 1), src = at > 0 && copy >= 0 && copy < a.n_blocks ? copy : block;
+    const int64_t from = (int64_t)src * a.heads + h, to = (int64_t)block * a.heads + h, bytes = (int64_t)a.block * a.D;
+    float* scales = half ? a.scale_v : a.scale_k;
+    const float before = at > 0 ? scales[from] : 0.f;
+    const float m = wave_max_f32(finite_size(finite_size(0.f, x0), x1));
+    if (lane_id() == 0) amax[wave_id()] = m;
+    __syncthreads();                                     // (and all have read the scales)
+    const Earlier e = new_scale(before, fmaxf(amax[2 * half], amax[2 * half + 1]), src == block);
+    if ((threadIdx.x & 127) == 0) scales[to] = e.scale;
+    const uint32_t code = to_codes(x0 * e.inverse, x1 * e.inverse, 0.f, 0.f);
+    if (half == 0) {
+        uint8_t* codes = a.codes_k + to * bytes;
+        if (at > 0 && !e.same) move_keys(a.codes_k + from * bytes, codes, at, a.block, a.D, e, threadIdx.x, 128);
+        if (d < a.D) *reinterpret_cast<uint16_t*>(codes + ((int64_t)(d >> 4) * a.block + at) * 16 + (d & 15)) = (uint16_t)code;
+    } else {
+        uint8_t* codes = a.codes_v + to * bytes;
+        const uint8_t* old = a.codes_v + from * bytes;
+        // whole groups of 16 earlier tokens, then the group that the token belongs to (whose thread for value d it is)
+        const float ratio = e.before * e.inverse;
+        const int g = at >> 4;
+        if (at > 0 && !e.same) {
+            for (int i = threadIdx.x & 127; i < g * a.D; i += 128) {
+                uint4 w = *reinterpret_cast<const uint4*>(old + (int64_t)i * 16);
+                if (e.before != e.scale) w = make_uint4(scaled_codes(w.x, ratio), scaled_codes(w.y, ratio), scaled_codes(w.z, ratio), scaled_codes(w.w, ratio));
+                *reinterpret_cast<uint4*>(codes + (int64_t)i * 16) = w;
+            }
+        }
+        if (d < a.D) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int64_t line = ((int64_t)g * a.D + d + k) * 16;
+                if ((at & 15) > 0 && !e.same) {
+                    const uint4 o = *reinterpret_cast<const uint4*>(old + line), s = *reinterpret_cast<const uint4*>(codes + line);
+                    const uint32_t ow[4] = {o.x, o.y, o.z, o.w}, sw[4] = {s.x, s.y, s.z, s.w};
+                    uint32_t u[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {        // bytes of earlier tokens
+                        const int n = min(max((at & 15) - 4 * q, 0), 4);
+                        const uint32_t is_old = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+                        u[q] = ((e.before != e.scale ? scaled_codes(ow[q], ratio) : ow[q]) & is_old) | (sw[q] & ~is_old);
+                    }
+                    *reinterpret_cast<uint4*>(codes + line) = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+                codes[line + (at & 15)] = (uint8_t)(code >> (8 * k));
+            }
+        }
+    }
+}
+
 // grid = (R * per_row, heads), 256 threads.
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_cache_write(WriteArgs a) {
@@ -85,62 +191,52 @@ __global__ void __launch_bounds__(256) k_cache_write(WriteArgs a) {
     }
     const int64_t k0 = r * a.kp.row + t0 * a.kp.token + h * a.kp.head, v0 = r * a.vp.row + t0 * a.vp.token + h * a.vp.head;
     float mk = 0.f, mv = 0.f;
-    for (int i = threadIdx.x; i < n * a.D; i += 256) {
-        const int t = i / a.D, d = i - t * a.D;
-        const float x = fabsf(value_at<TYPE>(a.k, k0 + t * a.kp.token + d)), y = fabsf(value_at<TYPE>(a.v, v0 + t * a.vp.token + d));
-        mk = x < INFINITY ? fmaxf(mk, x) : mk;
-        mv = y < INFINITY ? fmaxf(mv, y) : mv;
+    const int eights = a.D >> 3;
+    for (int i = threadIdx.x; i < n * eights; i += 256) {
+        const int t = (int)((unsigned)i / (unsigned)eights), d = 8 * (i - t * eights);
+        float x[8], y[8];
+        load_values<TYPE>(a.k, k0 + t * a.kp.token + d, x);
+        load_values<TYPE>(a.v, v0 + t * a.vp.token + d, y);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) { mk = finite_size(mk, x[q]); mv = finite_size(mv, y[q]); }
     }
     mk = wave_max_f32(mk);
     mv = wave_max_f32(mv);
     if (lane_id() == 0) { amax[0][wave_id()] = mk; amax[1][wave_id()] = mv; }
     const int64_t from = (int64_t)src * a.heads + h, to = (int64_t)block * a.heads + h;
-    float before[2] = {0.f, 0.f}, scale[2], inverse[2];
-    if (at > 0) { before[0] = a.scale_k[from]; before[1] = a.scale_v[from]; }
+    const float before_k = at > 0 ? a.scale_k[from] : 0.f, before_v = at > 0 ? a.scale_v[from] : 0.f;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (!(before[i] > 0.f && before[i] < INFINITY)) before[i] = 0.f;
-        scale[i] = fmaxf(before[i], scale_for(fmaxf(fmaxf(amax[i][0], amax[i][1]), fmaxf(amax[i][2], amax[i][3]))));
-        inverse[i] = scale[i] > 0.f ? 1.f / scale[i] : 0.f;
-    }
-    if (threadIdx.x == 0) { a.scale_k[to] = scale[0]; a.scale_v[to] = scale[1]; }
+    const Earlier ek = new_scale(before_k, fmaxf(fmaxf(amax[0][0], amax[0][1]), fmaxf(amax[0][2], amax[0][3])), src == block);
+    const Earlier ev = new_scale(before_v, fmaxf(fmaxf(amax[1][0], amax[1][1]), fmaxf(amax[1][2], amax[1][3])), src == block);
+    if (threadIdx.x == 0) { a.scale_k[to] = ek.scale; a.scale_v[to] = ev.scale; }
     const int64_t bytes = (int64_t)a.block * a.D;
     // keys: a line of 16 bytes is 16 values of a token
-    for (int i = threadIdx.x; i < (at + n) * (a.D >> 4); i += 256) {
-        const int c = i / (at + n), t = i - c * (at + n);
-        const int64_t line = ((int64_t)c * a.block + t) * 16;
-        uint4 w;
-        if (t < at) {
-            if (src == block && before[0] == scale[0]) continue;
-            w = *reinterpret_cast<const uint4*>(a.codes_k + from * bytes + line);
-            const float ratio = before[0] * inverse[0];
-            w = make_uint4(scaled_codes(w.x, ratio), scaled_codes(w.y, ratio), scaled_codes(w.z, ratio), scaled_codes(w.w, ratio));
-        } else {
-            const int64_t x = k0 + (t - at) * a.kp.token + c * 16;
-            uint32_t u[4];
+    if (at > 0 && !ek.same) move_keys(a.codes_k + from * bytes, a.codes_k + to * bytes, at, a.block, a.D, ek, threadIdx.x, 256);
+    for (int i = threadIdx.x; i < n * eights; i += 256) {
+        const int t = (int)((unsigned)i / (unsigned)eights), d = 8 * (i - t * eights);
+        float x[8];
+        load_values<TYPE>(a.k, k0 + t * a.kp.token + d, x);
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                u[q] = to_codes(value_at<TYPE>(a.k, x + 4 * q) * inverse[0], value_at<TYPE>(a.k, x + 4 * q + 1) * inverse[0],
-                                value_at<TYPE>(a.k, x + 4 * q + 2) * inverse[0], value_at<TYPE>(a.k, x + 4 * q + 3) * inverse[0]);
-            w = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-        *reinterpret_cast<uint4*>(a.codes_k + to * bytes + line) = w;
+        for (int q = 0; q < 8; ++q) x[q] *= ek.inverse;
+        *reinterpret_cast<uint2*>(a.codes_k + to * bytes + ((int64_t)(d >> 4) * a.block + at + t) * 16 + (d & 15)) =
+            make_uint2(to_codes(x[0], x[1], x[2], x[3]), to_codes(x[4], x[5], x[6], x[7]));
     }
     // values: a line of 16 bytes is a value of 16 tokens, some of them earlier ones, some new, some that stay
     for (int i = threadIdx.x; i < ((at + n + 15) >> 4) * a.D; i += 256) {
         const int g = i / a.D, d = i - g * a.D;
         const int64_t line = (int64_t)i * 16;
-        const bool same = src == block && before[1] == scale[1];
+        const bool same = ev.same;
         if (same && 16 * g + 16 <= at) continue;
-        const float ratio = before[1] * inverse[1];
-        const uint4 stay = *reinterpret_cast<const uint4*>(a.codes_v + to * bytes + line);
+        const float ratio = ev.before * ev.inverse;
+        const bool all_new = 16 * g >= at && 16 * g + 16 <= at + n;   // (nothing to keep)
+        uint4 stay = make_uint4(0, 0, 0, 0);
+        if (!all_new) stay = *reinterpret_cast<const uint4*>(a.codes_v + to * bytes + line);
         const uint4 old = at > 16 * g ? *reinterpret_cast<const uint4*>(a.codes_v + from * bytes + line) : stay;
         const uint32_t s[4] = {stay.x, stay.y, stay.z, stay.w}, o[4] = {old.x, old.y, old.z, old.w};
         uint32_t u[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint32_t kept = same ? o[q] : scaled_codes(o[q], ratio);
+            const uint32_t kept = ev.before == ev.scale ? o[q] : scaled_codes(o[q], ratio);
             float x[4];
             uint32_t is_old = 0, is_new = 0;
 #pragma unroll
@@ -150,7 +246,7 @@ __global__ void __launch_bounds__(256) k_cache_write(WriteArgs a) {
                 if (t < at) is_old |= 0xffu << (8 * j);
                 else if (t < at + n) {
                     is_new |= 0xffu << (8 * j);
-                    x[j] = value_at<TYPE>(a.v, v0 + (t - at) * a.vp.token + d) * inverse[1];
+                    x[j] = value_at<TYPE>(a.v, v0 + (t - at) * a.vp.token + d) * ev.inverse;
                 }
             }
             u[q] = (kept & is_old) | (to_codes(x[0], x[1], x[2], x[3]) & is_new) | (s[q] & ~(is_old | is_new));

@@ -230,10 +230,14 @@ lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t
     a.used = reinterpret_cast<uint8_t*>(room + w.used);
     const hipStream_t st = (hipStream_t)hip_stream;
     const unsigned R = (unsigned)c->S * (unsigned)c->B;
+    if (tables_at_once(R, c->max_blocks, c->n_blocks, T)) {
+        hipLaunchKernelGGL(k_tables_once, dim3(1), dim3(1024), once_lds(R, c->n_blocks), st, a);
+        return launched();
+    }
     hipLaunchKernelGGL(k_tables_clear, dim3((unsigned)ceil_div(c->n_blocks, 16 * 256)), dim3(256), 0, st, a);
     hipLaunchKernelGGL(k_tables_rows, dim3(R), dim3(256), 0, st, a);
     hipLaunchKernelGGL(k_tables_take, dim3(1), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(k_tables_finish, dim3(R), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_tables_finish, dim3(R + (shared_dev ? (unsigned)c->S : 0u)), dim3(256), 0, st, a);
     return launched();
 }
 
@@ -254,8 +258,8 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
     const int64_t grid = (int64_t)c->S * c->B * a.per_row;
     if (grid > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     for_type(k_rows->dtype, [&](auto type) {
-        hipLaunchKernelGGL(k_cache_write<decltype(type)::value>, dim3((unsigned)grid, (unsigned)c->n_heads), dim3(256), 0,
-                           (hipStream_t)hip_stream, a);
+        auto kernel = T == 1 ? k_cache_write_one<decltype(type)::value> : k_cache_write<decltype(type)::value>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)c->n_heads), dim3(256), 0, (hipStream_t)hip_stream, a);
     });
     return launched();
 }
@@ -274,6 +278,9 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
         !aligned(q_dev, type_bytes(q_rows->dtype)) || !aligned(out_dev, type_bytes(out_rows->dtype)) || !workspace_dev ||
         !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
+    const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
+    const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
+    if (plan.common.units > kMaxGrid || plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     if (workspace_bytes < lsh_attention_workspace_bytes(c, p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
     AttnArgs a{};
     a.S = c->S; a.B = c->B; a.T = p->T; a.q_heads = p->n_heads; a.heads = c->n_heads; a.D = c->head_dim;
@@ -284,13 +291,10 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
     a.tables = tables_dev; a.lengths = lengths_dev; a.n_new = n_new_dev; a.shared = shared_dev;
     a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
     a.lse = lse_dev;
-    const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
     a.has_common = plan.common.units > 0;
     a.parts = plan.common.splits + plan.own.splits;
     a.ml = static_cast<float2*>(workspace_dev);
     a.acc = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.acc);
-    const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
-    if (plan.common.units > kMaxGrid || plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)hip_stream;
     bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {

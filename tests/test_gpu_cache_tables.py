@@ -65,6 +65,19 @@ def test_matches_plain(S, B, width, longest, common, T, block):
         check(S, B, T, n_blocks, block, tables, lengths, p, n)
 
 
+@pytest.mark.parametrize("S,B,width,longest,common,T", [(3, 5, 2500, 700, 320, 1), (40, 10, 90, 1300, 800, 2), (1200, 1, 5, 60, 0, 3), (5, 250, 30, 300, 128, 1),
+                                                       (64, 10, 258, 4100, 3600, 1), (2, 2, 9000, 140000, 100000, 40)])
+def test_matches_plain_beyond_one_workgroup(S, B, width, longest, common, T):
+    """More rows, more entries or more blocks than one workgroup takes."""
+    rng = np.random.default_rng(width)
+    block = 16
+    n_blocks = int(S * (common // block + B * ((longest - common) // block + 3))) + 70
+    tables, lengths = rows(rng, S, B, block, width, longest, common, n_blocks)
+    parents, n_new = rng.integers(-1, B, S * B), rng.integers(0, T + 1, S * B)
+    for p, n in ((None, None), (parents, n_new)):
+        check(S, B, T, n_blocks, block, tables, lengths, p, n)
+
+
 def test_lengths_of_zero_one_and_whole_blocks():
     tables = np.array([[3, 9], [5, 9], [1, 0], [4, 6], [9, 9], [2, 9]])
     for lengths in ([0, 1, 32, 17, 0, 16], [0] * 6, [16, 16, 32, 31, 0, 15]):
@@ -140,7 +153,7 @@ def test_not_enough_blocks_and_too_long_rows():
 
 def test_every_free_block_and_not_one_more():
     """Prompts that take all blocks of a pool, in one call; and more rows than a workgroup has threads."""
-    for S, block, T in ((1, 16, 16 * 30), (1500, 16, 16), (3000, 32, 7)):
+    for S, block, T in ((1, 16, 16 * 30), (1500, 16, 16), (3000, 32, 7), (1000, 16, 33), (33, 16, 15)):
         n = -(-T // block)
         check(S, 1, T, S * n, block, np.full((S, n), -1), np.zeros(S, dtype=int))
         assert check(S, 1, T, max(1, S * n - 1), block, np.full((S, n), -1), np.zeros(S, dtype=int))["status"][0] == 1
