@@ -215,7 +215,10 @@ lsh_status lsh_beam_select(const lsh_select_params* p, const void* logits_dev, c
  *   lsh_cache_advance    rows continue their parents' tables, blocks are taken for new tokens, every new token gets a slot
  *   lsh_cache_write      for each layer: keys and values of the new tokens go to their slots
  *   lsh_cache_attention  for each layer: queries over the rows' tokens
- * One set of tables serves all layers; a layer has a pool. */
+ * One set of tables serves all layers; a layer has a pool.  All calls are made with the device that the memory lies on
+ * current; workspaces are aligned to 256 bytes, need not be initialised, and are not shared by calls that overlap in time.
+ * Lengths, tables and slots are read on the device and cannot be refused: senseless ones give senseless results, but nothing
+ * outside the arrays is touched. */
 
 typedef struct {
     int32_t S, B;       /* as in lsh_step_params; rows R = S * B <= 2^20                               */
@@ -272,7 +275,7 @@ lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t
 
 /* Keys and values of new tokens (fp32, bf16 or fp16; both of one type) into a layer's pool.
  *   slots_dev      int32 [R, T] as lsh_cache_advance leaves them: a row's tokens have consecutive positions, -1 behind the
- *                  last.  Slots that no block of the pool has, and what follows a gap, are left out.
+ *                  last.  Slots that no block of the pool has are left out, and so is what follows a gap in a block.
  *   copy_from_dev  int32 [R], or NULL: the block that the row's first block begins as a copy of
  * A block's scale (of each head, of keys and of values) is the smallest power of two, 2^-126 at least, with which its largest
  * finite value is at most 448, 0 for a block of zeros, and never less than its earlier tokens'; codes are rounded to nearest

@@ -169,6 +169,19 @@ def test_large_pool():
     check(28, 1, 130, n_blocks, 16, tables, np.full(28, 32000), None, rng.integers(0, 131, 28))
 
 
+@pytest.mark.parametrize("R,width,n_blocks,T", [(1024, 32, 1 << 17, 64), (1024, 32, (1 << 17) + 1, 64), (1024, 33, 1 << 17, 64), (1, 32768, 1 << 17, 65536)])
+def test_the_largest_calls_of_one_workgroup(R, width, n_blocks, T):
+    rng = np.random.default_rng(R)
+    old = rng.integers(0, width * 16 - T + 1, R) if R > 1 else np.array([width * 16 - T])
+    ids, at = rng.permutation(n_blocks), 0
+    tables = np.full((R, width), -1)
+    for r in range(R):
+        n = -(-int(old[r]) // 16)
+        tables[r, :n] = ids[at:at + n]
+        at += n
+    check(R, 1, T, n_blocks, 16, tables, old, None, rng.integers(0, T + 1, R))
+
+
 def test_senseless_input_stays_inside():
     """Lengths below zero or beyond the table, blocks that no pool has, parents that no sentence has: nothing outside the arrays is
     touched, and what can be said is said."""
