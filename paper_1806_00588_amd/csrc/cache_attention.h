@@ -209,17 +209,28 @@ __device__ __forceinline__ void find_positions(const AttnArgs& a, AttnPlace& p, 
 __device__ __forceinline__ int32_t table_entry(const AttnArgs& a, int table_row, int64_t pos) {
     return a.tables[(int64_t)table_row * a.width + min(pos >> __builtin_ctz(a.block), (int64_t)a.width - 1)];
 }
-// Blocks and scales of n tiles (kLookup at most) from `tile` on, 16 tokens at a time: thread i the i-th of them.  `entry` is its table entry.
-__device__ __forceinline__ void put_lookup(const AttnArgs& a, AttnShared& sh, const AttnPlace& p, int64_t tile, int n, int32_t entry) {
-    const int i = threadIdx.x;
-    if (i >= 4 * n) return;
-    const int64_t pos = tile * kAttnTile + 16 * i;
-    const int32_t id = pos < p.vhi && pos + 15 >= p.vlo && entry >= 0 && entry < a.n_blocks && pos < (int64_t)a.width * a.block ? entry : -1;
-    const int64_t at = (int64_t)max(id, 0) * a.heads + p.h;
-    sh.id[i] = id;
-    sh.k_scale[i] = id >= 0 ? a.scale_k[at] * (a.scale * 1.44269504f) : 0.f;
-    sh.v_scale[i] = id >= 0 ? a.scale_v[at] : 0.f;
-}
+// Blocks and scales of n tiles (kLookup at most) from `tile` on, 16 tokens at a time: thread i the i-th of them.  `entry` is its table
+// entry.  ids() puts the blocks to LDS and asks for the scales, put() puts those there: what the blocks alone are needed for can be
+// asked for in between.
+struct Lookup {
+    float k, v;
+    __device__ __forceinline__ void ids(const AttnArgs& a, AttnShared& sh, const AttnPlace& p, int64_t tile, int n, int32_t entry) {
+        const int i = threadIdx.x;
+        k = v = 0.f;
+        if (i >= 4 * n) return;
+        const int64_t pos = tile * kAttnTile + 16 * i;
+        const int32_t id = pos < p.vhi && pos + 15 >= p.vlo && entry >= 0 && entry < a.n_blocks && pos < (int64_t)a.width * a.block ? entry : -1;
+        const int64_t at = (int64_t)max(id, 0) * a.heads + p.h;
+        sh.id[i] = id;
+        if (id >= 0) { k = a.scale_k[at]; v = a.scale_v[at]; }
+    }
+    __device__ __forceinline__ void put(const AttnArgs& a, AttnShared& sh, int n) const {
+        const int i = threadIdx.x;
+        if (i >= 4 * n) return;
+        sh.k_scale[i] = k * (a.scale * 1.44269504f);
+        sh.v_scale[i] = v;
+    }
+};
 
 // Queries: asked for (whatever the row's tokens: they are there), then put to LDS as operands [plane, row tile, kk, half, lane].
 template <int TYPE, int DP, int MT, int THREADS> struct Queries {
@@ -460,8 +471,9 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
         if (rel0 != p.split * p.chunk) __syncthreads();
         if (p.tile0 + rel0 != tile_guess || p.table_row != table_guess)
             entry = table_entry(a, p.table_row, ((int64_t)p.tile0 + rel0) * kAttnTile + 16 * threadIdx.x);
-        put_lookup(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
-        __syncthreads();
+        Lookup lookup;
+        lookup.ids(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
+        lds_barrier();                                   // (the scales are on their way)
         uint4 kw[KK][4], vw[DT];
         auto load_k = [&](int rel) {
             const int group = n16 >> 2, in_block = ((p.tile0 + rel0 + rel) * kAttnTile + 16 * group) & (a.block - 1);
@@ -475,6 +487,8 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
                 }
         };
         if (wv < n) load_k(wv);
+        lookup.put(a, sh, n);
+        lds_barrier();
         for (int rel = wv; rel < n; rel += 4) {
             {
                 const int in_block = ((p.tile0 + rel0 + rel) * kAttnTile + 16 * c) & (a.block - 1);
@@ -565,7 +579,9 @@ __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
         if (rel0 != p.split * p.chunk) __syncthreads();
         if (p.tile0 + rel0 != tile_guess || p.table_row != table_guess)
             entry = table_entry(a, p.table_row, ((int64_t)p.tile0 + rel0) * kAttnTile + 16 * threadIdx.x);
-        put_lookup(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
+        Lookup lookup;
+        lookup.ids(a, sh, p, (int64_t)p.tile0 + rel0, n, entry);
+        lookup.put(a, sh, n);
         __syncthreads();
         // every wave asks for LOADS kilobytes of a tile, the last of them twice where they do not come out even
         auto ask = [&](int rel) {
