@@ -108,15 +108,17 @@ struct AttnPlan {
     size_t acc, bytes;  // where the parts' products begin in the workspace; its size
 };
 // sets: pairs of a row set and a head; tiles: of a row at most -- what a row has is known on the device only, and a chunk behind its
-// last tile costs little.  A chunk has four tiles at least (eight of k_attention_rows: what a workgroup's begin and end are worth),
-// more where a row would have more chunks than workgroups.  Rows of at most eight tiles are not split: one tile more for each wave
-// costs less than the join (ten tiles of fp32 queries, 18 rows of 3 heads: split 14.9 us a call, not split 16.8).
+// last tile costs little.  A chunk of few rows has four tiles at least, eight or 16 where that still makes workgroups for the chip (a
+// workgroup's begin and end and its part of the join are worth some tiles: 128 rows of up to 1024 tokens, 8 heads of 64, chunks of
+// 4, 8, 16 tiles 25.9, 25.2, 19.1 us; 2 rows of 8192 13.8, 12.6, 14.2), one of k_attention_rows eight; more where a row would have
+// more chunks than workgroups.  Rows of at most eight tiles are not split: one tile more for each wave costs less than the join
+// (ten tiles of fp32 queries, 18 rows of 3 heads: split 14.9 us a call, not split 16.8).
 AttnLaunch attention_launch(int64_t rows, int64_t sets, int64_t tiles, int64_t most_splits) {
     AttnLaunch w{};
     w.groups = (int)ceil_div(rows, 64);
     w.row_tiles = (int)ceil_div(ceil_div(rows, w.groups), 16);
     sets *= w.groups;
-    w.chunk = tiles <= 8 || w.row_tiles > 1 ? 8 : 4;
+    w.chunk = w.row_tiles > 1 || tiles <= 8 ? 8 : sets * ceil_div(tiles, 4) <= 256 ? 4 : sets * ceil_div(tiles, 8) <= 512 ? 8 : 16;
     w.splits = (int)std::min({ceil_div(tiles, w.chunk), std::max<int64_t>(1, (w.row_tiles > 1 ? 1024 : 2048) / sets), most_splits});
     w.units = sets * w.splits;
     return w;
