@@ -286,21 +286,30 @@ __device__ __forceinline__ SelLimit limit_of_threads(SelShared& sh, float f, int
     return to;
 }
 
-// The row's lse from its parts, by a wave; also its offset in shared memory.
-__device__ __forceinline__ void row_offset(const SelArgs& a, SelShared& sh, int64_t r, int b, const SelPart* part, int parts) {
+// The row's lse from its parts, by a wave; also its offset in shared memory.  first: the first 64 parts and the row's score, asked
+// for while the row before was worked on.
+struct RowStart {
+    SelPart part;
+    float score;
+    __device__ __forceinline__ void ask(const SelArgs& a, int64_t r, const SelPart* of_row, int parts) {
+        part = lane_id() < parts ? of_row[lane_id()] : SelPart{0.0, -INFINITY, 0.f};
+        score = a.scores[r];
+    }
+};
+__device__ __forceinline__ void row_offset(const SelArgs& a, SelShared& sh, int64_t r, int b, const SelPart* part, int parts, const RowStart& first) {
     const int ln = lane_id();
-    float m = -INFINITY;
-    for (int i = ln; i < parts; i += kWave) m = fmaxf(m, part[i].max);
+    float m = first.part.max;
+    for (int i = ln + kWave; i < parts; i += kWave) m = fmaxf(m, part[i].max);
     m = wave_max_f32(m);
     double sum = 0.0;
     for (int i = ln; i < parts; i += kWave) {
-        const SelPart p = part[i];
+        const SelPart p = i < kWave ? first.part : part[i];
         sum += isinf(m) || isinf(p.max) ? p.sum : p.sum * exp((double)p.max - (double)m);
     }
     sum = wave_sum_f64(sum);
     if (ln == 0) {
         const double lg = log(sum);      // (of nothing: -inf)
-        sh.off[b] = (double)a.scores[r] - lg;
+        sh.off[b] = (double)first.score - lg;
         sh.top[b] = m;
         sh.rough[b] = (float)sh.off[b];
         if (a.out_lse) a.out_lse[r] = (float)(m > -INFINITY ? (double)m + lg : lg);
@@ -428,7 +437,9 @@ __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
     __shared__ SelShared sh;
     const int s = blockIdx.x, wv = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
     const int64_t r0 = (int64_t)s * a.B;
-    // wave w takes 64 tiles of a row at a time, unit w, w + 16, ..., sixteen of them under way together; the first sixteen it keeps
+    // Up to 16384 tiles: wave w has 64 tiles of a row at a time, units w, w + 16, ..., sixteen of them under way together and kept.  More:
+    // the parts first, then the tiles of those that can have a winner (2 sentences of 56 beams, 193 407 words in fp32: all tiles,
+    // twice, 92 us a call, parts first below 40).
     constexpr int kHeld = 16, kWaves = kSelThreads / kWave;
     const int runs = (a.tiles + kWave - 1) / kWave, units = a.B * runs;
     const float* top = a.tile_max + r0 * a.tiles;
@@ -443,26 +454,33 @@ __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
         }
     };
     float held[kHeld];
-    ask(wv, held);
+    const bool by_tiles = units <= kHeld * kWaves;
+    if (by_tiles) ask(wv, held);
     if (threadIdx.x == 0) sh.n_tiles = sh.n_words = 0;
-    for (int b = wv; b < a.B; b += kWaves) row_offset(a, sh, r0 + b, b, a.part + (r0 + b) * a.parts, a.parts);
+    const SelPart* parts = a.part + r0 * a.parts;
+    RowStart now;
+    if (wv < a.B) now.ask(a, r0 + wv, parts + (int64_t)wv * a.parts, a.parts);
+    for (int b = wv; b < a.B; b += kWaves) {
+        RowStart next = now;
+        if (b + kWaves < a.B) next.ask(a, r0 + b + kWaves, parts + (int64_t)(b + kWaves) * a.parts, a.parts);
+        row_offset(a, sh, r0 + b, b, parts + (int64_t)b * a.parts, a.parts, now);
+        now = next;
+    }
     __syncthreads();
-    // the threads' best tiles: N distinct tiles reach the N-th of them, and no word below can be among the N best
+    // the threads' best tiles, or parts: N distinct ones reach the N-th of them, and no word below can be among the N best
     float best = -INFINITY;
-    auto score = [&](int u0, float (&x)[kHeld]) {   // in the place of the maxima
+    const int n_parts = a.B * a.parts;
+    if (by_tiles) {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            const int u = u0 + i * kWaves;
+        for (int i = 0; i < kHeld; ++i) {   // in the place of the maxima
+            const int u = wv + i * kWaves;
             if (u >= units) continue;
-            x[i] = rough_score(sh, (int)((unsigned)u / (unsigned)runs), x[i]);
-            best = fmaxf(best, x[i]);
+            held[i] = rough_score(sh, (int)((unsigned)u / (unsigned)runs), held[i]);
+            best = fmaxf(best, held[i]);
         }
-    };
-    score(wv, held);
-    for (int u0 = wv + kWaves * kHeld; u0 < units; u0 += kWaves * kHeld) {
-        float x[kHeld];
-        ask(u0, x);
-        score(u0, x);
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n_parts; i += kSelThreads) best = fmaxf(best, rough_score(sh, (int)((unsigned)i / (unsigned)a.parts), parts[i].max));
     }
     const SelLimit limit = limit_of_threads(sh, best, a.N);
     auto list = [&](int u) {             // (a lane of the wave's unit u)
@@ -472,17 +490,28 @@ __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
         if (to < kSelListed) sh.tile[to] = (uint32_t)(b * a.tiles + t);
     };
     uint64_t least = 1;
-    if (!limit.none) {
+    if (!limit.none && by_tiles) {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i)
-            if (limit.lets(held[i]) && wv + i * kWaves < units) list(wv + i * kWaves);
-        for (int u0 = wv + kHeld * kWaves; u0 < units; u0 += kHeld * kWaves) {
-            float x[kHeld];
-            ask(u0, x);
-            score(u0, x);
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (limit.lets(x[i]) && u0 + i * kWaves < units) list(u0 + i * kWaves);
+            if (wv + i * kWaves < units && limit.lets(held[i])) list(wv + i * kWaves);
+    } else if (!limit.none) {            // the parts that can have a winner, then their tiles
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n_parts; i += kSelThreads) {
+            if (!limit.lets(rough_score(sh, (int)((unsigned)i / (unsigned)a.parts), parts[i].max))) continue;
+            const uint32_t to = atomicAdd(&sh.n_words, 1u);
+            if (to < kSelListed) sh.pair[to] = (uint32_t)i;
+        }
+        __syncthreads();
+        const int n = (int)sh.n_words;
+        __syncthreads();
+        if (threadIdx.x == 0) { sh.n_words = 0; if (n > kSelListed) sh.n_tiles = kSelListed + 1; }
+        for (int j = threadIdx.x >> 4; j < (n > kSelListed ? 0 : n); j += kSelThreads / 16) {
+            const int i = (int)sh.pair[j], b = (int)((unsigned)i / (unsigned)a.parts), t0 = (i - b * a.parts) * a.pieces * (kSelPiece / kSelTile);
+            for (int t = t0 + (ln & 15); t < min(t0 + a.pieces * (kSelPiece / kSelTile), a.tiles); t += 16)
+                if (limit.lets(rough_score(sh, b, top[(int64_t)b * a.tiles + t]))) {
+                    const uint32_t to = atomicAdd(&sh.n_tiles, 1u);
+                    if (to < kSelListed) sh.tile[to] = (uint32_t)(b * a.tiles + t);
+                }
         }
     } else {                             // scores far apart, huge, or fewer than N: the same by keys
         uint64_t key = 0;
@@ -549,7 +578,11 @@ __global__ void __launch_bounds__(kSelThreads) k_select_small(SelArgs a) {
         }
     }
     __syncthreads();
-    for (int b = wv; b < a.B; b += kSelThreads / kWave) row_offset(a, sh, r0 + b, b, part + b * pieces, pieces);
+    for (int b = wv; b < a.B; b += kSelThreads / kWave) {
+        RowStart start;
+        start.ask(a, r0 + b, part + b * pieces, pieces);
+        row_offset(a, sh, r0 + b, b, part + b * pieces, pieces, start);
+    }
     __syncthreads();
     float lane_best[kOwn], best = -INFINITY;
 #pragma unroll
