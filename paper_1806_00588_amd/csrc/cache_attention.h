@@ -143,11 +143,10 @@ struct AttnPlace {
     int table_row;
     bool direct;                                     // nobody else has a part of these rows
 };
-__device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a) {
+__device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a, unsigned u) {   // u: the workgroup's number in its launch
     AttnPlace p;
     // (heads first: workgroups go round the eight XCDs one by one, and chunks next to each other in that order -- which short rows do
     // not have -- would leave some of them idle)
-    unsigned u = blockIdx.x;
     p.h = u % (unsigned)a.heads;
     u /= (unsigned)a.heads;
     p.group = u % (unsigned)a.groups;
@@ -162,7 +161,6 @@ __device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a) {
 
 constexpr int kLookup = 32;                          // tiles whose blocks are looked up at a time
 struct AttnShared {
-    AttnRow row[16];
     int id[4 * kLookup];                             // block of each 16 tokens, -1: none that anybody here sees
     float k_scale[4 * kLookup], v_scale[4 * kLookup];   // times scale * log2 e; as it is
 };
@@ -442,15 +440,21 @@ constexpr int larger(int a, int b) { return a > b ? a : b; }
 
 template <int TYPE, int DP> constexpr int kFewLds = larger(kQueriesLds<TYPE, DP, 1>, kSumsLds<DP, 4>);
 
-// grid = heads * groups * sets * splits workgroups of four waves; D <= DP, EXACT: D == DP.
+struct FewShared {
+    AttnShared sh;
+    AttnRow row[16];
+    float wave_m[4][16], wave_l[4][16];
+};
+// heads * groups * sets * splits workgroups of four waves; D <= DP, EXACT: D == DP.  lds: queries as operands, then each wave's sums
+// [wave, row, PITCH].
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArgs a) {
+__device__ __forceinline__ void attend_few(const AttnArgs& a, unsigned unit, uint4* lds, FewShared& few) {
     constexpr int KK = DP / 64, DT = DP / 16, PITCH = DP + 4;
-    extern __shared__ uint4 lds[];                       // queries as operands; then each wave's sums [wave, row, PITCH]
-    __shared__ AttnShared sh;
-    __shared__ float wave_m[4][16], wave_l[4][16];
+    AttnShared& sh = few.sh;
+    auto& wave_m = few.wave_m;
+    auto& wave_l = few.wave_l;
     const int ln = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), n16 = ln & 15, c = ln >> 4, pieces = a.D >> 4;
-    AttnPlace p = attn_place(a);
+    AttnPlace p = attn_place(a, unit);
     Queries<TYPE, DP, 1, 256> queries;
     queries.ask(a, p);
     // without a window the first tile is known before the lengths are
@@ -459,7 +463,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
     int32_t entry = table_entry(a, p.table_row, tile_guess * kAttnTile + 16 * threadIdx.x);
     AttnRow row = attn_row(a, p.sr, p.h, p.group * 16 + n16);
     find_positions(a, p, row);
-    if (threadIdx.x < 16) sh.row[threadIdx.x] = row;
+    if (threadIdx.x < 16) few.row[threadIdx.x] = row;
     const int lo = row.lo, hi = row.hi;
     RowSums<DP> sums;
     const bool some = p.split < p.chunks;
@@ -520,7 +524,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
     const int quads = a.D >> 2;
     for (int e = threadIdx.x; e < 16 * quads; e += 256) {
         const int at = (int)((unsigned)e / (unsigned)quads), d = 4 * (e - at * quads);
-        if (!sh.row[at].valid) continue;
+        if (!few.row[at].valid) continue;
         const float top = fmaxf(fmaxf(wave_m[0][at], wave_m[1][at]), fmaxf(wave_m[2][at], wave_m[3][at]));
         float sum = 0.f;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -532,8 +536,14 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArg
             sum += l * f;
             v += *reinterpret_cast<const f32x4*>(red + (w * 16 + at) * PITCH + d) * f;
         }
-        put_row<TYPE>(a, p, sh.row[at], d, v, top, sum);
+        put_row<TYPE>(a, p, few.row[at], d, v, top, sum);
     }
+}
+template <int TYPE, int DP, bool EXACT>
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArgs a) {
+    extern __shared__ uint4 lds[];
+    __shared__ FewShared few;
+    attend_few<TYPE, DP, EXACT>(a, blockIdx.x, lds, few);
 }
 
 template <int DP> constexpr int kRowsStages = DP > 128 ? 2 : 3;
@@ -544,14 +554,12 @@ template <int TYPE, int DP, int MT> constexpr int kRowsLds = kRowsStages<DP> * D
 // in 80 us.  Measured and not kept: two waves per 16 rows, each for half the tokens (108 us); queries in registers and a third
 // workgroup on a CU (81); all rows in each wave and tiles in registers as above (some 500 registers, which do not last).
 template <int TYPE, int DP, int MT, bool EXACT>
-__global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, unsigned unit, uint4* lds, AttnShared& sh) {
     constexpr int KK = DP / 64, DT = DP / 16, STAGES = kRowsStages<DP>, TILE = 2 * DT * 64;   // uint4 of a tile: keys [kk, i, lane], values [dt, lane]
     constexpr int LOADS = (2 * DT + MT - 1) / MT;                                             // of a wave for a tile, 1 KB each
-    extern __shared__ uint4 lds[];                       // tiles [stage, TILE], queries as operands
-    uint4* queries = lds + STAGES * TILE;
-    __shared__ AttnShared sh;
+    uint4* queries = lds + STAGES * TILE;                // (lds: tiles [stage, TILE], queries as operands)
     const int ln = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), n16 = ln & 15, c = ln >> 4, pieces = a.D >> 4;
-    AttnPlace p = attn_place(a);
+    AttnPlace p = attn_place(a, unit);
     RowSums<DP> sums;
     const int64_t tile_guess = p.shared_tokens / kAttnTile * (a.common ? 0 : 1) + (int64_t)p.split * a.chunk;
     const int table_guess = p.table_row;
@@ -629,6 +637,26 @@ __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
         if (EXACT || dt < pieces) put_row<TYPE>(a, p, row, dt * 16 + 4 * c, sums.acc[dt], live ? sums.m : -INFINITY, live ? l : 0.f);
+}
+template <int TYPE, int DP, int MT, bool EXACT>
+__global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
+    extern __shared__ uint4 lds[];
+    __shared__ AttnShared sh;
+    attend_rows<TYPE, DP, MT, EXACT>(a, blockIdx.x, lds, sh);
+}
+
+// What a sentence's beams have in common (the first `units` workgroups; MT: waves of each, 1: all four with at most 16 rows) and each
+// row's own part in one launch: neither waits for the other.  The waves behind the MT-th end at once, and a barrier does not wait for
+// waves that have ended.
+template <int TYPE, int DP, int MT> constexpr int kBothLds = MT == 1 ? kFewLds<TYPE, DP> : larger(kRowsLds<TYPE, DP, MT>, kFewLds<TYPE, DP>);
+struct BothArgs { AttnArgs common, own; unsigned units; };
+template <int TYPE, int DP, int MT, bool EXACT>
+__global__ void __launch_bounds__(256, 2) k_attention_both(BothArgs b) {
+    extern __shared__ uint4 lds[];
+    __shared__ FewShared few;
+    if (blockIdx.x >= b.units) return attend_few<TYPE, DP, EXACT>(b.own, blockIdx.x - b.units, lds, few);
+    if constexpr (MT == 1) attend_few<TYPE, DP, EXACT>(b.common, blockIdx.x, lds, few);
+    else if (__builtin_amdgcn_readfirstlane(wave_id()) < MT) attend_rows<TYPE, DP, MT, EXACT>(b.common, blockIdx.x, lds, few.sh);
 }
 
 // A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.

@@ -154,12 +154,27 @@ template <auto KERNEL, int LDS, typename ARGS> bool launch_lds(unsigned grid, un
     hipLaunchKernelGGL(KERNEL, dim3(grid), dim3(threads), LDS, st, a);
     return true;
 }
+// The launches over the cache: the common blocks' and the rows' own, one where the latter have at most 16 rows of queries.  (Heads of
+// more than 128 values need more registers for these than two waves per SIMD have.)
+template <int TYPE, int DP, bool EXACT> bool attend_both(const BothArgs& b, int row_tiles, unsigned grid, hipStream_t st) {
+    if (row_tiles == 1) return launch_lds<k_attention_both<TYPE, DP, 1, EXACT>, kBothLds<TYPE, DP, 1>>(grid, 256, st, b);
+    if (row_tiles == 2) return launch_lds<k_attention_both<TYPE, DP, 2, EXACT>, kBothLds<TYPE, DP, 2>>(grid, 256, st, b);
+    if (row_tiles == 3) return launch_lds<k_attention_both<TYPE, DP, 3, EXACT>, kBothLds<TYPE, DP, 3>>(grid, 256, st, b);
+    return launch_lds<k_attention_both<TYPE, DP, 4, EXACT>, kBothLds<TYPE, DP, 4>>(grid, 256, st, b);
+}
 template <int TYPE, int DP, bool EXACT> bool attend(const AttnArgs& a, const AttnLaunch& w, hipStream_t st) {
     const unsigned grid = (unsigned)w.units;
     if (w.row_tiles == 1) return launch_lds<k_attention_few<TYPE, DP, EXACT>, kFewLds<TYPE, DP>>(grid, 256, st, a);
     if (w.row_tiles == 2) return launch_lds<k_attention_rows<TYPE, DP, 2, EXACT>, kRowsLds<TYPE, DP, 2>>(grid, 128, st, a);
     if (w.row_tiles == 3) return launch_lds<k_attention_rows<TYPE, DP, 3, EXACT>, kRowsLds<TYPE, DP, 3>>(grid, 192, st, a);
     return launch_lds<k_attention_rows<TYPE, DP, 4, EXACT>, kRowsLds<TYPE, DP, 4>>(grid, 256, st, a);
+}
+template <int TYPE, int DP, bool EXACT> bool attend(const BothArgs& b, const AttnPlan& plan, hipStream_t st) {
+    if (plan.common.units == 0) return attend<TYPE, DP, EXACT>(b.own, plan.own, st);
+    if constexpr (DP <= 128) {
+        if (plan.own.row_tiles == 1) return attend_both<TYPE, DP, EXACT>(b, plan.common.row_tiles, (unsigned)(plan.common.units + plan.own.units), st);
+    }
+    return attend<TYPE, DP, EXACT>(b.common, plan.common, st) && attend<TYPE, DP, EXACT>(b.own, plan.own, st);
 }
 
 }  // namespace
@@ -283,7 +298,7 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
         return LSH_ERR_INVALID_ARG;
     const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
     const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
-    if (plan.common.units > kMaxGrid || plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    if (plan.common.units + plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     if (workspace_bytes < lsh_attention_workspace_bytes(c, p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
     AttnArgs a{};
     a.S = c->S; a.B = c->B; a.T = p->T; a.q_heads = p->n_heads; a.heads = c->n_heads; a.D = c->head_dim;
@@ -298,26 +313,27 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
     a.parts = plan.common.splits + plan.own.splits;
     a.ml = static_cast<float2*>(workspace_dev);
     a.acc = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.acc);
+    BothArgs both{a, a, (unsigned)plan.common.units};
+    for (int own = 0; own < 2; ++own) {
+        AttnArgs& to = own ? both.own : both.common;
+        const AttnLaunch& w = own ? plan.own : plan.common;
+        to.common = !own;
+        to.sets = own ? c->S * c->B : c->S;
+        to.chunk = w.chunk; to.groups = w.groups; to.splits = w.splits;
+        to.part0 = own ? plan.common.splits : 0;
+    }
     const hipStream_t st = (hipStream_t)hip_stream;
     bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
-        for (int own = 0; own < 2; ++own) {
-            const AttnLaunch& w = own ? plan.own : plan.common;
-            if (w.units == 0) continue;
-            a.common = !own;
-            a.sets = own ? c->S * c->B : c->S;
-            a.chunk = w.chunk; a.groups = w.groups; a.splits = w.splits;
-            a.part0 = own ? plan.common.splits : 0;
-            const int D = c->head_dim;
-            ok = ok && (D == 64    ? attend<kType, 64, true>(a, w, st)
-                        : D < 64   ? attend<kType, 64, false>(a, w, st)
-                        : D == 128 ? attend<kType, 128, true>(a, w, st)
-                        : D < 128  ? attend<kType, 128, false>(a, w, st)
-                        : D == 192 ? attend<kType, 192, true>(a, w, st)
-                        : D == 256 ? attend<kType, 256, true>(a, w, st)
-                                   : attend<kType, 256, false>(a, w, st));
-        }
+        const int D = c->head_dim;
+        ok = D == 64    ? attend<kType, 64, true>(both, plan, st)
+             : D < 64   ? attend<kType, 64, false>(both, plan, st)
+             : D == 128 ? attend<kType, 128, true>(both, plan, st)
+             : D < 128  ? attend<kType, 128, false>(both, plan, st)
+             : D == 192 ? attend<kType, 192, true>(both, plan, st)
+             : D == 256 ? attend<kType, 256, true>(both, plan, st)
+                        : attend<kType, 256, false>(both, plan, st);
         if (ok && a.parts > 1) hipLaunchKernelGGL(k_attention_join<kType>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
     });
     return ok ? launched() : LSH_ERR_HIP;
