@@ -252,3 +252,33 @@ def test_binding_refuses():
             binding.cache_advance(cp, 2, **{**ok, **bad})
     with pytest.raises(binding.LshBeamError):
         binding.cache_advance(cp, 2, **{**ok, "tables_out": ok["tables_in"]})
+
+
+@pytest.mark.parametrize("R,width,n_blocks,T", [(64, 64, 1 << 17, 32), (65, 63, 5000, 31), (64, 65, 5000, 32), (8, 512, 5000, 256), (7, 64, 5000, 257),
+                                                (9, 64, 5000, 230), (1, 4096, 1 << 17, 1), (64, 64, (1 << 17) + 1, 32)])
+def test_both_sides_of_the_border_of_one_workgroup(R, width, n_blocks, T):
+    rng = np.random.default_rng(R + T)
+    old = rng.integers(0, width * 16 - T + 1, R)
+    ids, at = rng.permutation(n_blocks), 0
+    tables = np.full((R, width), -1)
+    for r in range(R):
+        n = min(-(-int(old[r]) // 16), (n_blocks - at) // 2)
+        old[r] = min(old[r], n * 16)
+        tables[r, :n] = ids[at:at + n]
+        at += n
+    check(R, 1, T, n_blocks, 16, tables, old, None, rng.integers(0, T + 1, R))
+
+
+def test_senseless_input_of_many_rows_stays_inside():
+    """The same for calls of more rows than one workgroup takes."""
+    import torch
+    from paper_1806_00588_amd import binding
+    cp = binding.cache_params(40, 3, 20, 16, 4, 1, 16)
+    tables = np.array([[1, -5, 99, 1 << 30]] * 120)
+    got = call(cp, 5, ints(tables), ints([-5, 1 << 30, 64, 20, 63, 0] * 20), ints([0, 1, 7, -9, 1 << 30, 2] * 20), ints([1, 2, 3, 5, -4, 9] * 20))
+    torch.cuda.synchronize()
+    assert got["status"].tolist()[1] > 0 and torch.all(got["slots"] == -1)
+    got = call(cp, 5, ints(tables), ints([20, 20, 40, 20, 20, 0] * 20), None, ints([1, 2, 3, 5, -4, 5] * 20))
+    torch.cuda.synchronize()
+    slots = got["slots"].cpu().numpy()
+    assert got["status"].tolist()[1] == 0 and np.all(slots < 20 * 16) and np.all(slots >= -1)
