@@ -13,10 +13,12 @@
 // P^T operand as they are and lie in one block -- one scale of k and one of v for each lane.  Nothing is exchanged between lanes
 // but the rows' maximum.  The cache's layout gives the operands' 16 bytes per lane in pieces of 64 (k) and 256 (v) bytes at least.
 //
-// k_attention_few   up to 16 rows of queries: the four waves of a workgroup take every fourth tile, straight from memory into
-//                   registers (values of this tile asked for, products with its keys, keys of the next tile asked for, softmax,
-//                   products with the values), and join through LDS.
+// k_attention_few   up to 16 rows of queries (of a row, or of all beams over what they have in common): the four waves of a workgroup
+//                   take every fourth tile, straight from memory into registers (values of this tile asked for, products with its
+//                   keys, keys of the next tile asked for, softmax, products with the values), and join through LDS.  Bound by
+//                   memory: 64 rows of 8192, 32 heads on 8 of 128, fp16 198 us, 5.4 TB/s; 4 rows of 60 7.5 us, a chain of trips.
 // k_attention_rows  17 to 64 rows: a wave per 16 rows, all on the same tiles, which come through LDS two tiles ahead.
+// k_attention_both  the common blocks' workgroups of either kind and the rows' own in one launch.
 // The rows of a row set are split along the tokens into chunks, a workgroup's work.  Chunks leave (max, sum, products) in the
 // workspace, k_attention_join adds them up in order.
 #pragma once
@@ -539,8 +541,12 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, unsigned unit, uin
         put_row<TYPE>(a, p, few.row[at], d, v, top, sum);
     }
 }
+// Two waves on a SIMD at least, with 256 registers each; with heads of 256, and of 192 with fp32 queries, what would not fit costs more
+// than the second wave gives.  64 rows of 4096, 32 heads on 8 of 192, two waves against one: bf16 161 us against 173, fp16 177 against 176,
+// fp32 241 against 186; 378 rows of 14 tokens, bf16 24 against 39, fp16 27 against 41.
+template <int TYPE, int DP> constexpr int kFewWaves = DP > 192 || (DP > 128 && TYPE == kTypeF32) ? 1 : 2;
 template <int TYPE, int DP, bool EXACT>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) k_attention_few(AttnArgs a) {
+__global__ void __launch_bounds__(256, (kFewWaves<TYPE, DP>)) k_attention_few(AttnArgs a) {
     extern __shared__ uint4 lds[];
     __shared__ FewShared few;
     attend_few<TYPE, DP, EXACT>(a, blockIdx.x, lds, few);
@@ -645,6 +651,7 @@ __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
     attend_rows<TYPE, DP, MT, EXACT>(a, blockIdx.x, lds, sh);
 }
 
+// 4 sentences of 12 beams over 8192 common tokens, 32 heads on 8 of 128, bf16: 36.8 us a call, 39.8 as two launches (26 and 10).
 // What a sentence's beams have in common (the first `units` workgroups; MT: waves of each, 1: all four with at most 16 rows) and each
 // row's own part in one launch: neither waits for the other.  The waves behind the MT-th end at once, and a barrier does not wait for
 // waves that have ended.
@@ -659,7 +666,7 @@ __global__ void __launch_bounds__(256, 2) k_attention_both(BothArgs b) {
     else if (__builtin_amdgcn_readfirstlane(wave_id()) < MT) attend_rows<TYPE, DP, MT, EXACT>(b.common, blockIdx.x, lds, few.sh);
 }
 
-// A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.
+// Bound by latency: 4 to 6 us for 1500 to 2000 rows of some parts each.  A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_attention_join(AttnArgs a) {
     const int64_t at = (int64_t)blockIdx.x * 4 + wave_id(), rt = at / a.q_heads;

@@ -293,6 +293,15 @@ def test_beams_over_a_long_prompt(dtype):
         check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, group, shared=np.array([75]))
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("B,group,D", [(4, 16, 64), (4, 16, 128), (4, 13, 96), (3, 16, 48), (12, 4, 128), (5, 4, 112), (3, 5, 128)])
+def test_beams_with_many_query_heads(B, group, D, dtype):
+    """15 to 64 rows of queries over what the beams have in common, at most 16 of a beam over its own part."""
+    rng = np.random.default_rng(B * group)
+    cp, pool, ref, tables, lengths = scene(rng, 2, B, [400 + 37 * i for i in range(2 * B)], 16, 1, D, [320, 0], width=9000)
+    check_attention(rng, cp, pool, ref, tables, lengths, dtype, 1, group, shared=np.array([20, 0]))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_long_rows(dtype):
     rng = np.random.default_rng(4)
