@@ -226,3 +226,17 @@ def test_binding_refuses():
     with pytest.raises(binding.LshBeamError) as e:
         binding.beam_select(sp, **{**ok, "workspace": ws[:-256]})
     assert e.value.status == 6
+
+
+@pytest.mark.parametrize("V", [5000, 20001])
+def test_rows_far_apart(V):
+    """Offsets that pass 32 bits: a pitch of more than 2^29 words."""
+    import torch
+    S, B, pitch = 2, 4, (1 << 29) + 3
+    _, x, bs = inputs(12, S, B, V, "bf16")
+    room = torch.empty((S * B - 1) * pitch + V, dtype=torch.bfloat16, device="cuda")
+    far = room.as_strided((S * B, V), (pitch, 1))
+    far.copy_(x.cuda())
+    torch.cuda.synchronize()
+    want, got = run(x.cuda(), to_dev(bs), S, B, B), run(far, to_dev(bs), S, B, B)
+    assert all(np.array_equal(p, q) for p, q in zip(want, got))

@@ -445,3 +445,31 @@ def test_binding_refuses():
             binding.cache_write(cp, pool, *bad)
     with pytest.raises(ValueError):
         binding.cache_write(cp, pool, k, k, ints([[0], [16]]), ints([1]))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_pool_of_more_than_4_gib(dtype):
+    """Offsets that pass 32 bits: the same bits as in a small pool, from prompts, single tokens and the attention."""
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(12)
+    heads, D, block, lengths, first = 8, 256, 128, [300, 200], 16990      # (a block has 256 KB of keys)
+    new = [torch.from_numpy(rng.standard_normal((2, 301, heads, D))).to(getattr(torch, TYPES[dtype])).cuda() for _ in range(2)]
+    q = torch.from_numpy(rng.standard_normal((2, 1, 4 * heads, D))).to(getattr(torch, TYPES[dtype])).cuda()
+    ap = binding.attention_params(1, 4 * heads, 1 / 16)
+    got = []
+    for n_blocks, base in ((6, 0), (17000, first)):
+        cp = binding.cache_params(2, 1, n_blocks, block, 3, heads, D)
+        pool = binding.CachePool(cp)
+        tables = base + np.arange(6).reshape(2, 3)
+        slot = lambda r, t: int(tables[r, t // block]) * block + t % block
+        binding.cache_write(cp, pool, new[0][:, :300], new[1][:, :300], ints([[slot(r, t) if t < lengths[r] else -1 for t in range(300)] for r in range(2)]))
+        binding.cache_write(cp, pool, new[0][:, 300:], new[1][:, 300:], ints([[slot(r, lengths[r])] for r in range(2)]))
+        out, lse = torch.empty_like(q), torch.empty(2, 1, 4 * heads, device="cuda")
+        ws = torch.empty(binding.attention_workspace_bytes(cp, ap), dtype=torch.uint8, device="cuda")
+        binding.cache_attention(cp, ap, pool, q, ints(tables), ints([n + 1 for n in lengths]), ws, out, lse=lse)
+        torch.cuda.synchronize()
+        got.append([x[base:base + 6].clone() for x in (pool.k, pool.v, pool.k_scale, pool.v_scale)] + [out, lse])
+        if base:
+            assert pool.k.numel() > 1 << 32 and not pool.k[:first].any() and not pool.v[:first].any()
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(torch.isfinite(got[0][4]).all())
