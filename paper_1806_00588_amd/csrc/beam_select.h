@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select_words(SelArgs a) {
     __shared__ SelShared sh;
     const int s = blockIdx.x, wv = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
     const int64_t r0 = (int64_t)s * a.B;
-    // Up to 16384 tiles: wave w has 64 tiles of a row at a time, units w, w + 16, ..., sixteen of them under way together and kept.  More:
+    // Up to 256 units of 64 tiles of a row: wave w has units w, w + 16, ..., its sixteen under way together and kept.  More of them:
     // the parts first, then the tiles of those that can have a winner (2 sentences of 56 beams, 193 407 words in fp32: all tiles,
     // twice, 92 us a call, parts first below 40).
     constexpr int kHeld = 16, kWaves = kSelThreads / kWave;

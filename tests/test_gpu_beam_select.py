@@ -240,3 +240,37 @@ def test_rows_far_apart(V):
     torch.cuda.synchronize()
     want, got = run(x.cuda(), to_dev(bs), S, B, B), run(far, to_dev(bs), S, B, B)
     assert all(np.array_equal(p, q) for p, q in zip(want, got))
+
+
+# more than 16384 tiles of 128 words in a sentence, or 256 units of 64 of a row: found by way of the waves' parts
+MANY = [(1, 256, 9000, 256), (2, 130, 17001, 34), (1, 20, 150001, 20), (1, 5, 500003, 256)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("S,B,V,N", MANY)
+def test_many_tiles(S, B, V, N, dtype):
+    _, x, bs = inputs(V, S, B, V, dtype)
+    check(run(x.cuda(), to_dev(bs), S, B, N), x.double().numpy(), bs, S, B, N)
+
+
+@pytest.mark.parametrize("B,V,N", [(40, 120001, 256), (20, 150000, 30), (256, 9000, 3)])
+def test_many_tiles_of_ties(B, V, N):
+    x = np.full((B, V), 1.5, dtype=np.float32)
+    gb, gw, _, _ = run(to_dev(x), to_dev(np.zeros(B, dtype=np.float32)), 1, B, N)
+    assert np.all(gb == 0) and np.array_equal(gw[0], np.arange(N))
+
+
+def test_many_tiles_with_odd_rows_and_masks():
+    S, B, V, N = 1, 256, 9000, 40
+    rng, x, bs = inputs(21, S, B, V, "f32")
+    x = x.numpy()
+    x[::7] = np.finfo(np.float32).min
+    x[1], x[2, 5], x[3, 6] = -np.inf, np.nan, np.inf
+    bs[4:200] = -np.inf
+    allowed = rng.random((S * B, V)) < 0.01
+    allowed[210] = False
+    check(run(to_dev(x), to_dev(bs), S, B, N), x.astype(np.float64), bs, S, B, N)
+    check(run(to_dev(x), to_dev(bs), S, B, N, allowed=to_dev(bits_of(allowed))), x.astype(np.float64), bs, S, B, N, allowed)
+    y = (rng.standard_normal((B, V)) * 300).astype(np.float32)
+    bs = (-3e4 * rng.random(B)).astype(np.float32)
+    check(run(to_dev(y), to_dev(bs), S, B, N), y.astype(np.float64), bs, S, B, N)
