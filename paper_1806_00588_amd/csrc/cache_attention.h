@@ -17,7 +17,8 @@
 //                   take every fourth tile, straight from memory into registers (values of this tile asked for, products with its
 //                   keys, keys of the next tile asked for, softmax, products with the values), and join through LDS.  Bound by
 //                   memory: 64 rows of 8192, 32 heads on 8 of 128, fp16 198 us, 5.4 TB/s; 4 rows of 60 7.5 us, a chain of trips.
-// k_attention_rows  17 to 64 rows: a wave per 16 rows, all on the same tiles, which come through LDS two tiles ahead.
+// k_attention_rows  17 to 64 rows (48 of fp32 with heads of more than 192): a wave per 16 rows, all on the same tiles, which come through LDS two
+//                   tiles ahead.
 // k_attention_both  the common blocks' workgroups of either kind and the rows' own in one launch.
 // The rows of a row set are split along the tokens into chunks, a workgroup's work.  Chunks leave (max, sum, products) in the
 // workspace, k_attention_join adds them up in order.
@@ -439,6 +440,7 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const AttnPlace& p, c
 template <int TYPE, int DP, int MT> constexpr int kQueriesLds = kPlanes<TYPE> * MT * DP * 32;
 template <int DP, int SUMS> constexpr int kSumsLds = SUMS * 16 * (DP + 4) * 4;
 constexpr int larger(int a, int b) { return a > b ? a : b; }
+constexpr int kCuLds = 160 * 1024;   // what a workgroup can have, of its own and asked for at launch together
 
 template <int TYPE, int DP> constexpr int kFewLds = larger(kQueriesLds<TYPE, DP, 1>, kSumsLds<DP, 4>);
 
@@ -547,6 +549,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, unsigned unit, uin
 template <int TYPE, int DP> constexpr int kFewWaves = DP > 192 || (DP > 128 && TYPE == kTypeF32) ? 1 : 2;
 template <int TYPE, int DP, bool EXACT>
 __global__ void __launch_bounds__(256, (kFewWaves<TYPE, DP>)) k_attention_few(AttnArgs a) {
+    static_assert(kFewLds<TYPE, DP> + sizeof(FewShared) <= kCuLds, "LDS of a CU");
     extern __shared__ uint4 lds[];
     __shared__ FewShared few;
     attend_few<TYPE, DP, EXACT>(a, blockIdx.x, lds, few);
@@ -554,6 +557,8 @@ __global__ void __launch_bounds__(256, (kFewWaves<TYPE, DP>)) k_attention_few(At
 
 template <int DP> constexpr int kRowsStages = DP > 128 ? 2 : 3;
 template <int TYPE, int DP, int MT> constexpr int kRowsLds = kRowsStages<DP> * DP * 128 + kQueriesLds<TYPE, DP, MT>;
+// Waves that it can have: four, but three where two tiles of 256 values and 64 rows of fp32 queries (three planes: 160 KB) are all LDS there is.
+template <int TYPE, int DP> constexpr int kRowsMost = kRowsLds<TYPE, DP, 4> + (int)sizeof(AttnShared) <= kCuLds ? 4 : 3;
 
 // The same grid, MT waves: wave w has rows 16 w .. 16 w + 15 of the group.  Bound by how many workgroups a CU holds and by what each of
 // them does one thing after the other (about 1.3 us a tile): 16 sentences of 12 beams over 8000 common tokens of 8 heads, D = 128, bf16, 264 MB
@@ -646,6 +651,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, unsigned unit, ui
 }
 template <int TYPE, int DP, int MT, bool EXACT>
 __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
+    static_assert(kRowsLds<TYPE, DP, MT> + sizeof(AttnShared) <= kCuLds, "LDS of a CU");
     extern __shared__ uint4 lds[];
     __shared__ AttnShared sh;
     attend_rows<TYPE, DP, MT, EXACT>(a, blockIdx.x, lds, sh);
@@ -659,6 +665,7 @@ template <int TYPE, int DP, int MT> constexpr int kBothLds = MT == 1 ? kFewLds<T
 struct BothArgs { AttnArgs common, own; unsigned units; };
 template <int TYPE, int DP, int MT, bool EXACT>
 __global__ void __launch_bounds__(256, 2) k_attention_both(BothArgs b) {
+    static_assert(kBothLds<TYPE, DP, MT> + sizeof(FewShared) <= kCuLds, "LDS of a CU");
     extern __shared__ uint4 lds[];
     __shared__ FewShared few;
     if (blockIdx.x >= b.units) return attend_few<TYPE, DP, EXACT>(b.own, blockIdx.x - b.units, lds, few);

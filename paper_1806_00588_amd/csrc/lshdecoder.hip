@@ -113,9 +113,9 @@ struct AttnPlan {
 // 4, 8, 16 tiles 25.9, 25.2, 19.1 us; 2 rows of 8192 13.8, 12.6, 14.2), one of k_attention_rows eight; more where a row would have
 // more chunks than workgroups.  Rows of at most eight tiles are not split: one tile more for each wave costs less than the join
 // (ten tiles of fp32 queries, 18 rows of 3 heads: split 14.9 us a call, not split 16.8).
-AttnLaunch attention_launch(int64_t rows, int64_t sets, int64_t tiles, int64_t most_splits) {
+AttnLaunch attention_launch(int64_t rows, int64_t most_rows, int64_t sets, int64_t tiles, int64_t most_splits) {
     AttnLaunch w{};
-    w.groups = (int)ceil_div(rows, 64);
+    w.groups = (int)ceil_div(rows, most_rows);
     w.row_tiles = (int)ceil_div(ceil_div(rows, w.groups), 16);
     sets *= w.groups;
     w.chunk = w.row_tiles > 1 || tiles <= 8 ? 8 : sets * ceil_div(tiles, 4) <= 256 ? 4 : sets * ceil_div(tiles, 8) <= 512 ? 8 : 16;
@@ -123,16 +123,23 @@ AttnLaunch attention_launch(int64_t rows, int64_t sets, int64_t tiles, int64_t m
     w.units = sets * w.splits;
     return w;
 }
-AttnPlan attention_plan(const lsh_cache_params* c, const lsh_attention_params* p, bool shared) {
+// Rows of queries that a workgroup takes at most, by what the kernel for heads of D values has LDS for.
+int64_t most_rows(int32_t dtype, int32_t D) {
+    static_assert(kRowsMost<kTypeF32, 64> == 4 && kRowsMost<kTypeF32, 128> == 4 && kRowsMost<kTypeF32, 192> == 4 && kRowsMost<kTypeF16, 256> == 4 &&
+                  kRowsMost<kTypeBf16, 256> == 4, "only fp32 with heads of 256 (and those that run in their code) is asked for here");
+    return dtype == LSH_F32 && D > 128 && D != 192 ? 16 * kRowsMost<kTypeF32, 256> : 64;
+}
+AttnPlan attention_plan(const lsh_cache_params* c, const lsh_attention_params* p, int32_t dtype, bool shared) {
     AttnPlan w{};
+    const int64_t most = most_rows(dtype, c->head_dim);
     const int64_t R = (int64_t)c->S * c->B, per_row = (int64_t)p->T * (p->n_heads / c->n_heads);
     int64_t tiles = ceil_div((int64_t)c->max_blocks * c->block, kAttnTile);
     if (p->window > 0) tiles = std::min(tiles, ceil_div((int64_t)p->window + p->T, kAttnTile) + 1);
     // beams together where it saves reading more than two launches more cost: 32 MB
     const bool common = shared && c->B > 1 && R * c->n_heads * tiles * kAttnTile * 2 * c->head_dim > (int64_t)32 << 20;
-    if (common) w.common = attention_launch(c->B * per_row, (int64_t)c->S * c->n_heads, tiles, INT32_MAX);
+    if (common) w.common = attention_launch(c->B * per_row, most, (int64_t)c->S * c->n_heads, tiles, INT32_MAX);
     // (beams' own tokens are few, and whatever there is of them goes round the workgroups)
-    w.own = attention_launch(per_row, R * c->n_heads, tiles, common ? std::max<int64_t>(1, 512 / (R * c->n_heads)) : INT32_MAX);
+    w.own = attention_launch(per_row, most, R * c->n_heads, tiles, common ? std::max<int64_t>(1, 512 / (R * c->n_heads)) : INT32_MAX);
     const size_t parts = (size_t)(w.common.splits + w.own.splits), at = (size_t)R * p->T * p->n_heads * (parts > 1 ? parts : 0);
     w.acc = round_up(at * sizeof(float2));
     w.bytes = std::max<size_t>(256, w.acc + round_up(at * c->head_dim * sizeof(float)));
@@ -166,8 +173,10 @@ template <int TYPE, int DP, bool EXACT> bool attend(const AttnArgs& a, const Att
     const unsigned grid = (unsigned)w.units;
     if (w.row_tiles == 1) return launch_lds<k_attention_few<TYPE, DP, EXACT>, kFewLds<TYPE, DP>>(grid, 256, st, a);
     if (w.row_tiles == 2) return launch_lds<k_attention_rows<TYPE, DP, 2, EXACT>, kRowsLds<TYPE, DP, 2>>(grid, 128, st, a);
-    if (w.row_tiles == 3) return launch_lds<k_attention_rows<TYPE, DP, 3, EXACT>, kRowsLds<TYPE, DP, 3>>(grid, 192, st, a);
-    return launch_lds<k_attention_rows<TYPE, DP, 4, EXACT>, kRowsLds<TYPE, DP, 4>>(grid, 256, st, a);
+    if constexpr (kRowsMost<TYPE, DP> == 4) {
+        if (w.row_tiles == 4) return launch_lds<k_attention_rows<TYPE, DP, 4, EXACT>, kRowsLds<TYPE, DP, 4>>(grid, 256, st, a);
+    }
+    return launch_lds<k_attention_rows<TYPE, DP, 3, EXACT>, kRowsLds<TYPE, DP, 3>>(grid, 192, st, a);
 }
 template <int TYPE, int DP, bool EXACT> bool attend(const BothArgs& b, const AttnPlan& plan, hipStream_t st) {
     if (plan.common.units == 0) return attend<TYPE, DP, EXACT>(b.own, plan.own, st);
@@ -284,7 +293,10 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
 
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p) {
     if (!attention_ok(c, p)) return 0;
-    return std::max(attention_plan(c, p, false).bytes, attention_plan(c, p, true).bytes);   // (who has a workspace may leave `shared` out)
+    size_t bytes = 0;            // of any type's queries; and who has a workspace may leave `shared` out
+    for (int32_t dtype : {LSH_F32, LSH_BF16})
+        for (bool shared : {false, true}) bytes = std::max(bytes, attention_plan(c, p, dtype, shared).bytes);
+    return bytes;
 }
 
 lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
@@ -296,7 +308,7 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
         !aligned(q_dev, type_bytes(q_rows->dtype)) || !aligned(out_dev, type_bytes(out_rows->dtype)) || !workspace_dev ||
         !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
-    const AttnPlan plan = attention_plan(c, p, shared_dev != nullptr);
+    const AttnPlan plan = attention_plan(c, p, q_rows->dtype, shared_dev != nullptr);
     const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
     if (plan.common.units + plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
     if (workspace_bytes < lsh_attention_workspace_bytes(c, p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
