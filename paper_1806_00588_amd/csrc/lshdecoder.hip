@@ -348,6 +348,7 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
                         : attend<kType, 256, false>(both, plan, st);
         if (ok && a.parts > 1) hipLaunchKernelGGL(k_attention_join<kType>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
     });
+    if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
     return ok ? launched() : LSH_ERR_HIP;
 }
 

@@ -46,3 +46,11 @@ def test_every_launch_of_the_attention_has_the_lds_it_asks_for(record):
             assert lds + STATIC <= LDS and threads <= 256 and grid < 1 << 24, (kw, got)
         several += len(got["launches"]) > 1
     assert several > 100         # (calls of more than one launch are among them)
+
+
+def test_a_launch_that_is_refused_leaves_no_error_behind(record):
+    """More LDS than the runtime gives: the call says so, and the caller's next look at HIP's last error finds none."""
+    calls = [("attention", dict(T=40, q_heads=2, head_dim=128)), ("attention", dict(S=1, B=64, q_heads=2, head_dim=128, max_blocks=20000, n_blocks=30000, shared=1 << 20))]
+    assert [g["status"] for g in record(calls)] == [0, 0]
+    for got in record(calls, refuse=1 << 10):
+        assert got["status"] == 5 and got["last_error"] == 0, got
