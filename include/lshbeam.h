@@ -286,15 +286,16 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
                            const int32_t* copy_from_dev, void* hip_stream);
 
 typedef struct {
-    int32_t T;          /* queries of a row: its last tokens                                           */
-    int32_t n_heads;    /* heads of queries, a multiple of the cache's: head h reads head
+    int32_t T;          /* queries of a row: its last tokens, 1 .. 2^20                                */
+    int32_t n_heads;    /* heads of queries, a multiple of the cache's, up to 65535: head h reads head
                            h / (n_heads / cache heads) of it                                           */
     int32_t causal;     /* 1: a token sees the positions up to its own; 0: all of the row              */
     int32_t window;     /* > 0 (causal only): ... and of those the last `window`                       */
     float scale;        /* > 0; of the products, usually 1 / sqrt(head_dim)                            */
 } lsh_attention_params;
 
-/* Bytes of workspace lsh_cache_attention needs (0 on invalid arguments). */
+/* Bytes of workspace lsh_cache_attention needs, for queries of any type (0 on invalid arguments, and where the call would be
+ * LSH_ERR_UNSUPPORTED: more than some 2^26 rows of queries, S * B * T * n_heads, or 2^24 workgroups). */
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p);
 
 /* out = softmax(scale * q k^T over the positions a token sees) v.

@@ -94,6 +94,10 @@ TablesRoom tables_room(const lsh_cache_params* c) {
 bool attention_ok(const lsh_cache_params* c, const lsh_attention_params* p) {
     return cache_ok(c) && p && p->T >= 1 && p->T <= kMaxRows && p->n_heads >= 1 && p->n_heads <= 65535 && p->n_heads % c->n_heads == 0;
 }
+// Rows of queries, of all heads: the join has a wave for each.  What is derived from them (groups, workgroups, bytes) is not looked at before
+// that is known: it need not fit its type.
+int64_t query_rows(const lsh_cache_params* c, const lsh_attention_params* p) { return (int64_t)c->S * c->B * p->T * p->n_heads; }
+bool rows_fit(const lsh_cache_params* c, const lsh_attention_params* p) { return ceil_div(query_rows(c, p), 4) <= kMaxGrid; }
 
 // How a call of the attention is divided: a launch for all beams together (if the blocks that they have in common are given) and one
 // for each row by itself, which a third joins if there is more than one part of a row.
@@ -106,6 +110,7 @@ struct AttnLaunch {
 struct AttnPlan {
     AttnLaunch common, own;
     size_t acc, bytes;  // where the parts' products begin in the workspace; its size
+    bool fits() const { return common.units + own.units <= kMaxGrid; }
 };
 // sets: pairs of a row set and a head; tiles: of a row at most -- what a row has is known on the device only, and a chunk behind its
 // last tile costs little.  A chunk of few rows has four tiles at least, eight or 16 where that still makes workgroups for the chip (a
@@ -292,10 +297,13 @@ lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool
 }
 
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p) {
-    if (!attention_ok(c, p)) return 0;
+    if (!attention_ok(c, p) || !rows_fit(c, p)) return 0;
     size_t bytes = 0;            // of any type's queries; and who has a workspace may leave `shared` out
     for (int32_t dtype : {LSH_F32, LSH_BF16})
-        for (bool shared : {false, true}) bytes = std::max(bytes, attention_plan(c, p, dtype, shared).bytes);
+        for (bool shared : {false, true}) {
+            const AttnPlan plan = attention_plan(c, p, dtype, shared);
+            if (plan.fits()) bytes = std::max(bytes, plan.bytes);
+        }
     return bytes;
 }
 
@@ -308,9 +316,10 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
         !aligned(q_dev, type_bytes(q_rows->dtype)) || !aligned(out_dev, type_bytes(out_rows->dtype)) || !workspace_dev ||
         !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
+    if (!rows_fit(c, p)) return LSH_ERR_UNSUPPORTED;
     const AttnPlan plan = attention_plan(c, p, q_rows->dtype, shared_dev != nullptr);
-    const int64_t rows = (int64_t)c->S * c->B * p->T * p->n_heads;
-    if (plan.common.units + plan.own.units > kMaxGrid || ceil_div(rows, 4) > kMaxGrid) return LSH_ERR_UNSUPPORTED;
+    if (!plan.fits()) return LSH_ERR_UNSUPPORTED;
+    const int64_t rows = query_rows(c, p);
     if (workspace_bytes < lsh_attention_workspace_bytes(c, p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
     AttnArgs a{};
     a.S = c->S; a.B = c->B; a.T = p->T; a.q_heads = p->n_heads; a.heads = c->n_heads; a.D = c->head_dim;

@@ -136,3 +136,21 @@ def test_a_pool_of_host_tensors_is_refused():
     import torch
     with pytest.raises(ValueError):
         binding.CachePool(_cache(), k=torch.zeros(50, 2, 4, 16, 16, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(S=1, B=256, n_blocks=1000, max_blocks=1000, n_heads=1, T=1 << 20, q_heads=1024),      # groups of 64 rows: 2^32
+    dict(S=1, B=256, n_blocks=1000, max_blocks=1000, n_heads=1, T=1 << 20, q_heads=1025),
+    dict(S=1 << 20, B=1, n_heads=65535, T=1 << 20, q_heads=65535), dict(S=1, B=1, T=1 << 20, q_heads=65534), dict(S=1, B=1, T=1 << 20, q_heads=66)],
+    ids=lambda k: ",".join("%s=%s" % i for i in k.items()))
+def test_attention_of_too_many_rows(kw):
+    """Numbers of rows that no launch has, and whose groups and workgroups pass 32 or 64 bits."""
+    assert _attention(**kw) == UNSUPPORTED and _attention(shared=P, **kw) == UNSUPPORTED
+    assert binding.attention_workspace_bytes(_cache(**kw), binding.attention_params(kw["T"], kw["q_heads"], 1.0)) == 0
+
+
+def test_attention_workspace_of_many_rows_goes_with_the_call():
+    """Up to the last supported call the workspace has a size, and a byte less than that is too little."""
+    for kw in (dict(S=1, B=1, T=1 << 20, q_heads=62), dict(S=1 << 12, B=256, T=1, q_heads=10), dict(S=1, B=256, T=1 << 12, q_heads=62)):
+        n = binding.attention_workspace_bytes(_cache(**kw), binding.attention_params(kw["T"], kw["q_heads"], 1.0))
+        assert n > 0 and _attention(bytes=n - 1, **kw) == SMALL
