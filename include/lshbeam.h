@@ -305,7 +305,8 @@ size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attent
  *                behind a row's n-th token stays
  *   shared_dev   int32 [S] as lsh_cache_advance leaves them, or NULL: these leading blocks are read once for all beams
  *   lse_dev      fp32 [R, T, n_heads], or NULL: log sum exp of the scaled products
- * A token that sees nothing gets zeros and an lse of -inf.  What a token does not see does not reach its result, a NaN neither.
+ * A token that sees nothing gets zeros and an lse of -inf.  What a token does not see (keys, values, scales of
+ * blocks) does not reach its result, a NaN neither.
  * Products and sums are fp32 (queries of 16 bits: the probabilities are rounded to bf16 for bf16, kept to 16 bits for fp16).
  * Asynchronous on the stream, allocates nothing; the same inputs give the same outputs bit for bit. */
 lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,

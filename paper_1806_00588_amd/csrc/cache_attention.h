@@ -323,7 +323,8 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnPlace& 
     }
     between();
     const bool has = sh.id[4 * rel + c] >= 0;
-    const float k_scale = sh.k_scale[4 * rel + c], v_scale = sh.v_scale[4 * rel + c];
+    const float k_scale = sh.k_scale[4 * rel + c];
+    float v_scale = sh.v_scale[4 * rel + c];
     // which tokens the rows see: all of a tile but at the ends
     const bool whole = __builtin_amdgcn_readfirstlane(pos >= p.lo_most && pos + kAttnTile <= p.hi_least && __ballot(!has) == 0);
     const int first = pos + 16 * c;
@@ -334,6 +335,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnPlace& 
         const int from = max(lo - first, 0), end = has ? min(hi, p.vhi) - first : 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = i >= from && i < end ? x[i] : -INFINITY;
+        if (from >= min(end, 16)) v_scale = 0.f;   // (none of them: 0 times a scale that is not finite would be NaN)
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
