@@ -201,6 +201,7 @@ size_t lsh_select_workspace_bytes(const lsh_select_params* p);
  *   out_beam_dev / out_word_dev / out_score_dev   [S, N]; behind the last pair (-1, -1, -inf).  With N = B as
  *                    lsh_beam_advance takes them.
  *   out_lse_dev      fp32 [S*B], or NULL: log sum exp of each row (-inf without an allowed word).
+ * LSH_ERR_UNSUPPORTED: more workgroups than a launch has (2^24; some 2^38 logits).
  * Asynchronous on the stream, allocates nothing; the same inputs give the same outputs bit for bit. */
 lsh_status lsh_beam_select(const lsh_select_params* p, const void* logits_dev, const float* beam_scores_dev,
                            const uint32_t* allowed_dev, void* workspace_dev, size_t workspace_bytes,

@@ -45,7 +45,7 @@ bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) &
 
 bool select_ok(const lsh_select_params* p) {
     return p && p->S >= 1 && p->B >= 1 && p->B <= kMaxBeams && p->N >= 1 && p->N <= kMaxBeams && p->V >= 1 && p->V <= kMaxWords &&
-           (int64_t)p->S * p->B <= kMaxRows && (int64_t)p->S * p->N <= kMaxRows;
+           (int64_t)p->S * p->B <= kMaxRows;
 }
 int64_t row_pieces(const lsh_select_params* p) { return ceil_div(p->V, kSelPiece); }
 bool select_is_small(const lsh_select_params* p) { return p->B * row_pieces(p) <= kSelSmall; }

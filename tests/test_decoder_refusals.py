@@ -154,3 +154,10 @@ def test_attention_workspace_of_many_rows_goes_with_the_call():
     for kw in (dict(S=1, B=1, T=1 << 20, q_heads=62), dict(S=1 << 12, B=256, T=1, q_heads=10), dict(S=1, B=256, T=1 << 12, q_heads=62)):
         n = binding.attention_workspace_bytes(_cache(**kw), binding.attention_params(kw["T"], kw["q_heads"], 1.0))
         assert n > 0 and _attention(bytes=n - 1, **kw) == SMALL
+
+
+def test_select_takes_as_many_results_as_its_sentences_may_have():
+    """S * B is bounded, S * N is not: 2^20 sentences of a beam can have 256 results each."""
+    for S, N in ((8192, 200), (1 << 20, 256)):
+        n = binding.select_workspace_bytes(binding.select_params(S, 1, 100, N))
+        assert n > 0 and _select(S=S, B=1, N=N, bytes=n - 1) == SMALL

@@ -274,3 +274,10 @@ def test_many_tiles_with_odd_rows_and_masks():
     y = (rng.standard_normal((B, V)) * 300).astype(np.float32)
     bs = (-3e4 * rng.random(B)).astype(np.float32)
     check(run(to_dev(y), to_dev(bs), S, B, N), y.astype(np.float64), bs, S, B, N)
+
+
+def test_many_sentences_with_many_results():
+    """More than 2^20 results in all."""
+    S, B, V, N = 8192, 1, 300, 200
+    _, x, bs = inputs(22, S, B, V, "f32")
+    check(run(x.cuda(), to_dev(bs), S, B, N), x.double().numpy(), bs, S, B, N)
