@@ -254,7 +254,7 @@ size_t lsh_cache_workspace_bytes(const lsh_cache_params* c);
 
 /* The tables after a step.  Row r = s*B + b continues the tokens of row s*B + parents[r] (a parent outside 0 .. B-1: none) and
  * gets n_new[r] tokens more.
- *   T                 most new tokens of a row in this call
+ *   T                 most new tokens of a row in this call, 1 .. 2^27 (no table holds more)
  *   parents_dev       int32 [S, B] (out_beam of a selection), or NULL: every row continues itself
  *   n_new_dev         int32 [R], each 0 .. T, or NULL: T for rows with a parent, 0 for rows without
  *   tables_in_dev, lengths_in_dev     int32 [R, max_blocks] and [R]; only the entries that a row's length needs are read
@@ -274,14 +274,15 @@ lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t
                              int32_t* lengths_out_dev, int32_t* slots_dev, int32_t* copy_from_dev, int32_t* shared_dev,
                              int32_t* status_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
-/* Keys and values of new tokens (fp32, bf16 or fp16; both of one type) into a layer's pool.
+/* Keys and values of new tokens (fp32, bf16 or fp16; both of one type) into a layer's pool.  T as for lsh_cache_advance.
  *   slots_dev      int32 [R, T] as lsh_cache_advance leaves them: a row's tokens have consecutive positions, -1 behind the
  *                  last.  Slots that no block of the pool has are left out, and so is what follows a gap in a block.
  *   copy_from_dev  int32 [R], or NULL: the block that the row's first block begins as a copy of
  * A block's scale (of each head, of keys and of values) is the smallest power of two, 2^-126 at least, with which its largest
  * finite value is at most 448, 0 for a block of zeros, and never less than its earlier tokens'; codes are rounded to nearest
  * even, NaN and infinities become the code NaN.  Where the scale grows, the block's earlier codes are rounded once more.
- * What lies behind the new tokens in a block stays.  No two rows may have slots in one block. */
+ * What lies behind the new tokens in a block stays.  No two rows may have slots in one block.
+ * LSH_ERR_UNSUPPORTED: more workgroups than a launch has (2^24 pairs of a row and a block that its T tokens may touch). */
 lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool, int32_t T, const void* k_dev, const lsh_rows* k_rows,
                            const void* v_dev, const lsh_rows* v_rows, const int32_t* slots_dev,
                            const int32_t* copy_from_dev, void* hip_stream);

@@ -26,6 +26,7 @@ constexpr int64_t kMaxRows = 1 << 20;
 constexpr int64_t kMaxGrid = (1 << 24) - 1;   // workgroups of 256 threads: fewer than 2^32 threads
 constexpr int kMaxWords = 1 << 24, kMaxBeams = 256;
 constexpr int kMaxBlocks = 1 << 24, kMaxColumns = 1 << 20;
+constexpr int kMaxNew = kMaxColumns * 128;    // tokens that the widest table holds; kernels count new ones in 32 bits, a workgroup's threads at a time
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -245,7 +246,7 @@ lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t
                              const int32_t* tables_in_dev, const int32_t* lengths_in_dev, int32_t* tables_out_dev,
                              int32_t* lengths_out_dev, int32_t* slots_dev, int32_t* copy_from_dev, int32_t* shared_dev,
                              int32_t* status_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    if (!cache_ok(c) || T < 1 || !tables_in_dev || !lengths_in_dev || !tables_out_dev || !lengths_out_dev || !slots_dev || !copy_from_dev ||
+    if (!cache_ok(c) || T < 1 || T > kMaxNew || !tables_in_dev || !lengths_in_dev || !tables_out_dev || !lengths_out_dev || !slots_dev || !copy_from_dev ||
         !status_dev || tables_in_dev == tables_out_dev || lengths_in_dev == lengths_out_dev || !workspace_dev || !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
     const TablesRoom w = tables_room(c);
@@ -275,7 +276,7 @@ lsh_status lsh_cache_advance(const lsh_cache_params* c, int32_t T, const int32_t
 
 lsh_status lsh_cache_write(const lsh_cache_params* c, const lsh_cache_pool* pool, int32_t T, const void* k_dev, const lsh_rows* k_rows,
                            const void* v_dev, const lsh_rows* v_rows, const int32_t* slots_dev, const int32_t* copy_from_dev, void* hip_stream) {
-    if (!cache_ok(c) || !pool_ok(pool) || T < 1 || !k_dev || !v_dev || !slots_dev || !pitch_ok(k_rows, c->head_dim) ||
+    if (!cache_ok(c) || !pool_ok(pool) || T < 1 || T > kMaxNew || !k_dev || !v_dev || !slots_dev || !pitch_ok(k_rows, c->head_dim) ||
         !pitch_ok(v_rows, c->head_dim) || k_rows->dtype != v_rows->dtype || !aligned(k_dev, type_bytes(k_rows->dtype)) ||
         !aligned(v_dev, type_bytes(v_rows->dtype)))
         return LSH_ERR_INVALID_ARG;

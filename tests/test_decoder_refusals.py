@@ -161,3 +161,10 @@ def test_select_takes_as_many_results_as_its_sentences_may_have():
     for S, N in ((8192, 200), (1 << 20, 256)):
         n = binding.select_workspace_bytes(binding.select_params(S, 1, 100, N))
         assert n > 0 and _select(S=S, B=1, N=N, bytes=n - 1) == SMALL
+
+
+@pytest.mark.parametrize("T", [(1 << 27) + 1, (1 << 31) - 256, (1 << 31) - 1])
+def test_more_new_tokens_than_any_table_holds(T):
+    """2^20 blocks of 128 tokens are the most; counting beyond 2^31 by a workgroup's threads would pass 32 bits."""
+    assert _advance(T=T) == INVALID
+    assert _write(T=T) == INVALID and _write(T=T, block=128) == INVALID
