@@ -301,7 +301,8 @@ typedef struct {
 size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attention_params* p);
 
 /* out = softmax(scale * q k^T over the positions a token sees) v.
- *   q_dev        [R, T, n_heads, head_dim] with pitches q_rows; out_dev the same with out_rows, of the same type
+ *   q_dev        [R, T, n_heads, head_dim] with pitches q_rows; out_dev the same with out_rows, of the same type, no two of
+ *                its heads on each other
  *   tables_dev, lengths_dev   as lsh_cache_advance leaves them (a row's new tokens count); blocks outside the pool are not seen
  *   n_new_dev    int32 [R], or NULL: T.  Token t < n of a row is at position lengths[r] - n + t; what stands in out and lse
  *                behind a row's n-th token stays

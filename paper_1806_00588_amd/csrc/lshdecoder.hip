@@ -81,6 +81,32 @@ bool pitch_ok(const lsh_rows* x, int32_t head_dim) {
     return x && type_ok(x->dtype) && x->row >= 0 && x->token >= 0 && x->head >= 0 && head_dim > 0;
 }
 
+// Do two of the heads of x, D values each, lie on each other?  There is a difference of two rows, tokens and heads, not all 0, with
+// |dr row + dt token + dh head| < D.  Pitches that each reach over what lies within them (as views have, in any order) are seen at once; else the two
+// dimensions with the fewest members are gone through, and the third's difference follows (at most some 2^18 turns: R T n_heads <= 2^26).
+bool heads_overlap(const lsh_rows* x, int64_t R, int64_t T, int64_t n_heads, int32_t D) {
+    struct Dim { int64_t n; __int128 pitch; } dim[3] = {{R, x->row}, {T, x->token}, {n_heads, x->head}};
+    std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.pitch < b.pitch; });
+    __int128 reach = D;
+    bool nested = true;
+    for (const Dim& d : dim) {
+        if (d.n > 1 && d.pitch < reach) nested = false;
+        reach += (d.n - 1) * d.pitch;
+    }
+    if (nested) return false;
+    std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.n < b.n; });
+    for (int64_t i = 0; i < dim[0].n; ++i)
+        for (int64_t j = i > 0 ? 1 - dim[1].n : 0; j < dim[1].n; ++j) {
+            const __int128 s = i * dim[0].pitch + j * dim[1].pitch, p = dim[2].pitch;
+            const __int128 below = p == 0 ? 0 : s > 0 ? -((s + p - 1) / p) : -s / p;   // the largest k with s + k p <= 0
+            for (__int128 k = below; k <= below + 1; ++k) {
+                const __int128 off = s + k * p;
+                if (k > -dim[2].n && k < dim[2].n && off < D && off > -D && (i != 0 || j != 0 || k != 0)) return true;
+            }
+        }
+    return false;
+}
+
 struct TablesRoom { size_t plan, base, free_ids, used, bytes; };
 TablesRoom tables_room(const lsh_cache_params* c) {
     const size_t R = (size_t)c->S * c->B;
@@ -318,6 +344,7 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
         !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
     if (!rows_fit(c, p)) return LSH_ERR_UNSUPPORTED;
+    if (heads_overlap(out_rows, (int64_t)c->S * c->B, p->T, p->n_heads, c->head_dim)) return LSH_ERR_INVALID_ARG;
     const AttnPlan plan = attention_plan(c, p, q_rows->dtype, shared_dev != nullptr);
     if (!plan.fits()) return LSH_ERR_UNSUPPORTED;
     const int64_t rows = query_rows(c, p);

@@ -32,9 +32,10 @@ def _attention_calls():
     for D in range(16, 257, 16):
         for ty in (0, 1, 2):
             for T in (1, 15, 16, 17, 32, 33, 48, 49, 50, 63, 64, 65, 97, 128, 200, 1000):
-                yield dict(head_dim=D, q_type=ty, out_type=ty, T=T, q_heads=2)
+                yield dict(head_dim=D, q_type=ty, out_type=ty, T=T, q_heads=2, out_pitch=(2 * T * D, 2 * D, D))
             for B, group in ((4, 1), (12, 4), (16, 1), (17, 1), (12, 3), (25, 2), (5, 10), (8, 8), (64, 1), (13, 5), (256, 16)):
-                yield dict(head_dim=D, q_type=ty, out_type=ty, S=1, B=B, q_heads=2 * group, max_blocks=20000, n_blocks=30000, shared=1 << 20)
+                yield dict(head_dim=D, q_type=ty, out_type=ty, S=1, B=B, q_heads=2 * group, out_pitch=(2 * group * D, 0, D), max_blocks=20000,
+                           n_blocks=30000, shared=1 << 20)
 
 
 def test_every_launch_of_the_attention_has_the_lds_it_asks_for(record):
@@ -50,7 +51,7 @@ def test_every_launch_of_the_attention_has_the_lds_it_asks_for(record):
 
 def test_a_launch_that_is_refused_leaves_no_error_behind(record):
     """More LDS than the runtime gives: the call says so, and the caller's next look at HIP's last error finds none."""
-    calls = [("attention", dict(T=40, q_heads=2, head_dim=128)), ("attention", dict(S=1, B=64, q_heads=2, head_dim=128, max_blocks=20000, n_blocks=30000, shared=1 << 20))]
+    calls = [("attention", dict(T=40, q_heads=2, head_dim=128, out_pitch=(10240, 256, 128))), ("attention", dict(S=1, B=64, q_heads=2, head_dim=128, out_pitch=(256, 0, 128), max_blocks=20000, n_blocks=30000, shared=1 << 20))]
     assert [g["status"] for g in record(calls)] == [0, 0]
     for got in record(calls, refuse=1 << 10):
         assert got["status"] == 5 and got["last_error"] == 0, got

@@ -105,10 +105,10 @@ def test_write_refuses_more_workgroups_than_a_launch_has():
 
 def _attention(**kw):
     a = dict(T=1, q_heads=4, causal=1, window=0, scale=1.0, pool=_pool(), q=P, q_type=0, out_type=0, tables=P, lengths=P, n_new=None, shared=None,
-             ws=P, bytes=BIG, out=P, lse=None)
+             ws=P, bytes=BIG, out=P, lse=None, out_pitch=(256, 256, 64))
     a.update({k: v for k, v in kw.items() if k not in CACHE})
     p = binding.AttentionParams(a["T"], a["q_heads"], a["causal"], a["window"], a["scale"])
-    qr, orow = binding._Rows(a["q_type"], 256, 256, 64), binding._Rows(a["out_type"], 256, 256, 64)
+    qr, orow = binding._Rows(a["q_type"], 256, 256, 64), binding._Rows(a["out_type"], *a["out_pitch"])
     return _lib().lsh_cache_attention(ctypes.byref(_cache(**kw)), ctypes.byref(a["pool"]), ctypes.byref(p), a["q"], ctypes.byref(qr), a["tables"],
                                       a["lengths"], a["n_new"], a["shared"], a["ws"], a["bytes"], a["out"], ctypes.byref(orow), a["lse"], None)
 
@@ -153,7 +153,7 @@ def test_attention_workspace_of_many_rows_goes_with_the_call():
     """Up to the last supported call the workspace has a size, and a byte less than that is too little."""
     for kw in (dict(S=1, B=1, T=1 << 20, q_heads=62), dict(S=1 << 12, B=256, T=1, q_heads=10), dict(S=1, B=256, T=1 << 12, q_heads=62)):
         n = binding.attention_workspace_bytes(_cache(**kw), binding.attention_params(kw["T"], kw["q_heads"], 1.0))
-        assert n > 0 and _attention(bytes=n - 1, **kw) == SMALL
+        assert n > 0 and _attention(bytes=n - 1, out_pitch=side_by_side(kw["T"], kw["q_heads"], 64), **kw) == SMALL
 
 
 def test_select_takes_as_many_results_as_its_sentences_may_have():
@@ -168,3 +168,37 @@ def test_more_new_tokens_than_any_table_holds(T):
     """2^20 blocks of 128 tokens are the most; counting beyond 2^31 by a workgroup's threads would pass 32 bits."""
     assert _advance(T=T) == INVALID
     assert _write(T=T) == INVALID and _write(T=T, block=128) == INVALID
+
+
+def side_by_side(T, heads, D):
+    """Pitches of rows, tokens and heads with nothing between them."""
+    return T * heads * D, heads * D, D
+
+
+def _places(R, T, H, D, pitch):
+    """Whether heads lie on each other, by writing down every place."""
+    at = [r * pitch[0] + t * pitch[1] + h * pitch[2] + d for r in range(R) for t in range(T) for h in range(H) for d in range(D)]
+    return len(set(at)) < len(at)
+
+
+def test_results_that_lie_on_each_other_are_refused():
+    """Several workgroups would write the same place.  16 values a head, rows 2 * 3, any order of the three pitches and any distance."""
+    import itertools
+    kw = dict(head_dim=16, n_heads=1)
+    seen = {False: 0, True: 0}
+    for T, H in ((1, 1), (1, 3), (2, 1), (3, 2), (4, 3)):
+        n = binding.attention_workspace_bytes(_cache(**kw), binding.attention_params(T, H, 1.0))
+        for pitch in itertools.product((0, 8, 15, 16, 17, 32, 33, 48, 64, 96, 112, 200, 1000, 1 << 40, (1 << 62) + 5), repeat=3):
+            overlap = _places(6, T, H, 16, pitch)
+            seen[overlap] += 1
+            assert _attention(T=T, q_heads=H, out_pitch=pitch, bytes=n - 1, **kw) == (INVALID if overlap else SMALL), (T, H, pitch)
+    assert min(seen.values()) > 1000
+    # many heads, tokens and rows
+    for T, H, S, B in ((1000, 64, 4, 2), (1 << 13, 8, 1, 256), (1, 32, 1 << 10, 256)):
+        row, token, head = side_by_side(T, H, 64)
+        many = dict(T=T, q_heads=H, S=S, B=B, bytes=0)
+        assert _attention(out_pitch=(row, token, head), **many) == SMALL
+        assert _attention(out_pitch=(64, 64 * S * B * H, 64 * S * B), **many) == SMALL      # heads of all rows together
+        assert _attention(out_pitch=(row - 1, token, head), **many) == INVALID
+        assert _attention(out_pitch=(row, token, head - 1), **many) == INVALID
+        assert _attention(out_pitch=(row + 1, token + 1, head), **many) == (SMALL if T == 1 else INVALID)
