@@ -33,6 +33,22 @@ def test_wide_heads_in_fp32_over_common_blocks(B, group, D):
     common_rows(D, "f32", B, group)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [80, 128, 144, 192, 256])
+@pytest.mark.parametrize("T,group", [(10, 4), (49, 1), (16, 4), (25, 4)])
+def test_rows_of_every_head_size(T, group, D, dtype):
+    """40, 49, 64 and 100 rows: three waves, four of them, two groups of four."""
+    own_rows(D, dtype, T, group)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [80, 128, 144, 192, 256])
+@pytest.mark.parametrize("B,group", [(8, 5), (7, 7), (16, 4), (25, 4), (6, 17)])
+def test_rows_of_every_head_size_over_common_blocks(B, group, D, dtype):
+    """The same, and (102 rows, 17 of a beam) with more than one wave for the beams' own parts too."""
+    common_rows(D, dtype, B, group)
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("T,group,D", [(6, 1, 64), (6, 2, 80), (18, 2, 128), (18, 3, 48)])
