@@ -332,7 +332,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnPlace& 
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sc[i >> 2][i & 3] * k_scale;
     if (!whole) {   // the row sees tokens from .. end - 1 of the lane's
-        const int from = max(lo - first, 0), end = has ? min(hi, p.vhi) - first : 0;
+        const int from = lo > first ? lo - first : 0, end = has ? min(hi, p.vhi) - first : 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = i >= from && i < end ? x[i] : -INFINITY;
         if (from >= min(end, 16)) v_scale = 0.f;   // (none of them: 0 times a scale that is not finite would be NaN)
