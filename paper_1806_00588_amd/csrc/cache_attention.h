@@ -177,7 +177,7 @@ __device__ __forceinline__ void find_positions(const AttnArgs& a, AttnPlace& p, 
     const bool live = w.valid && w.lo < w.hi;
     int vlo = live ? w.lo : INT32_MAX, vhi = live ? w.hi : 0;
     // a row without a position here is worked on like the rest and left out at the end
-    if (!live) { w.lo = INT32_MIN; w.hi = INT32_MAX; }
+    if (!live) { w.lo = 0; w.hi = INT32_MAX; }
     int lo_most = w.lo, hi_least = w.hi;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
@@ -332,7 +332,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const AttnPlace& 
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sc[i >> 2][i & 3] * k_scale;
     if (!whole) {   // the row sees tokens from .. end - 1 of the lane's
-        const int from = lo > first ? lo - first : 0, end = has ? min(hi, p.vhi) - first : 0;
+        const int from = max(lo - first, 0), end = has ? min(hi, p.vhi) - first : 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = i >= from && i < end ? x[i] : -INFINITY;
         if (from >= min(end, 16)) v_scale = 0.f;   // (none of them: 0 times a scale that is not finite would be NaN)
@@ -515,7 +515,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, unsigned unit, uin
         }
     }
     // the four waves' results together
-    const bool live = lo != INT32_MIN;
+    const bool live = hi != INT32_MAX;
     sums.l += __shfl_xor(sums.l, 16, kWave);
     sums.l += __shfl_xor(sums.l, 32, kWave);
     if (c == 0) { wave_m[wv][n16] = live ? sums.m : -INFINITY; wave_l[wv][n16] = live ? sums.l : 0.f; }
@@ -643,7 +643,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, unsigned unit, ui
         }
     }
     if (!row.valid) return;
-    const bool live = row.lo != INT32_MIN;
+    const bool live = row.hi != INT32_MAX;
     float l = sums.l;
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
