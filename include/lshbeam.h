@@ -195,9 +195,10 @@ size_t lsh_select_workspace_bytes(const lsh_select_params* p);
  *   allowed_dev      NULL, or bits: bit w % 32 of 32-bit word w / 32 of a row says that word w may follow.  A word that may not
  *                    counts as a logit of -inf, whatever stands there (a NaN too).
  *   workspace_dev    as for lsh_decode_step.
- * log-probability = logit - log sum exp over the row's allowed words; score = beam score + log-probability, both in 64 bits; per
- * sentence the N best pairs, best first, equal scores ordered by lower beam then lower word.  Pairs whose score is not finite
- * in fp32 are none: a row with a NaN or +inf among its allowed logits, or with no allowed word, has no pair.
+ * log-probability = logit - log sum exp over the row's allowed words (so what is not allowed makes the others more likely);
+ * score = beam score + log-probability, both in 64 bits; per sentence the N best pairs, best first, equal scores ordered by
+ * lower beam then lower word.  Pairs whose score is not finite in fp32 are none: a row with a NaN or +inf among its allowed
+ * logits, or with no allowed word, has no pair.
  *   out_beam_dev / out_word_dev / out_score_dev   [S, N]; behind the last pair (-1, -1, -inf).  With N = B as
  *                    lsh_beam_advance takes them.
  *   out_lse_dev      fp32 [S*B], or NULL: log sum exp of each row (-inf without an allowed word).
@@ -310,7 +311,8 @@ size_t lsh_attention_workspace_bytes(const lsh_cache_params* c, const lsh_attent
  *   lse_dev      fp32 [R, T, n_heads], or NULL: log sum exp of the scaled products
  * A token that sees nothing gets zeros and an lse of -inf.  What a token does not see (keys, values, scales of
  * blocks) does not reach its result, a NaN neither.
- * Products and sums are fp32 (queries of 16 bits: the probabilities are rounded to bf16 for bf16, kept to 16 bits for fp16).
+ * Products and sums are fp32 (queries of 16 bits: the probabilities are rounded to bf16 for bf16, cut to their first 16 bits for
+ * fp16; fp32 keeps all of them).
  * Asynchronous on the stream, allocates nothing; the same inputs give the same outputs bit for bit. */
 lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* pool, const lsh_attention_params* p, const void* q_dev,
                                const lsh_rows* q_rows, const int32_t* tables_dev, const int32_t* lengths_dev,

@@ -6,7 +6,12 @@
 // sentence's beams have their first blocks in common -- the beams.  Those are the columns of v_mfma_f32_16x16x32_bf16:
 //   S^T [tokens, rows] = K Q^T      O^T [values, rows] += V^T P^T
 // A code is exact in bf16.  Queries of 16 or 32 bits are taken apart into bf16 planes whose sum they are (bf16 1, fp16 2, fp32 3),
-// and so are the probabilities (bf16: rounded, half a step of 2^-8; fp16: the first 16 bits; fp32: all 24), products and sums are fp32.
+// and so are the probabilities, products and sums are fp32.  What the probabilities lose, and why no more is kept:
+//   bf16  rounded, at most 2^-8 of each.  Many of them add up, and the result is rounded to bf16 itself: 1.2e-3 off 64 bits in the mean,
+//         3e-4 off what probabilities of 32 bits give.  A second plane (16 bits) costs, 16 sentences of 12 beams over 8000 common
+//         tokens, 126 us against 114, a prompt of 4096 tokens 368 against 328.
+//   fp16  cut behind 16 bits: up to 2^-16 too small, where the result's own rounding is 2^-12 to 2^-11.  fp32: all 24 bits.
+// log2 e is one fp32 number, 1.3e-8 of it off; rounding its product with the scale can cost 6e-8.
 //
 // A wave takes tiles of 64 tokens.  Row m of the K operand of sub-tile i is token 16 (m / 4) + 4 i + m % 4, so that lane (n, c) of the
 // result holds, for row n of the queries, tokens 16 c + 4 i + j: the sixteen neighbours 16 c .. 16 c + 15, which are its part of the
@@ -16,8 +21,8 @@
 // k_attention_few   up to 16 rows of queries (of a row, or of all beams over what they have in common): the four waves of a workgroup
 //                   take every fourth tile, straight from memory into registers (values of this tile asked for, products with its
 //                   keys, keys of the next tile asked for, softmax, products with the values), and join through LDS.  Bound by
-//                   memory: 64 rows of 8192, 32 heads on 8 of 128, fp16 198 us, 5.4 TB/s; 4 rows of 60 7.5 us, a chain of trips.
-// k_attention_rows  17 to 64 rows (48 of fp32 with heads of more than 192): a wave per 16 rows, all on the same tiles, which come through LDS two
+//                   memory: 64 rows of 8192, 32 heads on 8 of 128, fp16 190 us, 5.6 TB/s; 4 rows of 60 7.3 us, a chain of trips.
+// k_attention_rows  17 to 64 rows (48 of fp32 in the code for heads of 256): a wave per 16 rows, all on the same tiles, which come through LDS two
 //                   tiles ahead.
 // k_attention_both  the common blocks' workgroups of either kind and the rows' own in one launch.
 // The rows of a row set are split along the tokens into chunks, a workgroup's work.  Chunks leave (max, sum, products) in the
@@ -564,8 +569,9 @@ template <int TYPE, int DP> constexpr int kRowsMost = kRowsLds<TYPE, DP, 4> + (i
 
 // The same grid, MT waves: wave w has rows 16 w .. 16 w + 15 of the group.  Bound by how many workgroups a CU holds and by what each of
 // them does one thing after the other (about 1.3 us a tile): 16 sentences of 12 beams over 8000 common tokens of 8 heads, D = 128, bf16, 264 MB
-// in 80 us.  Measured and not kept: two waves per 16 rows, each for half the tokens (108 us); queries in registers and a third
-// workgroup on a CU (81); all rows in each wave and tiles in registers as above (some 500 registers, which do not last).
+// in 80 us as a launch of its own.  Of the time of its waves half is waiting (for tiles and at barriers), a quarter vector instructions, a
+// hundredth waiting for LDS.  Measured against those 80 and not kept: two waves per 16 rows, each for half the tokens (108); queries in
+// registers and a third workgroup on a CU (81); all rows in each wave and tiles in registers as above (some 500 registers, which do not last).
 template <int TYPE, int DP, int MT, bool EXACT>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, unsigned unit, uint4* lds, AttnShared& sh) {
     constexpr int KK = DP / 64, DT = DP / 16, STAGES = kRowsStages<DP>, TILE = 2 * DT * 64;   // uint4 of a tile: keys [kk, i, lane], values [dt, lane]
@@ -659,7 +665,8 @@ __global__ void __launch_bounds__(64 * MT, 2) k_attention_rows(AttnArgs a) {
     attend_rows<TYPE, DP, MT, EXACT>(a, blockIdx.x, lds, sh);
 }
 
-// 4 sentences of 12 beams over 8192 common tokens, 32 heads on 8 of 128, bf16: 36.8 us a call, 39.8 as two launches (26 and 10).
+// 4 sentences of 12 beams over 8192 common tokens, 32 heads on 8 of 128, bf16: 37 us a call, 40 as two launches (26 and 10); 16 sentences of 12
+// beams, 8000 of 8192 tokens common, 338 MB: 104 us, the join 9.
 // What a sentence's beams have in common (the first `units` workgroups; MT: waves of each, 1: all four with at most 16 rows) and each
 // row's own part in one launch: neither waits for the other.  The waves behind the MT-th end at once, and a barrier does not wait for
 // waves that have ended.
@@ -675,7 +682,7 @@ __global__ void __launch_bounds__(256, 2) k_attention_both(BothArgs b) {
     else if (__builtin_amdgcn_readfirstlane(wave_id()) < MT) attend_rows<TYPE, DP, MT, EXACT>(b.common, blockIdx.x, lds, few.sh);
 }
 
-// Bound by latency: 4 to 6 us for 1500 to 2000 rows of some parts each.  A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.
+// Bound by latency: 5 to 6 us for 1500 to 2000 rows of some parts each.  A wave per row of the queries adds up its parts, in order: D / 4 lanes (up to the next power of two) take every so many-th part.
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_attention_join(AttnArgs a) {
     const int64_t at = (int64_t)blockIdx.x * 4 + wave_id(), rt = at / a.q_heads;

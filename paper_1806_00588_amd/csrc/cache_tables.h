@@ -7,8 +7,8 @@
 //
 // Bound by latency: three dependent passes (who continues with what; how many blocks each row needs and which are free; tables
 // and slots) over a few bytes.  Small calls are one workgroup's (k_tables_once), which has plans and a bitmap of the pool in LDS:
-// 12 rows of 20 blocks 6.7 us, where the four launches of the others take 17 to be made (640 rows of 256 blocks: kernels of 1.9, 5.0,
-// 4.0 and 5.6).
+// 12 rows of 20 blocks 6.5 to 7.5 us, where the four launches of the others take 15 to 16 to be made (640 rows of 256 blocks: kernels of 1.8,
+// 5.1, 4.0 and 5.6).
 #pragma once
 #include "device_utils.h"
 
@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(256) k_tables_finish(TablesArgs a) {
 }
 
 // One workgroup does all of it.  LDS: the rows' plans, parents, last blocks and bases, a bit for each block of the pool (18 KB at most).
-// The limits are where it is no slower than the four launches, which take 14 to 16 us a call whatever the size: 12 rows of 20 blocks
-// 7.6 us, 64 of 64 10.7 (a pool of 4096 blocks; 13 with 131 072), 4 of 1024 8 to 15; beyond them 160 rows of 64 23, 1024 of 32 70, and
+// The limits are where it is no slower than the four launches, which take 15 to 16 us a call whatever the size: 12 rows of 20 blocks
+// 7.8 us a call, 64 of 64 10.7 (a pool of 4096 blocks; 13 with 131 072), 4 of 1024 8 to 15; beyond them 160 rows of 64 23, 1024 of 32 70, and
 // one row of 4096 new tokens 57, 8 of 512 13 to 18.
 constexpr int kOnceRows = 64, kOnceEntries = 4096, kOnceBlocks = 1 << 17, kOnceNew = 256, kOnceSlots = 2048;
 inline bool tables_at_once(int64_t R, int64_t width, int64_t n_blocks, int64_t T) {
