@@ -12,8 +12,8 @@ A case is a dict of plain values.  Kinds:
 Codes lie as [ceil(N / 16), ceil(K / 128), 4, 16, 16] bytes: 16 outputs and 128 inputs at a time, of them the c-th eight of
 every 32, an output, four words of 32 bits (one for each 32 inputs).  Byte i of a word holds input i of its eight in the lower and input
 i + 4 in the upper four bits.
-Scales [ceil(K / group), 16 ceil(N / 16)] of 16 bits, zeros the same in bytes; a value is (code - zero) * scale, the zero 8 where
-there are none.
+Scales [ceil(N / 16), ceil(K / 128), 16, 128 / group] of 16 bits, zeros the same in bytes: those of an output's groups of 128 inputs
+side by side; a value is (code - zero) * scale, the zero 8 where there are none.
 
 With `own` false the operators are computed from their formulas with elementary torch operations, otherwise by the package.
 """
@@ -128,11 +128,11 @@ def _weights(c, g):
     """Codes as rounding normal values leaves them, scales of a trained layer's size.  What stands behind the last output or
     input is never zeros: nobody clears it."""
     N, K = c["N"], c["K"]
-    tiles, parts, groups = -(-N // 16), -(-K // 128), -(-K // c["group"])
+    tiles, parts, each = -(-N // 16), -(-K // 128), 128 // c["group"]
     low, high = ((_randn(g, tiles, parts, 4, 16, 16) * 2.6).round_().clamp_(-7, 7).to(torch.int8) + 8 for _ in range(2))
     codes = (low + high * 16).view(torch.uint8)
-    scales = (torch.exp(_randn(g, groups, 16 * tiles) * 0.4) * (0.4 / math.sqrt(K))).to(DTYPES[c["scale"]])
-    zeros = torch.randint(4, 12, (groups, 16 * tiles), device="cuda", generator=g).to(torch.uint8) if c["zeros"] else None
+    scales = (torch.exp(_randn(g, tiles, parts, 16, each) * 0.4) * (0.4 / math.sqrt(K))).to(DTYPES[c["scale"]])
+    zeros = torch.randint(4, 12, (tiles, parts, 16, each), device="cuda", generator=g).to(torch.uint8) if c["zeros"] else None
     return {"codes": codes, "scales": scales, "zeros": zeros}
 
 
@@ -168,11 +168,11 @@ def prepare(case, seed):
         return st
     if c["kind"] == "quantize":
         N, K = c["N"], c["K"]
-        tiles, groups = -(-N // 16), -(-K // c["group"])
+        tiles, parts, each = -(-N // 16), -(-K // 128), 128 // c["group"]
         st["w"] = (_randn(g, N, K) * torch.exp(_randn(g, N, 1) * 0.3) * (1.0 / math.sqrt(K))).to(DTYPES[c["dtype"]])
-        st["codes"] = torch.zeros(tiles, -(-K // 128), 4, 16, 16, dtype=torch.uint8, device="cuda")
-        st["scales"] = torch.zeros(groups, 16 * tiles, dtype=DTYPES[c["scale"]], device="cuda")
-        st["zeros"] = torch.zeros(groups, 16 * tiles, dtype=torch.uint8, device="cuda") if c["zeros"] else None
+        st["codes"] = torch.zeros(tiles, parts, 4, 16, 16, dtype=torch.uint8, device="cuda")
+        st["scales"] = torch.zeros(tiles, parts, 16, each, dtype=DTYPES[c["scale"]], device="cuda")
+        st["zeros"] = torch.zeros(tiles, parts, 16, each, dtype=torch.uint8, device="cuda") if c["zeros"] else None
         st["values"] = torch.empty_like(st["w"])
         return st
     M, N, K = c["M"], c["N"], c["K"]
@@ -208,11 +208,24 @@ def _packed(codes, tiles, parts):
     return (both[..., 0::2] | both[..., 1::2] << 4).flatten(-2).contiguous()
 
 
+def _of_groups(x, c):
+    """[N, groups] numbers of a tensor of scales or zeros."""
+    return x.permute(0, 2, 1, 3).flatten(2).flatten(0, 1)[:c["N"], :-(-c["K"] // c["group"])].float()
+
+
+def _to_groups(x, to):
+    """The other way round, as they lie, 0 behind the last."""
+    all_of = torch.zeros(16 * to.shape[0], to.shape[1] * to.shape[3], dtype=x.dtype, device="cuda")
+    all_of[:x.shape[0], :x.shape[1]] = x
+    to.copy_(all_of.view(to.shape[0], 16, to.shape[1], to.shape[3]).permute(0, 2, 1, 3))
+
+
 def _values(w, c):
     N, K, group = c["N"], c["K"], c["group"]
-    zero = w["zeros"][:, :N].float().t() if w["zeros"] is not None else torch.full((N, w["scales"].shape[0]), 8.0, device="cuda")
+    scale = _of_groups(w["scales"], c)
+    zero = _of_groups(w["zeros"], c) if w["zeros"] is not None else torch.full_like(scale, 8.0)
     part = torch.arange(K, device="cuda") // group
-    return (_unpacked(w["codes"], N, K).float() - zero[:, part]) * w["scales"][:, :N].float().t()[:, part]
+    return (_unpacked(w["codes"], N, K).float() - zero[:, part]) * scale[:, part]
 
 
 def _act(x, name):
@@ -234,23 +247,23 @@ def _quantize_plain(st, c):
         scale = (hi - lo) / 15
     else:
         scale = w.abs().amax(2).double() / 7
-    # (quotients next to a half: 64 bits, rounded once)
+    # (what is next to a border: 64 bits; the scale rounded to 32 bits and then to 16)
     scale = scale.to(DTYPES[c["scale"]])
     s = torch.where(scale > 0, scale.double(), torch.full_like(scale, math.inf, dtype=torch.float64))
     zero = (-lo / s).round().clamp(0, 15) if c["zeros"] else torch.full_like(s, 8.0)
     code = ((w / s[..., None]).round() + zero[..., None]).clamp(0, 15).to(torch.uint8).flatten(1)[:, :K]
     st["codes"].copy_(_packed(code, tiles, parts))
-    st["scales"][:, :N] = scale.t()
+    _to_groups(scale, st["scales"])
     if c["zeros"]:
-        st["zeros"][:, :N] = zero.t().to(torch.uint8)
+        _to_groups(zero, st["zeros"])
     st["values"].copy_(_values(st, c))
     return _quantized(st, c)
 
 
 def _quantized(st, c):
-    out = {"values": st["values"], "scales": st["scales"][:, :c["N"]]}
+    out = {"values": st["values"], "scales": st["scales"]}
     if c["zeros"]:
-        out["zeros"] = st["zeros"][:, :c["N"]]
+        out["zeros"] = st["zeros"]
     return out
 
 
@@ -372,10 +385,11 @@ def _exact_matrix(w, c):
     for place, i in enumerate(PLACES):
         to[..., i] = (words >> (4 * place) & 15).double().permute(0, 3, 1, 4, 2)
     m = m[:N, :K]
-    for at in range(w["scales"].shape[0]):
+    each = 128 // group
+    for at in range(-(-K // group)):
         part = m[:, at * group:(at + 1) * group]
-        part -= w["zeros"][at, :N, None].double() if w["zeros"] is not None else 8.0
-        part *= w["scales"][at, :N, None].double()
+        part -= w["zeros"][:, at // each, :, at % each].reshape(-1, 1)[:N].double() if w["zeros"] is not None else 8.0
+        part *= w["scales"][:, at // each, :, at % each].reshape(-1, 1)[:N].double()
     return m
 
 
@@ -384,26 +398,25 @@ def exact(case, seed):
     st = prepare(c, seed)
     if c["kind"] == "quantize":
         N, K, group = c["N"], c["K"], c["group"]
-        scales = torch.zeros(st["scales"].shape[0], N, dtype=torch.float64, device="cuda")
+        tiles, parts, _, each = st["scales"].shape
+        scales, zeros = (torch.zeros(16 * tiles, parts * each, dtype=torch.float64, device="cuda") for _ in range(2))
         values = torch.zeros(N, K, dtype=torch.float64, device="cuda")
-        zeros = torch.zeros_like(scales)
-        for at in range(scales.shape[0]):
+        for at in range(-(-K // group)):
             part = st["w"][:, at * group:(at + 1) * group].double()
             if c["zeros"]:
                 least, most = torch.clamp(part.amin(1), max=0), torch.clamp(part.amax(1), min=0)
                 step = ((most - least) / 15).to(DTYPES[c["scale"]]).double()
-                zeros[at] = torch.clamp(torch.round(torch.nan_to_num(-least / step)), 0, 15)
-                lowest, highest = -zeros[at], 15 - zeros[at]
+                zero = torch.clamp(torch.round(torch.nan_to_num(-least / step)), 0, 15)
+                zeros[:N, at] = zero
+                lowest, highest = -zero, 15 - zero
             else:
                 step = (part.abs().amax(1) / 7).to(DTYPES[c["scale"]]).double()
                 lowest, highest = torch.full_like(step, -8), torch.full_like(step, 7)
             whole = torch.round(torch.nan_to_num(part / step[:, None]))
             values[:, at * group:(at + 1) * group] = torch.minimum(torch.maximum(whole, lowest[:, None]), highest[:, None]) * step[:, None]
-            scales[at] = step
-        out = {"values": values, "scales": scales}
-        if c["zeros"]:
-            out["zeros"] = zeros
-        return out
+            scales[:N, at] = step
+        scales, zeros = (x.view(tiles, 16, parts, each).transpose(1, 2) for x in (scales, zeros))
+        return {"values": values, "scales": scales, "zeros": zeros} if c["zeros"] else {"values": values, "scales": scales}
     if c["kind"] == "linear":
         y = torch.matmul(st["x"].double(), _exact_matrix(st["w"], c).t())
         if st["bias"] is not None:
