@@ -320,6 +320,112 @@ lsh_status lsh_cache_attention(const lsh_cache_params* c, const lsh_cache_pool* 
                                size_t workspace_bytes, void* out_dev, const lsh_rows* out_rows, float* lse_dev,
                                void* hip_stream);
 
+/* ---- layers of a decoder: weights of 4 bits, a recurrent state with a gated delta rule -----------------------------------
+ *
+ * What a decoder's own layers spend a step on.  A layer's products are y = x W^T for a few rows of x (a row for each beam) or many
+ * (prompts), with the weights W [N outputs, K inputs] packed; lsh_delta_rule is attention's place in layers that keep a state of
+ * fixed size instead of keys and values:
+ *   lsh_packed_quantize   once: weights to codes, scales (and zeros); lsh_packed_values reads them back
+ *   lsh_packed_linear     projections, the output layer (its result in fp32 as lsh_beam_select takes it)
+ *   lsh_packed_gated      the first half of a gated feed-forward block, lsh_packed_linear being the second
+ *   lsh_delta_rule        new tokens of rows, each from the state that its parent left
+ * All calls are made with the device that the memory lies on current, are asynchronous on the stream and allocate nothing; workspaces as
+ * for the cache.  The same inputs give the same outputs bit for bit, and a row's results do not depend on where its results lie. */
+
+typedef struct {
+    int32_t N;          /* outputs, 1 .. 2^24                                                           */
+    int32_t K;          /* inputs, 1 .. 2^20                                                            */
+    int32_t group;      /* inputs with a scale (and a zero) of their own: 32, 64 or 128                 */
+} lsh_packed_params;
+
+/* Weights of 4 bits: device memory, caller-owned, at multiples of 16 bytes.  With tiles = ceil(N / 16), parts = ceil(K / 128):
+ *   codes    [tiles, parts, 4, 16, 16] bytes: 16 outputs and 128 inputs together, of them the c-th eight of every 32 inputs, an output,
+ *            four words of 32 bits (one for each 32 inputs).  Byte i of a word holds input i of its eight in the lower and input
+ *            i + 4 in the upper four bits
+ *   scales   [tiles, parts, 16, 128 / group] of scale_dtype, LSH_BF16 or LSH_F16
+ *   zeros    the same in bytes, each 0 .. 15, or NULL: 8 everywhere
+ * A weight is (code - zero) * scale.  What stands behind the last output or input is not used. */
+typedef struct {
+    uint8_t* codes;
+    void* scales;
+    uint8_t* zeros;
+    int32_t scale_dtype;
+} lsh_packed_weights;
+
+/* Where a matrix's rows begin: row r at r * ld elements of `dtype` behind its address, a row's elements side by side. */
+typedef struct {
+    int32_t dtype;
+    int64_t ld;
+} lsh_matrix;
+
+/* W [N, K] (fp32, bf16 or fp16; ld >= K) to codes.  For a group of weights w:
+ *   without zeros   scale = max |w| / 7, code = 8 + round(w / scale)
+ *   with zeros      lo = min(0, w), hi = max(0, w), scale = (hi - lo) / 15, zero = round(-lo / scale), code = zero + round(w / scale)
+ * The scale is rounded to fp32 and then to its type, and used as rounded; the other quotients are exact, rounded to nearest even;
+ * zeros and codes are cut to 0 .. 15, and of a group whose scale is 0 they are 8 (without zeros) or 0.  A group with a NaN or an infinity
+ * gets a scale that is NaN, and codes 0.  Behind the last output or input codes, scales and zeros are set to 0. */
+lsh_status lsh_packed_quantize(const lsh_packed_params* p, const void* w_dev, const lsh_matrix* w, const lsh_packed_weights* to,
+                               void* hip_stream);
+
+/* The weights that codes stand for: out [N, K], fp32, bf16 or fp16, rounded once. */
+lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weights* from, void* out_dev, const lsh_matrix* out,
+                             void* hip_stream);
+
+/* Bytes of workspace lsh_packed_linear and lsh_packed_gated need for M rows of any type (0 on invalid arguments). */
+size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M);
+
+/* out[m, n] = sum_k x[m, k] W[n, k] + bias[n] + add[m, n].
+ *   M          rows, 1 .. 2^20
+ *   x          [M, K] fp32, bf16 or fp16
+ *   bias_dev   fp32 [N], or NULL
+ *   add_dev    [M, N] of out's type, with pitch add_ld, or NULL; it may be out itself (same address and pitch)
+ *   out        [M, N] of any of the three types, on none of the inputs but add
+ * Codes enter the products as they are, whatever x's type; products and sums are fp32, a group's scale and zero are applied to its sum,
+ * the result is rounded once.  A row with a NaN or an infinity gives NaN (or infinities), and no other row does. */
+lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
+                             const float* bias_dev, const void* add_dev, int64_t add_ld, void* workspace_dev, size_t workspace_bytes,
+                             void* out_dev, const lsh_matrix* out, void* hip_stream);
+
+typedef enum { LSH_SILU = 0 /* z / (1 + e^-z) */, LSH_GELU = 1 /* z (1 + erf(z / sqrt 2)) / 2 */,
+               LSH_GELU_TANH = 2 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */ } lsh_activation;
+
+/* out[m, n] = act(sum_k x[m, k] gate[n, k]) * sum_k x[m, k] up[n, k], as lsh_packed_linear; both matrices of the same parameters, each with
+ * or without zeros, scales of one type. */
+lsh_status lsh_packed_gated(const lsh_packed_params* p, const lsh_packed_weights* gate, const lsh_packed_weights* up, int32_t M,
+                            const void* x_dev, const lsh_matrix* x, int32_t activation, void* workspace_dev, size_t workspace_bytes,
+                            void* out_dev, const lsh_matrix* out, void* hip_stream);
+
+typedef struct {
+    int32_t S, B;       /* as in lsh_step_params; rows R = S * B <= 2^20                               */
+    int32_t T;          /* new tokens of a row at most, 1 .. 2^20                                      */
+    int32_t n_heads;    /* heads of values, states and results, a multiple of n_k_heads                */
+    int32_t n_k_heads;  /* heads of queries and keys: head h has those of h / (n_heads / n_k_heads)    */
+    int32_t k_dim;      /* values of a query and a key: a multiple of 16, 16 .. 256                    */
+    int32_t v_dim;      /* values of a value and a result: the same                                    */
+    float scale;        /* of the results, usually 1 / sqrt(k_dim); finite                             */
+} lsh_delta_params;
+
+/* Bytes of workspace lsh_delta_rule needs, for any type (0 on invalid arguments, and where the call would be LSH_ERR_UNSUPPORTED:
+ * R * T * n_heads > 2^26, or more than 2^24 workgroups). */
+size_t lsh_delta_workspace_bytes(const lsh_delta_params* p);
+
+/* For each row and head, token after token, with the state H [k_dim, v_dim], the key k, the value v and the query q of the token:
+ *   u = beta (v - e^decay H^T k),   H <- e^decay H + k u^T,   out = scale H^T q
+ *   q_dev, k_dev        [R, T, n_k_heads, k_dim] with pitches, v_dev [R, T, n_heads, v_dim], out_dev the same; all of one type (fp32, bf16 or
+ *                       fp16), no two of out's heads on each other and none on an input
+ *   decay_dev, beta_dev fp32 [R, T, n_heads]
+ *   state_in_dev        fp32 [R, n_heads, k_dim, v_dim], or NULL: all rows begin with zeros
+ *   parents_dev         int32 [S, B] (out_beam of a selection), or NULL: row s*B + b begins with the state of row s*B + parents[r], with zeros
+ *                       where that is outside 0 .. B-1.  So states need not be moved (lsh_beam_advance) before
+ *   n_new_dev           int32 [R], each 0 .. T, or NULL: T.  Behind a row's last token nothing is read, and what stands in out stays
+ *   state_out_dev       fp32 as state_in: the states afterwards.  It may be state_in itself if parents is NULL; else the two do not overlap
+ * States, sums and everything between the inputs and out are fp32 or more.
+ * Addresses of the states are multiples of 16 bytes. */
+lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,
+                          const void* v_dev, const lsh_rows* v_rows, const float* decay_dev, const float* beta_dev,
+                          const float* state_in_dev, const int32_t* parents_dev, const int32_t* n_new_dev, float* state_out_dev,
+                          void* workspace_dev, size_t workspace_bytes, void* out_dev, const lsh_rows* out_rows, void* hip_stream);
+
 /* ---- inspection (synchronous device-to-host copies; never on the timed path) ---------------- */
 
 /* Band codes (Eq. 6-8) of R fp32 rows of pitch d, computed by the same device hash routine the

@@ -24,6 +24,8 @@ EXPORTED_SYMBOLS = (
     "lsh_static_scratch_bytes", "lsh_debug_counts", "lsh_release_kept",
     "lsh_select_workspace_bytes", "lsh_beam_select", "lsh_cache_workspace_bytes", "lsh_cache_advance", "lsh_cache_write",
     "lsh_attention_workspace_bytes", "lsh_cache_attention",
+    "lsh_packed_quantize", "lsh_packed_values", "lsh_packed_workspace_bytes", "lsh_packed_linear", "lsh_packed_gated",
+    "lsh_delta_workspace_bytes", "lsh_delta_rule",
 )
 
 OPTION_AUTO = -1
@@ -67,6 +69,23 @@ class CacheParams(ctypes.Structure):
 class AttentionParams(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class PackedParams(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class DeltaParams(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int32), ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_k_heads", ctypes.c_int32),
+                ("k_dim", ctypes.c_int32), ("v_dim", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class _WeightPointers(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p), ("scale_dtype", ctypes.c_int32)]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("ld", ctypes.c_int64)]
 
 
 class _PoolPointers(ctypes.Structure):
@@ -145,6 +164,17 @@ def load_library():
     lib.lsh_attention_workspace_bytes.restype = sz
     lib.lsh_cache_attention.argtypes = [ctypes.POINTER(CacheParams), ctypes.POINTER(_PoolPointers), ctypes.POINTER(AttentionParams), vp,
                                         rows, vp, vp, vp, vp, vp, sz, vp, rows, vp, vp]
+    params, weights, matrix, rows = (ctypes.POINTER(x) for x in (PackedParams, _WeightPointers, _Matrix, _Rows))
+    lib.lsh_packed_quantize.argtypes = [params, vp, matrix, weights, vp]
+    lib.lsh_packed_values.argtypes = [params, weights, vp, matrix, vp]
+    lib.lsh_packed_workspace_bytes.argtypes = [params, i32]
+    lib.lsh_packed_linear.argtypes = [params, weights, i32, vp, matrix, vp, vp, ctypes.c_int64, vp, sz, vp, matrix, vp]
+    lib.lsh_packed_gated.argtypes = [params, weights, weights, i32, vp, matrix, i32, vp, sz, vp, matrix, vp]
+    lib.lsh_delta_workspace_bytes.argtypes = [ctypes.POINTER(DeltaParams)]
+    lib.lsh_delta_rule.argtypes = [ctypes.POINTER(DeltaParams), vp, rows, vp, rows, vp, rows, vp, vp, vp, vp, vp, vp, vp, sz, vp, rows, vp]
+    for f in (lib.lsh_packed_quantize, lib.lsh_packed_values, lib.lsh_packed_linear, lib.lsh_packed_gated, lib.lsh_delta_rule):
+        f.restype = i32
+    lib.lsh_packed_workspace_bytes.restype = lib.lsh_delta_workspace_bytes.restype = sz
     lib.lsh_status_string.argtypes = [ctypes.c_int]
     lib.lsh_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -697,3 +727,129 @@ def cache_attention(cp: CacheParams, ap: AttentionParams, pool: CachePool, q, ta
         None if n_new is None else _ptr(n_new, i32, R, "n_new", dev), None if shared is None else _ptr(shared, i32, cp.S, "shared", dev),
         ws, room, out.data_ptr(), ctypes.byref(orow), None if lse is None else _ptr(lse, t.f32, R * T * H, "lse", dev),
         _stream_ptr(stream)), "lsh_cache_attention")
+
+
+# ---- layers of a decoder: weights of 4 bits, a recurrent state with a gated delta rule ----------
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def packed_params(N: int, K: int, group: int = 128) -> PackedParams:
+    return PackedParams(N, K, group)
+
+
+class PackedWeights:
+    """Caller-owned device memory of a matrix of 4-bit weights (torch is only the allocator): codes as uint8 [tiles, parts, 4, 16, 16],
+    scales as float16 or bfloat16 [tiles, parts, 16, 128 / group], zeros as uint8 of that shape, or None.  Tensors that are handed in are
+    kept and used as they are; else codes and scales are made, and zeros where `zeros` is True."""
+
+    def __init__(self, pp: PackedParams, codes=None, scales=None, zeros=None, scale_dtype=None):
+        import torch
+        tiles, parts = -(-pp.N // 16), -(-pp.K // 128)
+        shape, of_groups = (tiles, parts, 4, 16, 16), (tiles, parts, 16, 128 // pp.group)
+        if codes is None:
+            codes = torch.zeros(shape, dtype=torch.uint8, device="cuda")
+        if scales is None:
+            scales = torch.zeros(of_groups, dtype=torch.float16 if scale_dtype is None else scale_dtype, device="cuda")
+        if zeros is True:
+            zeros = torch.zeros(of_groups, dtype=torch.uint8, device="cuda")
+        _require_cuda(codes, "codes", (torch.uint8,))
+        _require_cuda(scales, "scales", (torch.float16, torch.bfloat16))
+        if zeros is not None:
+            _require_cuda(zeros, "zeros", (torch.uint8,))
+        for x, name, want in ((codes, "codes", shape), (scales, "scales", of_groups), (zeros, "zeros", of_groups)):
+            if x is not None and tuple(x.shape) != want:
+                raise ValueError(f"{name} must be {want}, is {tuple(x.shape)}")
+        given = [x for x in (codes, scales, zeros) if x is not None]
+        if len({x.get_device() for x in given}) != 1:
+            raise ValueError("a matrix's tensors must be on one device")
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self._shape = (pp.N, pp.K, pp.group)
+        self._device = codes.get_device()
+        self._pointers = _WeightPointers(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), _t().types[scales.dtype])
+
+    def _of(self, pp: PackedParams, device: int):
+        if (pp.N, pp.K, pp.group) != self._shape or device != self._device:
+            raise ValueError("the weights were made for other parameters, or on another device than the current one")
+        return ctypes.byref(self._pointers)
+
+
+def _matrix(x, name, shape, dev):
+    """lsh_matrix of a tensor with contiguous rows."""
+    t = _t().types.get(x.dtype)
+    if t is None or x.get_device() != dev or tuple(x.shape) != shape or (shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name} must be {shape} with contiguous rows on the current device, of {tuple(_t().types)}")
+    return _Matrix(t, x.stride(0) if shape[0] > 1 else shape[1])
+
+
+def packed_quantize(pp: PackedParams, w, to: PackedWeights, stream=None):
+    """lsh_packed_quantize: w [N, K]; with zeros if `to` has them."""
+    dev = _t().device()
+    m = _matrix(w, "w", (pp.N, pp.K), dev)
+    _check(load_library().lsh_packed_quantize(ctypes.byref(pp), w.data_ptr(), ctypes.byref(m), to._of(pp, dev), _stream_ptr(stream)),
+           "lsh_packed_quantize")
+
+
+def packed_values(pp: PackedParams, weights: PackedWeights, out, stream=None):
+    """lsh_packed_values: out [N, K]."""
+    dev = _t().device()
+    m = _matrix(out, "out", (pp.N, pp.K), dev)
+    _check(load_library().lsh_packed_values(ctypes.byref(pp), weights._of(pp, dev), out.data_ptr(), ctypes.byref(m), _stream_ptr(stream)),
+           "lsh_packed_values")
+
+
+def packed_workspace_bytes(pp: PackedParams, M: int) -> int:
+    return int(load_library().lsh_packed_workspace_bytes(ctypes.byref(pp), M))
+
+
+def packed_linear(pp: PackedParams, weights: PackedWeights, x, workspace, out, bias=None, add=None, stream=None):
+    """lsh_packed_linear: x [M, K], out [M, N], bias float32 [N] or None, add [M, N] of out's type or None (out itself, say)."""
+    t = _t()
+    dev, M = t.device(), x.shape[0]
+    xm, om = _matrix(x, "x", (M, pp.K), dev), _matrix(out, "out", (M, pp.N), dev)
+    add_ld = 0
+    if add is not None:
+        am = _matrix(add, "add", (M, pp.N), dev)
+        if am.dtype != om.dtype:
+            raise ValueError("add must be of out's type")
+        add_ld = am.ld
+    ws, room = _room(workspace, dev)
+    _check(load_library().lsh_packed_linear(
+        ctypes.byref(pp), weights._of(pp, dev), M, x.data_ptr(), ctypes.byref(xm), None if bias is None else _ptr(bias, t.f32, pp.N, "bias", dev),
+        None if add is None else add.data_ptr(), add_ld, ws, room, out.data_ptr(), ctypes.byref(om), _stream_ptr(stream)), "lsh_packed_linear")
+
+
+def packed_gated(pp: PackedParams, gate: PackedWeights, up: PackedWeights, x, workspace, out, act: str = "silu", stream=None):
+    """lsh_packed_gated: x [M, K], out [M, N]; act one of ACTIVATIONS."""
+    dev, M = _t().device(), x.shape[0]
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {tuple(ACTIVATIONS)}")
+    xm, om = _matrix(x, "x", (M, pp.K), dev), _matrix(out, "out", (M, pp.N), dev)
+    ws, room = _room(workspace, dev)
+    _check(load_library().lsh_packed_gated(
+        ctypes.byref(pp), gate._of(pp, dev), up._of(pp, dev), M, x.data_ptr(), ctypes.byref(xm), ACTIVATIONS[act], ws, room, out.data_ptr(),
+        ctypes.byref(om), _stream_ptr(stream)), "lsh_packed_gated")
+
+
+def delta_params(S: int, B: int, T: int, n_heads: int, n_k_heads: int, k_dim: int, v_dim: int, scale: float) -> DeltaParams:
+    return DeltaParams(S, B, T, n_heads, n_k_heads, k_dim, v_dim, scale)
+
+
+def delta_workspace_bytes(dp: DeltaParams) -> int:
+    return int(load_library().lsh_delta_workspace_bytes(ctypes.byref(dp)))
+
+
+def delta_rule(dp: DeltaParams, q, k, v, decay, beta, state_in, state_out, workspace, out, parents=None, n_new=None, stream=None):
+    """lsh_delta_rule: q, k [S*B, T, n_k_heads, k_dim], v, out [S*B, T, n_heads, v_dim] of one type (views into a fused projection, say), decay, beta
+    float32 [S*B, T, n_heads], states float32 [S*B, n_heads, k_dim, v_dim], state_in None: zeros."""
+    t = _t()
+    dev, f32, R, T, H = t.device(), t.f32, dp.S * dp.B, dp.T, dp.n_heads
+    kr, qr = _rows(k, "k", R, T, dp.n_k_heads, dp.k_dim, dev), _rows(q, "q", R, T, dp.n_k_heads, dp.k_dim, dev)
+    vr, orow = _rows(v, "v", R, T, H, dp.v_dim, dev), _rows(out, "out", R, T, H, dp.v_dim, dev)
+    n, size = R * T * H, R * H * dp.k_dim * dp.v_dim
+    ws, room = _room(workspace, dev)
+    _check(load_library().lsh_delta_rule(
+        ctypes.byref(dp), q.data_ptr(), ctypes.byref(qr), k.data_ptr(), ctypes.byref(kr), v.data_ptr(), ctypes.byref(vr),
+        _ptr(decay, f32, n, "decay", dev), _ptr(beta, f32, n, "beta", dev), None if state_in is None else _ptr(state_in, f32, size, "state_in", dev),
+        None if parents is None else _ptr(parents, t.i32, R, "parents", dev), None if n_new is None else _ptr(n_new, t.i32, R, "n_new", dev),
+        _ptr(state_out, f32, size, "state_out", dev), ws, room, out.data_ptr(), ctypes.byref(orow), _stream_ptr(stream)), "lsh_delta_rule")

@@ -69,20 +69,6 @@ __device__ __forceinline__ void seen(const AttnArgs& a, int len, int n, int t, i
 __device__ __forceinline__ int row_length(const AttnArgs& a, int r) { return (int)min((int64_t)max(a.lengths[r], 0), (int64_t)a.width * a.block); }
 __device__ __forceinline__ int row_new(const AttnArgs& a, int r) { return a.n_new ? min(max(a.n_new[r], 0), a.T) : a.T; }
 
-template <int TYPE> __device__ __forceinline__ void put_value(void* p, int64_t i, float v) {
-    if constexpr (TYPE == kTypeF32) static_cast<float*>(p)[i] = v;
-    else if constexpr (TYPE == kTypeF16) static_cast<uint16_t*>(p)[i] = __half_as_ushort(__float2half_rn(v));
-    else {
-        const uint32_t u = __float_as_uint(v);   // nearest even; a NaN stays one
-        static_cast<uint16_t*>(p)[i] = v != v ? (uint16_t)0x7fc0 : (uint16_t)((u + 0x7fffu + (u >> 16 & 1u)) >> 16);
-    }
-}
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-template <int TYPE> constexpr int kPlanes = TYPE == kTypeBf16 ? 1 : TYPE == kTypeF16 ? 2 : 3;
 constexpr int kAttnTile = 64;    // tokens of a wave at a time
 
 // Eight codes as an operand.
@@ -90,33 +76,6 @@ __device__ __forceinline__ bf16x8 codes_to_operand(uint32_t a, uint32_t b) {
     const bf16x2 r0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), r1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
     const bf16x2 r2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), r3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
     return bf16x8{r0.x, r0.y, r1.x, r1.y, r2.x, r2.y, r3.x, r3.y};
-}
-
-// Eight values as NP operands that add up to them: each but a rounded single one holds the upper 16 bits of what is left.
-template <int NP> __device__ __forceinline__ void planes_of(const float (&x)[8], uint4 (&out)[NP]) {
-    if constexpr (NP == 1) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2 v = {x[2 * i], x[2 * i + 1]};
-            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-        }
-        out[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        float rest[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rest[i] = x[i];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * i + 1]), __float_as_uint(rest[2 * i]), 0x07060302u);
-            out[p] = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
-        }
-    }
 }
 
 // Bytes of a word whose low seven bits are all ones (the code NaN), each as 0xff.

@@ -11,11 +11,9 @@
 //
 // A workgroup per row, head and block of tokens: it alone writes that head of that block.
 #pragma once
-#include "beam_select.h"
+#include "operands.h"
 
 namespace lshbeam {
-
-struct RowsPitch { int64_t row, token, head; };   // elements; the values of a head lie side by side
 
 struct WriteArgs {
     int T, n_blocks, block, heads, D;
@@ -45,30 +43,11 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t scaled_codes(uint32_t w, float ratio) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     return to_codes(lo.x * ratio, lo.y * ratio, hi.x * ratio, hi.y * ratio);
 }
 
-template <int TYPE> __device__ __forceinline__ float value_at(const void* p, int64_t i) {
-    return word_f32<TYPE>(static_cast<const typename WordOf<TYPE>::type*>(p)[i]);
-}
-
-// Eight values from any element on.
-template <int TYPE> __device__ __forceinline__ void load_values(const void* p, int64_t i, float (&x)[8]) {
-    using T = typename WordOf<TYPE>::type;
-    const T* from = static_cast<const T*>(p) + i;
-#pragma unroll
-    for (int h = 0; h < (TYPE == kTypeF32 ? 2 : 1); ++h) {
-        const Chunk16U<T> v = *reinterpret_cast<const Chunk16U<T>*>(from + 4 * h);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (TYPE == kTypeF32) x[4 * h + q] = __uint_as_float(v.w[q]);
-            else { x[2 * q] = word_f32<TYPE>((T)(v.w[q] & 0xffffu)); x[2 * q + 1] = word_f32<TYPE>((T)(v.w[q] >> 16)); }
-        }
-    }
-}
 __device__ __forceinline__ float finite_size(float m, float x) {   // the larger of m and |x|, if x is finite
     x = fabsf(x);
     return x < INFINITY ? fmaxf(m, x) : m;

@@ -1,0 +1,227 @@
+// C ABI of a decoder's layers (see include/lshbeam.h): weights of 4 bits and rows times them, the gated delta rule.  Host side: argument
+// validation, the choice of kernels, launches.  A translation unit, and so a code object, of its own, like the others.
+#ifdef LSHBEAM_TRACE   // (the phase timestamps belong to the decode step's kernels)
+#undef LSHBEAM_TRACE
+#endif
+#include "delta_rule.h"
+#include "launch.h"
+#include "packed_rows.h"
+
+using namespace lshbeam;
+
+namespace {
+
+// ---- weights of 4 bits --------------------------------------------------------------------------
+
+constexpr int kMaxOutputs = 1 << 24, kMaxInputs = 1 << 20;
+
+bool packed_ok(const lsh_packed_params* p) {
+    return p && p->N >= 1 && p->N <= kMaxOutputs && p->K >= 1 && p->K <= kMaxInputs && (p->group == 32 || p->group == 64 || p->group == 128);
+}
+bool weights_ok(const lsh_packed_weights* w) {
+    return w && w->codes && w->scales && aligned(w->codes, 16) && aligned(w->scales, 16) && aligned(w->zeros, 16) &&
+           (w->scale_dtype == LSH_BF16 || w->scale_dtype == LSH_F16);
+}
+bool matrix_ok(const void* at, const lsh_matrix* m, int32_t columns) {
+    return at && m && type_ok(m->dtype) && m->ld >= columns && aligned(at, type_bytes(m->dtype));
+}
+int log2_of(int32_t group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
+int64_t tiles_of(const lsh_packed_params* p) { return ceil_div(p->N, kPackOutputs); }
+int64_t parts_of(const lsh_packed_params* p) { return ceil_div(p->K, kPackInputs); }
+PackedRef ref(const lsh_packed_weights* w) { return PackedRef{w->codes, static_cast<uint16_t*>(w->scales), w->zeros}; }
+
+bool quantize_args(const lsh_packed_params* p, const lsh_packed_weights* w, const void* x, int64_t ld, QuantArgs* a) {
+    a->N = p->N; a->K = p->K; a->parts = (int)parts_of(p); a->shift = log2_of(p->group);
+    a->units = tiles_of(p) * parts_of(p);
+    a->w = x; a->ld = ld; a->to = ref(w);
+    return ceil_div(a->units, 4) <= kMaxGrid;
+}
+
+// How a product is divided among workgroups of eight waves.  More than 64 rows go in groups.
+struct RowsPlan {
+    int groups, rows, row_tiles;   // of rows
+    int streams;                   // tiles of a wave (gated: of both matrices)
+    int across, chunk;
+    int64_t sets;
+    unsigned grid;                 // workgroups of a group of rows
+    size_t lds;
+    int join_at;
+};
+RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
+    RowsPlan w{};
+    w.groups = (int)ceil_div(M, 64);
+    w.rows = (int)ceil_div(M, w.groups);
+    w.row_tiles = (int)ceil_div(w.rows, 16);
+    const int64_t tiles = tiles_of(p), parts = parts_of(p);
+    const int each = tiles * w.groups >= 1024 && !gated && w.row_tiles <= 2 ? 4 : tiles * w.groups >= 512 ? 2 : 1;
+    w.streams = gated ? 2 * each : each;
+    w.across = 1;
+    while (w.across < kPackedWaves && kPackedWaves / w.across > parts) w.across *= 2;
+    w.sets = ceil_div(tiles, (int64_t)w.across * each);
+    w.grid = (unsigned)std::min<int64_t>(w.sets, std::max(1, 256 / w.groups));
+    const int deep = kPackedWaves / w.across;
+    const size_t row_c = 256 * w.row_tiles + 32, of_part = (dtype == LSH_F32 ? 3 : 1) * 16 * row_c + 256 * w.row_tiles;
+    const size_t join = deep > 1 ? (size_t)kPackedWaves * w.row_tiles * w.streams * 1024 : 0;
+    // all rows in LDS, and beside them what is added up, or parts of them and that over them
+    bool all = parts * of_part + join <= kMaxDynLds;
+    int64_t chunk = all ? parts : std::max<int64_t>(1, kMaxDynLds / of_part);
+    const int64_t chunks = ceil_div(parts, chunk);
+    chunk = ceil_div(parts, chunks);
+    if (!all && chunk > deep) chunk = chunk / deep * deep;
+    w.chunk = (int)chunk;
+    if (w.sets <= w.grid) all = false;
+    w.join_at = all ? (int)(parts * of_part) : 0;
+    if (!all) w.grid = (unsigned)w.sets;
+    w.lds = all ? parts * of_part + join : std::max(chunk * of_part, join);
+    return w;
+}
+
+template <int TYPE, int MT, int NS, bool GATED> bool rows_launch(const PackedArgs& a, const RowsPlan& w, hipStream_t st) {
+    return launch_room<k_packed_rows<TYPE, MT, NS, GATED>>(dim3(w.grid, (unsigned)w.groups), 64 * kPackedWaves, w.lds, st, a);
+}
+template <int TYPE, int MT> bool rows_launch(const PackedArgs& a, const RowsPlan& w, bool gated, hipStream_t st) {
+    if (gated) return w.streams == 2 ? rows_launch<TYPE, MT, 2, true>(a, w, st) : rows_launch<TYPE, MT, 4, true>(a, w, st);
+    if (w.streams == 1) return rows_launch<TYPE, MT, 1, false>(a, w, st);
+    if constexpr (MT <= 2) {
+        if (w.streams == 4) return rows_launch<TYPE, MT, 4, false>(a, w, st);
+    }
+    return rows_launch<TYPE, MT, 2, false>(a, w, st);
+}
+
+lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* const (&weights)[2], int32_t M, const void* x_dev, const lsh_matrix* x,
+                          const float* bias_dev, const void* add_dev, int64_t add_ld, int32_t activation, void* workspace_dev, size_t workspace_bytes,
+                          void* out_dev, const lsh_matrix* out, void* hip_stream) {
+    const bool gated = weights[1] != nullptr;
+    if (!packed_ok(p) || !weights_ok(weights[0]) || M < 1 || M > kMaxRows || !matrix_ok(x_dev, x, p->K) || !matrix_ok(out_dev, out, p->N) ||
+        !aligned(bias_dev, 4) || (add_dev && (add_ld < p->N || !aligned(add_dev, type_bytes(out->dtype)))) || !workspace_dev || !aligned(workspace_dev, 256))
+        return LSH_ERR_INVALID_ARG;
+    if (workspace_bytes < lsh_packed_workspace_bytes(p, M)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    const RowsPlan w = rows_plan(p, M, x->dtype, gated);
+    if (w.grid > kMaxGrid / 2 || w.groups > 65535) return LSH_ERR_UNSUPPORTED;
+    PackedArgs a{};
+    a.M = M; a.N = p->N; a.K = p->K; a.tiles = (int)tiles_of(p); a.parts = (int)parts_of(p);
+    a.shift = log2_of(p->group);
+    a.scale_f16 = weights[0]->scale_dtype == LSH_F16;
+    a.x = x_dev; a.ldx = x->ld;
+    a.w[0] = ref(weights[0]);
+    if (gated) a.w[1] = ref(weights[1]);
+    a.bias = bias_dev; a.add = add_dev; a.ld_add = add_ld;
+    a.out = out_dev; a.ld_out = out->ld; a.out_type = out->dtype == LSH_F32 ? kTypeF32 : out->dtype == LSH_BF16 ? kTypeBf16 : kTypeF16;
+    a.activation = activation;
+    a.rows = w.rows; a.across = w.across; a.chunk = w.chunk; a.sets = (int)w.sets; a.join_at = w.join_at;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    bool ok = true;
+    for_type(x->dtype, [&](auto type) {
+        constexpr int kType = decltype(type)::value;
+        ok = w.row_tiles == 1   ? rows_launch<kType, 1>(a, w, gated, st)
+             : w.row_tiles == 2 ? rows_launch<kType, 2>(a, w, gated, st)
+             : w.row_tiles == 3 ? rows_launch<kType, 3>(a, w, gated, st)
+                                : rows_launch<kType, 4>(a, w, gated, st);
+    });
+    if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
+    return ok ? launched() : LSH_ERR_HIP;
+}
+
+// ---- gated delta rule ---------------------------------------------------------------------------
+
+bool delta_ok(const lsh_delta_params* p) {
+    return p && p->S >= 1 && p->B >= 1 && p->B <= 256 && (int64_t)p->S * p->B <= kMaxRows && p->T >= 1 && p->T <= kMaxRows && p->n_k_heads >= 1 &&
+           p->n_heads >= 1 && p->n_heads <= 65535 && p->n_heads % p->n_k_heads == 0 && p->k_dim >= 16 && p->k_dim <= 256 && p->k_dim % 16 == 0 &&
+           p->v_dim >= 16 && p->v_dim <= 256 && p->v_dim % 16 == 0;
+}
+int64_t delta_slices(const lsh_delta_params* p) { return ceil_div(p->v_dim, kDeltaColumns); }
+bool delta_fits(const lsh_delta_params* p) {
+    const int64_t heads = (int64_t)p->S * p->B * p->n_heads;
+    return heads <= kMaxGrid && heads * p->T <= (int64_t)1 << 26 && heads * delta_slices(p) <= kMaxGrid;
+}
+bool rows_aligned(const void* at, const lsh_rows* x, int32_t dim) { return at && pitch_ok(x, dim) && aligned(at, type_bytes(x->dtype)); }
+
+}  // namespace
+
+extern "C" {
+
+lsh_status lsh_packed_quantize(const lsh_packed_params* p, const void* w_dev, const lsh_matrix* w, const lsh_packed_weights* to, void* hip_stream) {
+    if (!packed_ok(p) || !weights_ok(to) || !matrix_ok(w_dev, w, p->K)) return LSH_ERR_INVALID_ARG;
+    QuantArgs a{};
+    if (!quantize_args(p, to, w_dev, w->ld, &a)) return LSH_ERR_UNSUPPORTED;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    for_type(w->dtype, [&](auto type) {
+        constexpr int kType = decltype(type)::value;
+        const bool f16 = to->scale_dtype == LSH_F16;
+        auto kernel = f16 ? (to->zeros ? k_packed_quantize<kType, true, true> : k_packed_quantize<kType, true, false>)
+                          : (to->zeros ? k_packed_quantize<kType, false, true> : k_packed_quantize<kType, false, false>);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(a.units, 4)), dim3(256), 0, st, a);
+    });
+    return launched();
+}
+
+lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weights* from, void* out_dev, const lsh_matrix* out, void* hip_stream) {
+    if (!packed_ok(p) || !weights_ok(from) || !matrix_ok(out_dev, out, p->K)) return LSH_ERR_INVALID_ARG;
+    QuantArgs a{};
+    if (!quantize_args(p, from, out_dev, out->ld, &a)) return LSH_ERR_UNSUPPORTED;
+    for_type(out->dtype, [&](auto type) {
+        constexpr int kType = decltype(type)::value;
+        auto kernel = from->scale_dtype == LSH_F16 ? k_packed_values<kType, true> : k_packed_values<kType, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(a.units, 4)), dim3(256), 0, (hipStream_t)hip_stream, a);
+    });
+    return launched();
+}
+
+size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) { return packed_ok(p) && M >= 1 && M <= kMaxRows ? 256 : 0; }
+
+lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
+                             const float* bias_dev, const void* add_dev, int64_t add_ld, void* workspace_dev, size_t workspace_bytes,
+                             void* out_dev, const lsh_matrix* out, void* hip_stream) {
+    return packed_product(p, {w, nullptr}, M, x_dev, x, bias_dev, add_dev, add_ld, 0, workspace_dev, workspace_bytes, out_dev, out, hip_stream);
+}
+
+lsh_status lsh_packed_gated(const lsh_packed_params* p, const lsh_packed_weights* gate, const lsh_packed_weights* up, int32_t M,
+                            const void* x_dev, const lsh_matrix* x, int32_t activation, void* workspace_dev, size_t workspace_bytes,
+                            void* out_dev, const lsh_matrix* out, void* hip_stream) {
+    if (!weights_ok(gate) || !weights_ok(up) || gate->scale_dtype != up->scale_dtype || activation < LSH_SILU || activation > LSH_GELU_TANH)
+        return LSH_ERR_INVALID_ARG;
+    return packed_product(p, {gate, up}, M, x_dev, x, nullptr, nullptr, 0, activation, workspace_dev, workspace_bytes, out_dev, out, hip_stream);
+}
+
+size_t lsh_delta_workspace_bytes(const lsh_delta_params* p) { return delta_ok(p) && delta_fits(p) ? 256 : 0; }
+
+lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,
+                          const void* v_dev, const lsh_rows* v_rows, const float* decay_dev, const float* beta_dev,
+                          const float* state_in_dev, const int32_t* parents_dev, const int32_t* n_new_dev, float* state_out_dev,
+                          void* workspace_dev, size_t workspace_bytes, void* out_dev, const lsh_rows* out_rows, void* hip_stream) {
+    if (!delta_ok(p) || !(p->scale > -INFINITY && p->scale < INFINITY) || !rows_aligned(q_dev, q_rows, p->k_dim) || !rows_aligned(k_dev, k_rows, p->k_dim) ||
+        !rows_aligned(v_dev, v_rows, p->v_dim) || !rows_aligned(out_dev, out_rows, p->v_dim) || q_rows->dtype != k_rows->dtype ||
+        q_rows->dtype != v_rows->dtype || q_rows->dtype != out_rows->dtype || !decay_dev || !beta_dev || !aligned(decay_dev, 4) || !aligned(beta_dev, 4) ||
+        !state_out_dev || !aligned(state_out_dev, 16) || !aligned(state_in_dev, 16) || !aligned(parents_dev, 4) || !aligned(n_new_dev, 4) ||
+        !workspace_dev || !aligned(workspace_dev, 256))
+        return LSH_ERR_INVALID_ARG;
+    if (!delta_fits(p)) return LSH_ERR_UNSUPPORTED;
+    const int64_t R = (int64_t)p->S * p->B;
+    if (state_in_dev) {   // a state is read by workgroups of other rows, unless each row continues its own
+        const uintptr_t in = reinterpret_cast<uintptr_t>(state_in_dev), to = reinterpret_cast<uintptr_t>(state_out_dev);
+        const uintptr_t size = (uintptr_t)(R * p->n_heads) * p->k_dim * p->v_dim * sizeof(float);
+        if (in < to + size && to < in + size && (parents_dev || in != to)) return LSH_ERR_INVALID_ARG;
+    }
+    if (heads_overlap(out_rows, R, p->T, p->n_heads, p->v_dim)) return LSH_ERR_INVALID_ARG;
+    if (workspace_bytes < lsh_delta_workspace_bytes(p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    DeltaArgs a{};
+    a.S = p->S; a.B = p->B; a.T = p->T; a.heads = p->n_heads; a.k_heads = p->n_k_heads; a.Dk = p->k_dim; a.Dv = p->v_dim;
+    a.scale = p->scale;
+    a.q = q_dev; a.k = k_dev; a.v = v_dev;
+    a.qp = RowsPitch{q_rows->row, q_rows->token, q_rows->head};
+    a.kp = RowsPitch{k_rows->row, k_rows->token, k_rows->head};
+    a.vp = RowsPitch{v_rows->row, v_rows->token, v_rows->head};
+    a.decay = decay_dev; a.beta = beta_dev; a.state_in = state_in_dev; a.parents = parents_dev; a.n_new = n_new_dev;
+    a.state_out = state_out_dev;
+    a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
+    a.slices = (int)delta_slices(p);
+    const unsigned grid = (unsigned)(R * p->n_heads * a.slices);
+    for_type(q_rows->dtype, [&](auto type) {
+        constexpr int kType = decltype(type)::value;
+        auto kernel = p->k_dim <= 64 ? k_delta_tokens<kType, 4> : p->k_dim <= 128 ? k_delta_tokens<kType, 8> : k_delta_tokens<kType, 16>;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)hip_stream, a);
+    });
+    return launched();
+}
+
+}  // extern "C"
