@@ -3,7 +3,7 @@
 #ifdef LSHBEAM_TRACE   // (the phase timestamps belong to the decode step's kernels)
 #undef LSHBEAM_TRACE
 #endif
-#include "delta_rule.h"
+#include "delta_chunks.h"
 #include "launch.h"
 #include "packed_rows.h"
 
@@ -130,9 +130,56 @@ bool delta_ok(const lsh_delta_params* p) {
            p->v_dim >= 16 && p->v_dim <= 256 && p->v_dim % 16 == 0;
 }
 int64_t delta_slices(const lsh_delta_params* p) { return ceil_div(p->v_dim, kDeltaColumns); }
+int64_t delta_pairs(const lsh_delta_params* p) { return (int64_t)p->S * p->B * p->n_heads; }
 bool delta_fits(const lsh_delta_params* p) {
-    const int64_t heads = (int64_t)p->S * p->B * p->n_heads;
-    return heads <= kMaxGrid && heads * p->T <= (int64_t)1 << 26 && heads * delta_slices(p) <= kMaxGrid;
+    return delta_pairs(p) <= kMaxGrid && delta_pairs(p) * p->T <= (int64_t)1 << 26 && delta_pairs(p) * delta_slices(p) <= kMaxGrid;
+}
+// Rows of more tokens than this go in chunks of 64.
+constexpr int kTokensMost = 32;
+
+// The chunks' operands take turns in the workspace: as many pairs of a row and a head and as many of their chunks at a time as have room.
+struct ChunksPlan {
+    size_t of_chunk, bytes;
+    int64_t pairs;             // of a launch
+    int chunks;                // of a segment
+};
+constexpr size_t kChunksRoom = (size_t)256 << 20;
+template <typename F> void for_dims(int32_t dim, F f) {   // f(std::integral_constant<int, ceil(k_dim / 32)>), some of them rounded up
+    const int nk = (dim + 31) / 32;
+    if (nk == 1) f(std::integral_constant<int, 1>());
+    else if (nk == 2) f(std::integral_constant<int, 2>());
+    else if (nk == 3) f(std::integral_constant<int, 3>());
+    else if (nk == 4) f(std::integral_constant<int, 4>());
+    else if (nk <= 6) f(std::integral_constant<int, 6>());
+    else f(std::integral_constant<int, 8>());
+}
+ChunksPlan chunks_plan(const lsh_delta_params* p, int32_t dtype) {
+    ChunksPlan w{};
+    for_type(dtype, [&](auto type) {
+        for_dims(p->k_dim, [&](auto nk) { w.of_chunk = ChunkPlan<decltype(type)::value, decltype(nk)::value>::bytes(p->v_dim); });
+    });
+    const int64_t most = std::max<int64_t>(1, kChunksRoom / w.of_chunk), all = ceil_div(p->T, kChunk);
+    w.pairs = std::min(most, delta_pairs(p));
+    w.chunks = (int)std::min(std::max<int64_t>(1, most / w.pairs), all);
+    w.bytes = w.of_chunk * (size_t)w.pairs * w.chunks;
+    return w;
+}
+template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const DeltaArgs& d, const ChunksPlan& w, char* room, hipStream_t st) {
+    ChunkArgs a{};
+    a.d = d; a.room = room; a.bytes = w.of_chunk;
+    const int all = (int)ceil_div(p->T, kChunk);
+    for (int64_t pair = 0; pair < delta_pairs(p); pair += w.pairs) {
+        const int64_t pairs = std::min(w.pairs, delta_pairs(p) - pair);
+        a.pair0 = pair;
+        for (int chunk = 0; chunk < all; chunk += w.chunks) {
+            a.chunk0 = chunk;
+            a.chunks = std::min(w.chunks, all - chunk);
+            a.first = chunk == 0;
+            if (!launch_room<k_delta_prepare<TYPE, NK>>(dim3((unsigned)(pairs * a.chunks)), 256, kPrepareLds<TYPE, NK>, st, a)) return false;
+            if (!launch_room<k_delta_chain<TYPE, NK>>(dim3((unsigned)(pairs * d.slices)), 256, kChainLds, st, a)) return false;
+        }
+    }
+    return true;
 }
 bool rows_aligned(const void* at, const lsh_rows* x, int32_t dim) { return at && pitch_ok(x, dim) && aligned(at, type_bytes(x->dtype)); }
 
@@ -183,7 +230,13 @@ lsh_status lsh_packed_gated(const lsh_packed_params* p, const lsh_packed_weights
     return packed_product(p, {gate, up}, M, x_dev, x, nullptr, nullptr, 0, activation, workspace_dev, workspace_bytes, out_dev, out, hip_stream);
 }
 
-size_t lsh_delta_workspace_bytes(const lsh_delta_params* p) { return delta_ok(p) && delta_fits(p) ? 256 : 0; }
+size_t lsh_delta_workspace_bytes(const lsh_delta_params* p) {
+    if (!delta_ok(p) || !delta_fits(p)) return 0;
+    size_t bytes = 256;
+    if (p->T > kTokensMost)
+        for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16}) bytes = std::max(bytes, chunks_plan(p, dtype).bytes);
+    return bytes;
+}
 
 lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,
                           const void* v_dev, const lsh_rows* v_rows, const float* decay_dev, const float* beta_dev,
@@ -215,13 +268,20 @@ lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const ls
     a.state_out = state_out_dev;
     a.out = out_dev; a.op = RowsPitch{out_rows->row, out_rows->token, out_rows->head};
     a.slices = (int)delta_slices(p);
-    const unsigned grid = (unsigned)(R * p->n_heads * a.slices);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
+        if (p->T > kTokensMost) {
+            const ChunksPlan w = chunks_plan(p, q_rows->dtype);
+            for_dims(p->k_dim, [&](auto nk) { ok = chunks_launch<kType, decltype(nk)::value>(p, a, w, static_cast<char*>(workspace_dev), st); });
+            return;
+        }
         auto kernel = p->k_dim <= 64 ? k_delta_tokens<kType, 4> : p->k_dim <= 128 ? k_delta_tokens<kType, 8> : k_delta_tokens<kType, 16>;
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)hip_stream, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(delta_pairs(p) * a.slices)), dim3(256), 0, st, a);
     });
-    return launched();
+    if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
+    return ok ? launched() : LSH_ERR_HIP;
 }
 
 }  // extern "C"
