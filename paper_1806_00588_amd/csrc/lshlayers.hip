@@ -5,7 +5,7 @@
 #endif
 #include "delta_chunks.h"
 #include "launch.h"
-#include "packed_rows.h"
+#include "packed_tiles.h"
 
 using namespace lshbeam;
 
@@ -88,6 +88,37 @@ template <int TYPE, int MT> bool rows_launch(const PackedArgs& a, const RowsPlan
     return rows_launch<TYPE, MT, 2, false>(a, w, st);
 }
 
+// More rows: 128 of them and 64, 128 or 256 outputs a workgroup.
+struct TilesLaunch {
+    int streams, row_tiles, row_groups;
+    int64_t sets;
+    size_t room;               // the rows as operands
+};
+constexpr int kFewRows = 128;
+bool takes_tiles(int32_t M) { return M > kFewRows; }
+TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
+    TilesLaunch w{};
+    w.row_tiles = (int)ceil_div(M, 16);
+    w.row_groups = (int)ceil_div(w.row_tiles, kTileRows);
+    const int least = gated ? 2 : 1;
+    for (w.streams = 4;; w.streams /= 2) {
+        w.sets = ceil_div(tiles_of(p), kTileWaves * (gated ? w.streams / 2 : w.streams));
+        if (w.streams == least || w.sets * w.row_groups >= 256) break;
+    }
+    w.room = (size_t)w.row_tiles * parts_of(p) * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
+    return w;
+}
+template <int TYPE, int NS, bool GATED> bool tiles_launch(const TilesArgs& a, hipStream_t st) {
+    return launch_room<k_packed_tiles<TYPE, NS, GATED>>(dim3((unsigned)((a.row_groups * (int64_t)a.sets + 7) / 8 * 8)), 64 * kTileWaves, TilesPlan<TYPE, NS>::kLds, st, a);
+}
+template <int TYPE> bool tiles_launch(const PackedArgs& p, const TilesLaunch& w, bool gated, char* room, hipStream_t st) {
+    const int64_t units = (int64_t)w.row_tiles * p.parts;
+    hipLaunchKernelGGL(k_packed_lay<TYPE>, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, st, p, room, units);
+    const TilesArgs a{p, room, w.row_tiles, w.row_groups, (int)w.sets};
+    if (gated) return w.streams == 2 ? tiles_launch<TYPE, 2, true>(a, st) : tiles_launch<TYPE, 4, true>(a, st);
+    return w.streams == 1 ? tiles_launch<TYPE, 1, false>(a, st) : w.streams == 2 ? tiles_launch<TYPE, 2, false>(a, st) : tiles_launch<TYPE, 4, false>(a, st);
+}
+
 lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* const (&weights)[2], int32_t M, const void* x_dev, const lsh_matrix* x,
                           const float* bias_dev, const void* add_dev, int64_t add_ld, int32_t activation, void* workspace_dev, size_t workspace_bytes,
                           void* out_dev, const lsh_matrix* out, void* hip_stream) {
@@ -96,8 +127,11 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
         !aligned(bias_dev, 4) || (add_dev && (add_ld < p->N || !aligned(add_dev, type_bytes(out->dtype)))) || !workspace_dev || !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
     if (workspace_bytes < lsh_packed_workspace_bytes(p, M)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    const bool many = takes_tiles(M);
     const RowsPlan w = rows_plan(p, M, x->dtype, gated);
-    if (w.grid > kMaxGrid / 2 || w.groups > 65535) return LSH_ERR_UNSUPPORTED;
+    const TilesLaunch tiles = tiles_plan(p, M, x->dtype, gated);
+    if (many ? ceil_div((int64_t)tiles.row_tiles * parts_of(p), 4) > kMaxGrid || tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 2)
+        return LSH_ERR_UNSUPPORTED;
     PackedArgs a{};
     a.M = M; a.N = p->N; a.K = p->K; a.tiles = (int)tiles_of(p); a.parts = (int)parts_of(p);
     a.shift = log2_of(p->group);
@@ -113,6 +147,10 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     bool ok = true;
     for_type(x->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
+        if (many) {
+            ok = tiles_launch<kType>(a, tiles, gated, static_cast<char*>(workspace_dev), st);
+            return;
+        }
         ok = w.row_tiles == 1   ? rows_launch<kType, 1>(a, w, gated, st)
              : w.row_tiles == 2 ? rows_launch<kType, 2>(a, w, gated, st)
              : w.row_tiles == 3 ? rows_launch<kType, 3>(a, w, gated, st)
@@ -214,7 +252,10 @@ lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weight
     return launched();
 }
 
-size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) { return packed_ok(p) && M >= 1 && M <= kMaxRows ? 256 : 0; }
+size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) {
+    if (!packed_ok(p) || M < 1 || M > kMaxRows) return 0;
+    return takes_tiles(M) ? std::max<size_t>(256, tiles_plan(p, M, LSH_F32, false).room) : 256;
+}
 
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
                              const float* bias_dev, const void* add_dev, int64_t add_ld, void* workspace_dev, size_t workspace_bytes,

@@ -64,6 +64,16 @@ template <int TYPE> __device__ __forceinline__ f32x4 product(uint4 x, typename O
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), w, acc, 0, 0, 0);
 }
 
+// Eight inputs of a row as operands.
+template <int TYPE> __device__ __forceinline__ void row_operand(const float (&x)[8], uint4 (&op)[kRowPlanes<TYPE>]) {
+    if constexpr (TYPE == kTypeF16) {
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i])) | (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i + 1])) << 16;
+        op[0] = make_uint4(b[0], b[1], b[2], b[3]);
+    } else planes_of<kRowPlanes<TYPE>>(x, op);
+}
+
 __device__ __forceinline__ float activate(float z, int kind) {
     if (kind == 0) return z / (1.f + expf(-z));
     if (kind == 1) return z * (0.5f * erfcf(-0.70710678118654752f * z));
@@ -156,13 +166,7 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
                             for (int i = 0; i < 8; ++i) x[i] = k + i < a.K ? value_at<TYPE>(a.x, from + i) : 0.f;
                         }
                         uint4 op[NP];
-                        if constexpr (TYPE == kTypeF16) {
-                            uint32_t b[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                b[i] = (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i])) | (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i + 1])) << 16;
-                            op[0] = make_uint4(b[0], b[1], b[2], b[3]);
-                        } else planes_of<NP>(x, op);
+                        row_operand<TYPE>(x, op);
                         char* to = lds + ((p * 4 + w) * 4 + c) * CS + m * 16;
 #pragma unroll
                         for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(to + i * plane) = op[i];
