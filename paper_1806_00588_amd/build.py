@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "lshbeam.hip")              # the decode step and the tables it looks up
 DECODER_SRC = os.path.join(HERE, "csrc", "lshdecoder.hip")   # what stands around a decoder with a cache
-LAYERS_SRC = os.path.join(HERE, "csrc", "lshlayers.hip")     # a decoder's layers
+LAYERS_SRC = [os.path.join(HERE, "csrc", f) for f in ("lshlayers.hip", "packed_rows.hip", "packed_tiles.hip")]   # a decoder's layers
 LIB = os.path.join(HERE, "liblshbeam.so")
 
 HIPCC_FLAGS = [
@@ -29,7 +29,7 @@ def build(verbose: bool = True) -> str:
     """The translation units at the same time, then the library of all."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    units = (SRC, DECODER_SRC, LAYERS_SRC)
+    units = [SRC, DECODER_SRC] + LAYERS_SRC
     objects = [tmp + ".%d.o" % i for i in range(len(units))]
     compiles = [[hipcc] + HIPCC_FLAGS + ["-c", "-o", o, src] for o, src in zip(objects, units)]
     link = [hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp] + objects

@@ -5,6 +5,7 @@
 #endif
 #include "delta_chunks.h"
 #include "launch.h"
+#include "packed_launch.h"
 #include "packed_tiles.h"
 
 using namespace lshbeam;
@@ -37,86 +38,69 @@ bool quantize_args(const lsh_packed_params* p, const lsh_packed_weights* w, cons
     return ceil_div(a->units, 4) <= kMaxGrid;
 }
 
-// How a product is divided among workgroups of eight waves.  More than 64 rows go in groups.
+// How few rows' products are divided among workgroups of eight waves.
 struct RowsPlan {
     int groups, rows, row_tiles;   // of rows
     int streams;                   // tiles of a wave (gated: of both matrices)
-    int across, chunk;
+    int log_across, chunk, turns;
     int64_t sets;
     unsigned grid;                 // workgroups of a group of rows
     size_t lds;
     int join_at;
 };
+constexpr int kFewRows = 32;
 RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     RowsPlan w{};
-    w.groups = (int)ceil_div(M, 64);
+    w.groups = (int)ceil_div(M, kFewRows);
     w.rows = (int)ceil_div(M, w.groups);
     w.row_tiles = (int)ceil_div(w.rows, 16);
-    const int64_t tiles = tiles_of(p), parts = parts_of(p);
-    const int each = tiles * w.groups >= 1024 && !gated && w.row_tiles <= 2 ? 4 : tiles * w.groups >= 512 ? 2 : 1;
-    w.streams = gated ? 2 * each : each;
-    w.across = 1;
-    while (w.across < kPackedWaves && kPackedWaves / w.across > parts) w.across *= 2;
-    w.sets = ceil_div(tiles, (int64_t)w.across * each);
+    const int64_t tiles = tiles_of(p), parts = parts_of(p), planes = dtype == LSH_F32 ? 3 : 1;
+    // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in cycles -- a wave's tile some 300 a
+    // part, its rows' operands some 60 a part and plane, adding up and the results 1200 a round
+    int64_t best = INT64_MAX;
+    for (int each = 1; each <= (gated ? 2 : 4); each *= 2)
+        for (int lg = 0; (w.row_tiles * each << lg) <= kPackedWaves; ++lg) {
+            const int64_t sets = ceil_div(tiles, (int64_t)each << lg), rounds = ceil_div(sets * w.groups, 256), streams = gated ? 2 * each : each;
+            const int64_t cost = rounds * (ceil_div(parts, kPackedWaves >> lg) * w.row_tiles * (300 * streams + 60 * planes) + 1200);
+            if (cost < best) { best = cost; w.streams = (int)streams; w.log_across = lg; w.sets = sets; }
+        }
+    const int deep = kPackedWaves >> w.log_across;
     w.grid = (unsigned)std::min<int64_t>(w.sets, std::max(1, 256 / w.groups));
-    const int deep = kPackedWaves / w.across;
-    const size_t row_c = 256 * w.row_tiles + 32, of_part = (dtype == LSH_F32 ? 3 : 1) * 16 * row_c + 256 * w.row_tiles;
-    const size_t join = deep > 1 ? (size_t)kPackedWaves * w.row_tiles * w.streams * 1024 : 0;
-    // all rows in LDS, and beside them what is added up, or parts of them and that over them
-    bool all = parts * of_part + join <= kMaxDynLds;
-    int64_t chunk = all ? parts : std::max<int64_t>(1, kMaxDynLds / of_part);
-    const int64_t chunks = ceil_div(parts, chunk);
-    chunk = ceil_div(parts, chunks);
-    if (!all && chunk > deep) chunk = chunk / deep * deep;
+    // all rows in LDS, or as many of their parts as there is room for
+    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1), join = 2 * packed_join(w.row_tiles, w.streams);
+    const int64_t chunks = ceil_div(parts, (int64_t)((kMaxDynLds - join) / of_part));
+    int64_t chunk = ceil_div(parts, chunks);
+    if (chunks > 1 && chunk > deep) chunk = chunk / deep * deep;
     w.chunk = (int)chunk;
-    if (w.sets <= w.grid) all = false;
-    w.join_at = all ? (int)(parts * of_part) : 0;
-    if (!all) w.grid = (unsigned)w.sets;
-    w.lds = all ? parts * of_part + join : std::max(chunk * of_part, join);
+    w.turns = (int)ceil_div(ceil_div(chunk, deep), 2) * 2;
+    w.join_at = (int)(chunk * of_part);
+    w.lds = w.join_at + join;
     return w;
 }
 
-template <int TYPE, int MT, int NS, bool GATED> bool rows_launch(const PackedArgs& a, const RowsPlan& w, hipStream_t st) {
-    return launch_room<k_packed_rows<TYPE, MT, NS, GATED>>(dim3(w.grid, (unsigned)w.groups), 64 * kPackedWaves, w.lds, st, a);
-}
-template <int TYPE, int MT> bool rows_launch(const PackedArgs& a, const RowsPlan& w, bool gated, hipStream_t st) {
-    if (gated) return w.streams == 2 ? rows_launch<TYPE, MT, 2, true>(a, w, st) : rows_launch<TYPE, MT, 4, true>(a, w, st);
-    if (w.streams == 1) return rows_launch<TYPE, MT, 1, false>(a, w, st);
-    if constexpr (MT <= 2) {
-        if (w.streams == 4) return rows_launch<TYPE, MT, 4, false>(a, w, st);
-    }
-    return rows_launch<TYPE, MT, 2, false>(a, w, st);
-}
-
-// More rows: 128 of them and 64, 128 or 256 outputs a workgroup.
+// More rows: 64 or 128 of them and 64, 128 or 256 outputs a workgroup, whatever makes the least work of the rounds of 256 workgroups (a part of 64 x 256
+// results some 1000 cycles on the matrix cores, and some 500 for the rest of it).
 struct TilesLaunch {
-    int streams, row_tiles, row_groups;
+    int wave_rows, streams, row_tiles, row_groups;   // wave_rows: times 16
     int64_t sets;
-    size_t room;               // the rows as operands
+    size_t rows, room;         // the rows as operands; and their groups' sums
 };
-constexpr int kFewRows = 128;
 bool takes_tiles(int32_t M) { return M > kFewRows; }
 TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     TilesLaunch w{};
     w.row_tiles = (int)ceil_div(M, 16);
-    w.row_groups = (int)ceil_div(w.row_tiles, kTileRows);
-    const int least = gated ? 2 : 1;
-    for (w.streams = 4;; w.streams /= 2) {
-        w.sets = ceil_div(tiles_of(p), kTileWaves * (gated ? w.streams / 2 : w.streams));
-        if (w.streams == least || w.sets * w.row_groups >= 256) break;
-    }
-    w.room = (size_t)w.row_tiles * parts_of(p) * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
+    int64_t best = INT64_MAX;
+    for (int rows = 4; rows >= 2; rows -= 2)
+        for (int streams = 4; streams >= (gated || rows == 4 ? 2 : 1); streams /= 2) {
+            if (rows * streams == 16 && p->group == 32) continue;     // (four groups of a part: no registers for them)
+            const int64_t groups = ceil_div(w.row_tiles, 2 * rows), sets = ceil_div(tiles_of(p), kTileAcross * (gated ? streams / 2 : streams));
+            const int64_t cost = ceil_div(groups * sets, 256) * (rows * streams * (dtype == LSH_F32 ? 3 : 1) * 125 + 500);
+            if (cost < best) { best = cost; w.wave_rows = rows; w.streams = streams; w.row_groups = (int)groups; w.sets = sets; }
+        }
+    const size_t units = (size_t)w.row_tiles * parts_of(p);
+    w.rows = units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
+    w.room = w.rows + units * 64 * (kPackInputs / p->group);
     return w;
-}
-template <int TYPE, int NS, bool GATED> bool tiles_launch(const TilesArgs& a, hipStream_t st) {
-    return launch_room<k_packed_tiles<TYPE, NS, GATED>>(dim3((unsigned)((a.row_groups * (int64_t)a.sets + 7) / 8 * 8)), 64 * kTileWaves, TilesPlan<TYPE, NS>::kLds, st, a);
-}
-template <int TYPE> bool tiles_launch(const PackedArgs& p, const TilesLaunch& w, bool gated, char* room, hipStream_t st) {
-    const int64_t units = (int64_t)w.row_tiles * p.parts;
-    hipLaunchKernelGGL(k_packed_lay<TYPE>, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, st, p, room, units);
-    const TilesArgs a{p, room, w.row_tiles, w.row_groups, (int)w.sets};
-    if (gated) return w.streams == 2 ? tiles_launch<TYPE, 2, true>(a, st) : tiles_launch<TYPE, 4, true>(a, st);
-    return w.streams == 1 ? tiles_launch<TYPE, 1, false>(a, st) : w.streams == 2 ? tiles_launch<TYPE, 2, false>(a, st) : tiles_launch<TYPE, 4, false>(a, st);
 }
 
 lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* const (&weights)[2], int32_t M, const void* x_dev, const lsh_matrix* x,
@@ -142,20 +126,14 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     a.bias = bias_dev; a.add = add_dev; a.ld_add = add_ld;
     a.out = out_dev; a.ld_out = out->ld; a.out_type = out->dtype == LSH_F32 ? kTypeF32 : out->dtype == LSH_BF16 ? kTypeBf16 : kTypeF16;
     a.activation = activation;
-    a.rows = w.rows; a.across = w.across; a.chunk = w.chunk; a.sets = (int)w.sets; a.join_at = w.join_at;
+    a.rows = w.rows; a.log_across = w.log_across; a.chunk = w.chunk; a.turns = w.turns; a.sets = (int)w.sets; a.join_at = w.join_at;
     const hipStream_t st = (hipStream_t)hip_stream;
-    bool ok = true;
-    for_type(x->dtype, [&](auto type) {
-        constexpr int kType = decltype(type)::value;
-        if (many) {
-            ok = tiles_launch<kType>(a, tiles, gated, static_cast<char*>(workspace_dev), st);
-            return;
-        }
-        ok = w.row_tiles == 1   ? rows_launch<kType, 1>(a, w, gated, st)
-             : w.row_tiles == 2 ? rows_launch<kType, 2>(a, w, gated, st)
-             : w.row_tiles == 3 ? rows_launch<kType, 3>(a, w, gated, st)
-                                : rows_launch<kType, 4>(a, w, gated, st);
-    });
+    bool ok = false;
+    if (many) {
+        char* room = static_cast<char*>(workspace_dev);
+        const TilesArgs t{a, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
+        ok = launch_packed_tiles(x->dtype, tiles.wave_rows, tiles.streams, gated, t, st);
+    } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups), w.lds, st);
     if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
     return ok ? launched() : LSH_ERR_HIP;
 }

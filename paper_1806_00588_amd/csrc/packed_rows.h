@@ -3,7 +3,9 @@
 // with X[m, g] the sum of a row's inputs of group g.  Codes 0 .. 15 are exact in bf16 and fp16, rows of fp32 are taken apart into three planes of
 // bf16 that add up to them, so every product is exact and nothing but the fp32 sums rounds.
 //
-// Few rows: two operations a weight and row, so the weights' bytes bound it.
+// Few rows: two operations a weight and row, so the weights' bytes bound it.  The rows' operands are in LDS, made once where all of them fit; the weights come
+// straight to registers, two parts of a wave under way.  Eight waves of a workgroup are side by side along the outputs or share the inputs of the
+// same outputs among them, and workgroups go on to further outputs.
 #pragma once
 #include "packed.h"
 
@@ -26,22 +28,23 @@ struct PackedArgs {
     int64_t ld_out;
     int out_type;
     int activation;
-    // of the launch
+    // of k_packed_rows
     int rows;                  // of a workgroup
-    int across;                // waves side by side along the outputs; the others share their inputs
-    int chunk;                 // parts whose rows are in LDS at a time
+    int log_across;            // log2 of the waves side by side along the outputs; the others share their inputs
+    int chunk, turns;          // parts whose rows are in LDS at a time, the most that a wave has of them (even)
     int sets;                  // groups of tiles
-    int join_at;               // where in LDS waves that share inputs add up; 0: over the rows, which nothing asks for again
+    int join_at;               // where in LDS waves that share inputs add up
 };
 
 constexpr int kRowsPlanesF32 = 3;
 template <int TYPE> constexpr int kRowPlanes = TYPE == kTypeF32 ? kRowsPlanesF32 : 1;
-constexpr int kPackedWaves = 8;
+constexpr int kPackedWaves = 8, kLogWaves = 3;
 // LDS: operands of 32 inputs: [plane][of the chunk][c][row] 16 bytes, the c's 32 bytes apart so that four neighbouring lanes write to banks
-// of their own; sums of the rows' groups; what the waves that share inputs add up.
-template <int MT> constexpr int kRowsOfC = 16 * MT * 16 + 32;
-template <int MT> constexpr int packed_plane(int chunk) { return chunk * 4 * 4 * kRowsOfC<MT>; }
-template <int MT> constexpr int packed_sums(int chunk) { return chunk * 4 * 16 * MT * 4; }
+// of their own; sums of the rows' groups; twice (for one group of tiles and the next) what the waves that share inputs add up.
+constexpr int rows_of_c(int rows) { return rows * 16 + 32; }
+constexpr int packed_plane(int rows, int chunk) { return chunk * 4 * 4 * rows_of_c(rows); }
+constexpr int packed_sums(int row_tiles, int chunk) { return chunk * 4 * 16 * row_tiles * 4; }
+constexpr int packed_join(int row_tiles, int streams) { return kPackedWaves * row_tiles * streams * 1024; }
 
 template <int TYPE> struct OperandOf { using type = bf16x8; };
 template <> struct OperandOf<kTypeF16> { using type = f16x8; };
@@ -74,6 +77,13 @@ template <int TYPE> __device__ __forceinline__ void row_operand(const float (&x)
     } else planes_of<kRowPlanes<TYPE>>(x, op);
 }
 
+// The sum of the 32 values of four neighbouring lanes.
+__device__ __forceinline__ float quad_sum(const float (&x)[8]) {
+    float of = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    of += dpp_f32<0xB1>(of);
+    return of + dpp_f32<0x4E>(of);
+}
+
 __device__ __forceinline__ float activate(float z, int kind) {
     if (kind == 0) return z / (1.f + expf(-z));
     if (kind == 1) return z * (0.5f * erfcf(-0.70710678118654752f * z));
@@ -81,83 +91,136 @@ __device__ __forceinline__ float activate(float z, int kind) {
     return z / (1.f + expf(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
 }
 
-// A result to its place: bias, what is added, one rounding.
+// A result to its place, with what is added to it; one rounding.
+__device__ __forceinline__ float added(const PackedArgs& a, int64_t m, int64_t n) {
+    const int64_t at = m * a.ld_add + n;
+    return a.out_type == kTypeF32 ? value_at<kTypeF32>(a.add, at) : a.out_type == kTypeBf16 ? value_at<kTypeBf16>(a.add, at) : value_at<kTypeF16>(a.add, at);
+}
 __device__ __forceinline__ void put_result(const PackedArgs& a, int64_t m, int64_t n, float y) {
-    if (a.bias) y += a.bias[n];
-    const int64_t at = m * a.ld_out + n, add = m * a.ld_add + n;
-    if (a.out_type == kTypeF32) {
-        if (a.add) y += value_at<kTypeF32>(a.add, add);
-        put_value<kTypeF32>(a.out, at, y);
-    } else if (a.out_type == kTypeBf16) {
-        if (a.add) y += value_at<kTypeBf16>(a.add, add);
-        put_value<kTypeBf16>(a.out, at, y);
-    } else {
-        if (a.add) y += value_at<kTypeF16>(a.add, add);
-        put_value<kTypeF16>(a.out, at, y);
-    }
+    const int64_t at = m * a.ld_out + n;
+    if (a.out_type == kTypeF32) put_value<kTypeF32>(a.out, at, y);
+    else if (a.out_type == kTypeBf16) put_value<kTypeBf16>(a.out, at, y);
+    else put_value<kTypeF16>(a.out, at, y);
 }
 
-// What a wave asks of a tile's part.
-struct PackedPiece { uint4 codes; uint64_t scales; uint32_t zeros; };
-__device__ __forceinline__ PackedPiece load_piece(const PackedArgs& a, const PackedRef& w, int tile, int part) {
-    const int64_t unit = (int64_t)tile * a.parts + part;
-    const int ln = lane_id(), n = ln & 15, each = kPackInputs >> a.shift;
-    PackedPiece p;
-    p.codes = *reinterpret_cast<const uint4*>(w.codes + unit * kPackBytes + 16 * ln);
-    // 8 bytes of scales and 4 of zeros, of which the lane's may be the last ones: they stay inside the tile's part
-    const int at = min(n * each, 16 * each - 4);
-    const uint16_t* s = w.scales + unit * (16 * each) + at;
-    struct __attribute__((packed, aligned(2))) Eight { uint64_t v; };
-    p.scales = reinterpret_cast<const Eight*>(s)->v >> (16 * (n * each - at));
-    p.zeros = 0x08080808u;
-    if (w.zeros) {
-        struct __attribute__((packed, aligned(1))) Four { uint32_t v; };
-        p.zeros = reinterpret_cast<const Four*>(w.zeros + unit * (16 * each) + at)->v >> (8 * (n * each - at));
-    }
-    return p;
-}
+// What a wave asks of a tile's part: codes, its output's scales and zeros.
+template <int PER> struct PackedPiece {
+    uint4 codes;
+    uint32_t scales[PER == 1 ? 2 : 1], zeros;
+};
 
-// MT: 16 rows each; NS: tiles of a wave (gated: half of them of each matrix, gate and up in turn).
-template <int TYPE, int MT, int NS, bool GATED>
+// MT: 16 rows each; NS: tiles of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
+template <int TYPE, int MT, int NS, int PER, bool GATED>
 __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int NP = kRowPlanes<TYPE>, ROWS = 16 * MT, CS = kRowsOfC<MT>, NT = GATED ? NS / 2 : NS;
-    const int plane = packed_plane<MT>(a.chunk);
+    constexpr int NP = kRowPlanes<TYPE>, NT = GATED ? NS / 2 : NS, EACH = 4 / PER;
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), c = ln >> 4;
+    const int wn = wave & ((1 << a.log_across) - 1), wk = wave >> a.log_across;
+    const int log_deep = kLogWaves - a.log_across, deep = 1 << log_deep;
+    const int m0 = blockIdx.y * a.rows, rows = min(a.rows, a.M - m0), of_c = rows_of_c(a.rows), plane = packed_plane(a.rows, a.chunk);
     float* sums = reinterpret_cast<float*>(lds + NP * plane);
-    f32x4* join = reinterpret_cast<f32x4*>(lds + a.join_at);
-    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
-    const int across = a.across, deep = kPackedWaves / across, wn = wave % across, wk = wave / across;
-    const int m0 = blockIdx.y * a.rows, rows = min(a.rows, a.M - m0);
-    const int per = 1 << (a.shift - 5);                     // operands of a group
     const int chunks = (a.parts + a.chunk - 1) / a.chunk;
 
-    PackedPiece next[NS];
-    auto ask = [&](int set, int part) {
-        part = min(part, a.parts - 1);
+    // the next part of the wave: they are asked for in the order in which they are worked on, two ahead
+    int ask_set = blockIdx.x, ask_chunk = 0, ask_turn = 0;
+    auto ask = [&](PackedPiece<PER> (&to)[NS]) {
+        const int part = min(ask_chunk * a.chunk + min((ask_turn << log_deep) + wk, a.chunk - 1), a.parts - 1);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            const int tile = min((set * across + wn) * NT + (GATED ? s >> 1 : s), a.tiles - 1);
-            next[s] = load_piece(a, a.w[GATED ? s & 1 : 0], tile, part);
+            const int tile = min(((ask_set << a.log_across) + wn) * NT + (GATED ? s >> 1 : s), a.tiles - 1);
+            const PackedRef& w = a.w[GATED ? s & 1 : 0];
+            const int64_t unit = (int64_t)tile * a.parts + part, group = unit * (16 * EACH) + (ln & 15) * EACH;
+            to[s].codes = *reinterpret_cast<const uint4*>(w.codes + unit * kPackBytes + 16 * ln);
+            const uint16_t* scales = w.scales + group;
+            const uint8_t* zeros = w.zeros ? w.zeros + group : reinterpret_cast<const uint8_t*>(scales);
+            if constexpr (PER == 4) { to[s].scales[0] = *scales; to[s].zeros = *zeros; }
+            else if constexpr (PER == 2) { to[s].scales[0] = *reinterpret_cast<const uint32_t*>(scales); to[s].zeros = *reinterpret_cast<const uint16_t*>(zeros); }
+            else {
+                const uint2 two = *reinterpret_cast<const uint2*>(scales);
+                to[s].scales[0] = two.x; to[s].scales[1] = two.y;
+                to[s].zeros = *reinterpret_cast<const uint32_t*>(zeros);
+            }
+        }
+        if (++ask_turn == a.turns) {
+            ask_turn = 0;
+            if (++ask_chunk == chunks) { ask_chunk = 0; ask_set = min(ask_set + (int)gridDim.x, a.sets - 1); }   // (behind the end the last one once more)
         }
     };
-    ask(blockIdx.x, wk);
+    PackedPiece<PER> piece[2][NS];
+    ask(piece[0]);
+    ask(piece[1]);
+
+    f32x4 y[MT][NS];
+    auto work = [&](const PackedPiece<PER> (&now)[NS], int part0, int p) {
+        f32x4 acc[MT][NS];
+        const char* at = lds + p * (16 * of_c) + c * of_c;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint4 x[MT][NP];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+                    x[mt][i] = *reinterpret_cast<const uint4*>(at + i * plane + w * (4 * of_c) + 16 * min(16 * mt + (ln & 15), rows - 1));
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const auto op = codes_operand<TYPE>(w == 0 ? now[s].codes.x : w == 1 ? now[s].codes.y : w == 2 ? now[s].codes.z : now[s].codes.w);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = NP - 1; i >= 0; --i)
+                        acc[mt][s] = product<TYPE>(x[mt][i], op, w % PER == 0 && i == NP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[mt][s]);
+            }
+            if ((w + 1) % PER != 0) continue;
+            const int g = w / PER;
+            const bool counts = (part0 + p) * kPackInputs + g * (32 * PER) < a.K;     // (scales behind the last group are not used)
+            f32x4 X[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) X[mt] = *reinterpret_cast<const f32x4*>(sums + (p * EACH + g) * (16 * MT) + 16 * mt + 4 * c);
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const uint32_t bits = PER == 1 ? now[s].scales[PER == 1 ? g >> 1 : 0] >> (16 * (g & 1)) & 0xffffu : now[s].scales[0] >> (16 * g) & 0xffffu;
+                const float sc = !counts ? 0.f : a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
+                const float zero = a.w[GATED ? s & 1 : 0].zeros ? (float)(now[s].zeros >> (8 * g) & 0xffu) : 8.f;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[mt][s][i] = fmaf(sc, fmaf(-zero, X[mt][i], acc[mt][s][i]), y[mt][s][i]);
+            }
+            if constexpr (PER == 1 && MT * NS == 8) __builtin_amdgcn_sched_barrier(0);   // (several groups' sums at once have no registers)
+        }
+    };
+
+    const int finishing = (MT * NT) << a.log_across;    // tiles of results, eight at most
+    bool second = false;
     for (int set = blockIdx.x; set < a.sets; set += gridDim.x) {
-        f32x4 y[MT][NS], acc[MT][NS];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) { y[mt][s] = f32x4{0.f, 0.f, 0.f, 0.f}; acc[mt][s] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+            for (int s = 0; s < NS; ++s) y[mt][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // the tile of results that the wave finishes, and what is added to it
+        const int nt = wave % NT, mt_of = wave / NT % MT, of = wave / (NT * MT);
+        const int64_t n = ((int64_t)((set << a.log_across) + of) * NT + nt) * kPackOutputs + (ln & 15);
+        const bool mine = wave < finishing && n < a.N;
+        f32x4 plus = {0.f, 0.f, 0.f, 0.f};
+        if (!GATED && mine) {
+            const float b = a.bias ? a.bias[n] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int m = 16 * mt_of + 4 * c + i;
+                plus[i] = a.add && m < rows ? added(a, m0 + m, n) + b : b;
+            }
+        }
         for (int chunk = 0; chunk < chunks; ++chunk) {
             const int part0 = chunk * a.chunk, here = min(a.chunk, a.parts - part0);
             if (chunks > 1 || set == (int)blockIdx.x) {
                 __syncthreads();
-                for (int u = threadIdx.x; u < here * ROWS * 4; u += 64 * kPackedWaves) {
-                    const int c = u & 3, m = (u >> 2) % ROWS, p = (u >> 2) / ROWS;
-                    if (m >= rows) continue;
+                for (int u = threadIdx.x; u < here * rows * 4; u += 64 * kPackedWaves) {
+                    const int q = u >> 2, m = q % rows, p = q / rows, cc = u & 3;
                     float group = 0.f;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const int k = (part0 + p) * kPackInputs + 32 * w + 8 * c;
+                        const int k = (part0 + p) * kPackInputs + 32 * w + 8 * cc;
                         const int64_t from = (int64_t)(m0 + m) * a.ldx + k;
                         float x[8];
                         if (k + 8 <= a.K) load_values<TYPE>(a.x, from, x);
@@ -167,102 +230,49 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
                         }
                         uint4 op[NP];
                         row_operand<TYPE>(x, op);
-                        char* to = lds + ((p * 4 + w) * 4 + c) * CS + m * 16;
+                        char* to = lds + ((p * 4 + w) * 4 + cc) * of_c + m * 16;
 #pragma unroll
                         for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(to + i * plane) = op[i];
-                        // the sum of a row's group: eight inputs of this lane, the other three lanes' of the 32, earlier operands'
-                        float of = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                        of += dpp_f32<0xB1>(of);
-                        of += dpp_f32<0x4E>(of);
-                        group += of;
-                        if ((w + 1) % per == 0) {
-                            if (c == 0) sums[((p * 4 + w) / per) * ROWS + m] = group;
+                        group += quad_sum(x);
+                        if ((w + 1) % PER == 0) {
+                            if (cc == 0) sums[(p * EACH + w / PER) * (16 * MT) + m] = group;
                             group = 0.f;
                         }
                     }
                 }
                 __syncthreads();
             }
-            const int turns = (here + deep - 1) / deep;
-            for (int turn = 0; turn < turns; ++turn) {
+            for (int turn = 0; turn < a.turns; turn += 2) {
                 const int p = turn * deep + wk;
-                PackedPiece now[NS];
-#pragma unroll
-                for (int s = 0; s < NS; ++s) now[s] = next[s];
-                if (turn + 1 < turns) ask(set, part0 + p + deep);
-                else if (chunk + 1 < chunks) ask(set, part0 + a.chunk + wk);
-                else if (set + (int)gridDim.x < a.sets) ask(set + gridDim.x, wk);
-                if (p >= here) continue;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint4 x[MT][NP];
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int i = 0; i < NP; ++i)
-                            x[mt][i] = *reinterpret_cast<const uint4*>(lds + i * plane + ((p * 4 + w) * 4 + (ln >> 4)) * CS + (16 * mt + (ln & 15)) * 16);
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        const uint32_t word = w == 0 ? now[s].codes.x : w == 1 ? now[s].codes.y : w == 2 ? now[s].codes.z : now[s].codes.w;
-                        const auto op = codes_operand<TYPE>(word);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int i = NP - 1; i >= 0; --i) acc[mt][s] = product<TYPE>(x[mt][i], op, acc[mt][s]);
-                    }
-                    if ((w + 1) % per != 0) continue;
-                    const int g = w / per;
-                    if ((part0 + p) * kPackInputs + (g << a.shift) >= a.K) continue;     // (scales behind the last group are not used)
-                    f32x4 X[MT];
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) X[mt] = *reinterpret_cast<const f32x4*>(sums + ((p * 4 + w) / per) * ROWS + 16 * mt + 4 * (ln >> 4));
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        const uint32_t bits = (uint32_t)(now[s].scales >> (16 * g)) & 0xffffu;
-                        const float sc = a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
-                        const float zero = (float)(now[s].zeros >> (8 * g) & 0xffu);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) y[mt][s][i] = fmaf(sc, fmaf(-zero, X[mt][i], acc[mt][s][i]), y[mt][s][i]);
-                            acc[mt][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        }
-                    }
-                }
+                if (p < here) work(piece[0], part0, p);
+                ask(piece[0]);
+                if (p + deep < here) work(piece[1], part0, p + deep);
+                ask(piece[1]);
             }
         }
-        auto finish = [&](int of, int mt, int nt, f32x4 g, f32x4 u) {
-            const int64_t n = ((int64_t)(set * across + of) * NT + nt) * kPackOutputs + (ln & 15);
-            if (n >= a.N) return;
+        auto finish = [&](f32x4 g, f32x4 u, int mt) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int m = 16 * mt + 4 * (ln >> 4) + i;
-                if (m < rows) put_result(a, m0 + m, n, GATED ? activate(g[i], a.activation) * u[i] : g[i]);
+                const int m = 16 * mt + 4 * c + i;
+                if (m < rows) put_result(a, m0 + m, n, GATED ? activate(g[i], a.activation) * u[i] : g[i] + plus[i]);
             }
         };
-        if (deep == 1) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) finish(wn, mt, nt, y[mt][GATED ? 2 * nt : nt], y[mt][GATED ? 2 * nt + 1 : nt]);
-            continue;
-        }
-        // waves that share inputs: their sums through LDS, each wave adds up some of the tiles, in order
-        if (a.join_at == 0) __syncthreads();
+        // waves that share inputs: their sums through LDS, each wave adds up a tile, in order
+        f32x4* join = reinterpret_cast<f32x4*>(lds + a.join_at + (second ? packed_join(MT, NS) : 0));
+        second = !second;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) join[(((wk * across + wn) * MT + mt) * NS + s) * 64 + ln] = y[mt][s];
-        __syncthreads();
-        for (int i = wave; i < across * MT * NT; i += kPackedWaves) {
-            const int nt = i % NT, mt = i / NT % MT, of = i / (NT * MT);
+            for (int s = 0; s < NS; ++s) join[((wave * MT + mt) * NS + s) * 64 + ln] = y[mt][s];
+        lds_barrier();
+        if (mine) {
             f32x4 sum[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
             for (int d = 0; d < deep; ++d)
 #pragma unroll
-                for (int h = 0; h < (GATED ? 2 : 1); ++h) sum[h] += join[(((d * across + of) * MT + mt) * NS + (GATED ? 2 * nt + h : nt)) * 64 + ln];
-            finish(of, mt, nt, sum[0], sum[1]);
+                for (int h = 0; h < (GATED ? 2 : 1); ++h)
+                    sum[h] += join[((((d << a.log_across) + of) * MT + mt_of) * NS + (GATED ? 2 * nt + h : nt)) * 64 + ln];
+            finish(sum[0], sum[1], mt_of);
         }
-        __syncthreads();
     }
 }
 

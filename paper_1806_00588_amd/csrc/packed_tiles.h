@@ -1,25 +1,31 @@
 // Many rows times weights of 4 bits: y[m, n] = sum_g scale[n, g] sum_{k in g} x[m, k] (code[n, k] - zero[n, g]).
 //
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
-// blocks of 1 KB, straight to LDS.  A workgroup of four waves makes 128 rows; each wave has its own outputs, so no weight is converted twice in a
-// workgroup, and all share the rows.  code - zero is exact in bf16 and fp16; a group's products are summed up by themselves, then scaled and added to
-// what came before, so nothing but fp32 sums rounds.
+// blocks of 1 KB, straight to LDS.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
+// converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
+// that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.
+// (128 x 64 and four waves, with accumulators in the other 256, which only the matrix instructions reach: 2048 x 8192 x 8192 in fp16 541 us, moves being
+// most of it.)
 #pragma once
 #include "packed_rows.h"
 
 namespace lshbeam {
 
-constexpr int kTileRows = 8;        // times 16 rows of a workgroup
-constexpr int kTileWaves = 4;
+constexpr int kTileAcross = 4;      // waves along the outputs
+constexpr int kTileWaves = 2 * kTileAcross;
+// bf16: codes enter as they are, the zero is applied to a group's sum with the sum of its inputs (a conversion of 7 instructions for eight codes);
+// else code - zero enters (fp16 11, fp32, where products take three times as long, 19).
+template <int TYPE> constexpr bool kTileSums = TYPE == kTypeBf16;
 
 // [16 rows][part][4][plane] blocks of 1 KB.  A wave for 16 rows and a part; four neighbouring lanes read 32 neighbouring inputs.
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, int64_t units) {
+__global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, float* sums, int64_t units) {
     constexpr int P = kRowPlanes<TYPE>;
     const int64_t unit = (int64_t)blockIdx.x * 4 + wave_id();
     if (unit >= units) return;
     const int64_t mt = unit / a.parts, m = mt * 16 + (lane_id() >> 2);
-    const int part = (int)(unit - mt * a.parts), c = lane_id() & 3;
+    const int part = (int)(unit - mt * a.parts), c = lane_id() & 3, per = 1 << (a.shift - 5);
+    float group = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const int k = part * kPackInputs + 32 * w + 8 * c;
@@ -34,20 +40,31 @@ __global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, int6
         row_operand<TYPE>(x, op);
 #pragma unroll
         for (int p = 0; p < P; ++p) *reinterpret_cast<uint4*>(to + ((unit * 4 + w) * P + p) * 1024 + (16 * c + (lane_id() >> 2)) * 16) = op[p];
+        if constexpr (kTileSums<TYPE>) {         // [16 rows][part][group][row]
+            group += quad_sum(x);
+            if ((w + 1) % per == 0) {
+                if (c == 0) sums[(unit * (4 / per) + w / per) * 16 + (lane_id() >> 2)] = group;
+                group = 0.f;
+            }
+        }
     }
 }
 
-template <int TYPE, int NS> struct TilesPlan {
+template <int TYPE, int MT, int NS> struct TilesPlan {     // MT: times 16 rows of a wave, a workgroup has twice that
     static constexpr int P = kRowPlanes<TYPE>;
-    static constexpr int KS = P == 1 ? 2 : 1;                        // times 32 inputs of a stage
+    static constexpr int KS = P == 1 || MT < 4 ? 2 : 1;              // times 32 inputs of a stage
     static constexpr int kOf = 4 / KS;                               // stages of a part
     static constexpr int kRing = P == 1 ? 5 : 4;                     // stages of rows in LDS, or on their way
-    static constexpr int kRowsSlot = kTileRows * KS * P * 1024;
-    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kTileWaves * NS * 1024;          // parts: three
-    static constexpr int kScales = kCodes + 3 * kCodesSlot, kScalesSlot = kTileWaves * 768;
-    static constexpr int kLds = kScales + 3 * kScalesSlot;
+    static constexpr int kRowsSlot = 2 * MT * KS * P * 1024;
+    static constexpr int kRowsEach = 2 * MT * KS * P / kTileWaves;   // a wave's loads of rows
+    static constexpr int kCodesEach = NS < 2 ? 1 : NS / 2;           // a wave's loads of codes
+    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kTileAcross * NS * 1024;         // parts: three
+    static constexpr int kScales = kCodes + 3 * kCodesSlot, kScalesSlot = kTileAcross * 768;
+    static constexpr int kSums = kScales + 3 * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? 2 * MT * 256 : 0;
+    static constexpr int kLds = kSums + 3 * kSumsSlot;
+    static_assert(kLds <= (int)kMaxDynLds && kRowsEach * kTileWaves == 2 * MT * KS * P, "every wave asks for as much");
     // loads of a wave for the j-th stage of a part
-    static constexpr int loads(int j) { return 2 * KS * P + (j % kOf == 0 ? NS + 3 : 0); }
+    static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + 2 + kTileSums<TYPE> : 0); }
     // ... that may be under way when stage j begins: all but those for it and the next one
     static constexpr int later(int j) {
         int n = 0;
@@ -56,8 +73,9 @@ template <int TYPE, int NS> struct TilesPlan {
     }
 };
 
-// Eight codes less their zero, exactly.
+// Eight codes, less their zero unless that comes later, exactly.
 template <int TYPE> __device__ __forceinline__ typename OperandOf<TYPE>::type weights_operand(uint32_t word, float zero) {
+    if constexpr (kTileSums<TYPE>) return codes_operand<TYPE>(word);
     const uint32_t lo = word & 0x0f0f0f0fu, hi = word >> 4 & 0x0f0f0f0fu;
     if constexpr (TYPE == kTypeF16) {
         const _Float16 z = (_Float16)zero;
@@ -81,61 +99,74 @@ template <int TYPE> __device__ __forceinline__ typename OperandOf<TYPE>::type we
 
 struct TilesArgs {
     PackedArgs p;
-    const char* x;             // k_packed_lay's blocks
+    const char* x;             // k_packed_lay's blocks, and its sums
+    const char* sums;
     int row_tiles;             // 16 rows each
     int row_groups, sets;      // workgroups along the rows, along the outputs
 };
 
-// NS: tiles of 16 outputs of a wave (gated: half of them of each matrix, gate and up in turn).
-template <int TYPE, int NS, bool GATED>
+// NS: tiles of 16 outputs of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
+template <int TYPE, int MT, int NS, int PER, bool GATED>
 __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t) {
-    using Plan = TilesPlan<TYPE, NS>;
-    constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS;
+    using Plan = TilesPlan<TYPE, MT, NS>;
+    constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS, EACH = 4 / PER;
+    constexpr bool SUMS = kTileSums<TYPE>;
     extern __shared__ __align__(16) char lds[];
     const PackedArgs& a = t.p;
-    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), wn = wave % kTileAcross, wm = wave / kTileAcross;
     // workgroups go round the eight XCDs one by one; an XCD gets neighbouring ones: four along the outputs, then along the rows
     const int total = t.row_groups * t.sets, each_xcd = (total + 7) / 8;
     const int u = (int)(blockIdx.x & 7) * each_xcd + (int)(blockIdx.x >> 3);
     if (u >= total || (int)(blockIdx.x >> 3) >= each_xcd) return;
     const int band = u / (4 * t.row_groups), wide = min(4, t.sets - 4 * band), in_band = u - band * 4 * t.row_groups;
     const int group = in_band / wide, set = 4 * band + in_band % wide;
-    const int tile0 = (set * kTileWaves + wave) * NT, mt0 = group * kTileRows;
-    const int each = kPackInputs >> a.shift, per = 1 << (a.shift - 5);
+    const int tile0 = (set * kTileAcross + wn) * NT, mt0 = group * 2 * MT;
+    // stream s of the waves with outputs w: matrix, tile's first part
+    auto unit_of = [&](int w, int s) { return (int64_t)min((set * kTileAcross + w) * NT + (GATED ? s >> 1 : s), a.tiles - 1) * a.parts; };
 
-    const char* rows_from[2];
+    const char* rows_from[Plan::kRowsEach];      // of 16 rows those of a stage lie side by side
 #pragma unroll
-    for (int i = 0; i < 2; ++i) rows_from[i] = t.x + (int64_t)min(mt0 + 2 * wave + i, t.row_tiles - 1) * a.parts * (4 * P * 1024) + 16 * ln;
-    int64_t units[NS];         // the tiles' first parts
+    for (int i = 0; i < Plan::kRowsEach; ++i) {
+        const int b = wave * Plan::kRowsEach + i;
+        rows_from[i] = t.x + (int64_t)min(mt0 + b / (KS * P), t.row_tiles - 1) * a.parts * (4 * P * 1024) + b % (KS * P) * 1024 + 16 * ln;
+    }
+    const char* sums_from = t.sums + (int64_t)min(mt0 + wave % (2 * MT), t.row_tiles - 1) * a.parts * (EACH * 64) + 4 * min(ln, EACH * 16 - 1);
+    const char* codes_from[Plan::kCodesEach];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) units[s] = (int64_t)min(tile0 + (GATED ? s >> 1 : s), a.tiles - 1) * a.parts;
-    // scales and zeros, 4 bytes a lane: 16 lanes a tile (of eight, four of them twice)
+    for (int i = 0; i < Plan::kCodesEach; ++i) {
+        const int s = (wave * Plan::kCodesEach + i) % (kTileAcross * NS);
+        codes_from[i] = reinterpret_cast<const char*>(a.w[GATED ? s & 1 : 0].codes) + unit_of(s / NS, s % NS) * kPackBytes + 16 * ln;
+    }
+    // scales (the first four waves) and zeros of the wave's streams, 4 bytes a lane: 16 lanes a stream, scales twice that
     const int mine = min(ln >> 4, NS - 1);
-    const int64_t my_unit = (int64_t)min(tile0 + (GATED ? mine >> 1 : mine), a.tiles - 1) * a.parts;
     const PackedRef& my = a.w[GATED ? mine & 1 : 0];
     const char* scales_from[2];
+    int scales_step;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) scales_from[i] = reinterpret_cast<const char*>(my.scales) + my_unit * (32 * each) + 4 * min((ln & 15) + 16 * i, 8 * each - 1);
-    const char* zeros_from = my.zeros ? reinterpret_cast<const char*>(my.zeros) + my_unit * (16 * each) + 4 * min(ln & 15, 4 * each - 1) : scales_from[0];
-    const int zeros_step = my.zeros ? 16 * each : 32 * each;
+    for (int i = 0; i < 2; ++i) {
+        if (wm == 0 || !my.zeros) {
+            scales_step = 32 * EACH;
+            scales_from[i] = reinterpret_cast<const char*>(my.scales) + unit_of(wn, mine) * scales_step + 4 * min((ln & 15) + 16 * i, 8 * EACH - 1);
+        } else {
+            scales_step = 16 * EACH;
+            scales_from[i] = reinterpret_cast<const char*>(my.zeros) + unit_of(wn, mine) * scales_step + 4 * min(ln & 15, 4 * EACH - 1);
+        }
+    }
 
     int ask_part = 0, ask_in = 0, ask_slot = 0, ask_codes = 0;
     auto ask = [&]() {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int b = 0; b < KS * P; ++b)
-                load_to_lds16(rows_from[i] + ((int64_t)ask_part * 4 + ask_in * KS) * (P * 1024) + b * 1024,
-                              lds + ask_slot * Plan::kRowsSlot + ((2 * wave + i) * KS * P + b) * 1024);
+        for (int i = 0; i < Plan::kRowsEach; ++i)
+            load_to_lds16(rows_from[i] + ((int64_t)ask_part * 4 + ask_in * KS) * (P * 1024), lds + ask_slot * Plan::kRowsSlot + (wave * Plan::kRowsEach + i) * 1024);
         if (ask_in == 0) {
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-                load_to_lds16(a.w[GATED ? s & 1 : 0].codes + (units[s] + ask_part) * kPackBytes + 16 * ln,
-                              lds + Plan::kCodes + ask_codes * Plan::kCodesSlot + (wave * NS + s) * 1024);
-            char* to = lds + Plan::kScales + ask_codes * Plan::kScalesSlot + wave * 768;
-            load_to_lds4(scales_from[0] + (int64_t)ask_part * (32 * each), to);
-            load_to_lds4(scales_from[1] + (int64_t)ask_part * (32 * each), to + 256);
-            load_to_lds4(zeros_from + (int64_t)ask_part * zeros_step, to + 512);
+            for (int i = 0; i < Plan::kCodesEach; ++i)
+                load_to_lds16(codes_from[i] + (int64_t)ask_part * kPackBytes,
+                              lds + Plan::kCodes + ask_codes * Plan::kCodesSlot + (wave * Plan::kCodesEach + i) % (kTileAcross * NS) * 1024);
+            char* to = lds + Plan::kScales + ask_codes * Plan::kScalesSlot + wn * 768 + wm * 512;
+            load_to_lds4(scales_from[0] + (int64_t)ask_part * scales_step, to);
+            load_to_lds4(scales_from[1] + (int64_t)ask_part * scales_step, to + (wm == 0 ? 256 : 0));
+            if constexpr (SUMS) load_to_lds4(sums_from + (int64_t)ask_part * (EACH * 64), lds + Plan::kSums + ask_codes * Plan::kSumsSlot + wave % (2 * MT) * 256);
         }
         ask_slot = ask_slot + 1 == Plan::kRing ? 0 : ask_slot + 1;
         if (++ask_in == OF) {                    // (behind the end the last part once more)
@@ -146,19 +177,19 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
     };
     for (int i = 0; i < Plan::kRing - 1; ++i) ask();
 
-    f32x4 y[kTileRows][NS], acc[kTileRows][NS];
+    f32x4 y[MT][NS], acc[MT][NS];
 #pragma unroll
-    for (int m = 0; m < kTileRows; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) y[m][s] = acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < NS; ++s) y[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
     int slot = 0, codes_slot = 0;
     constexpr int AHEAD = P == 1;    // rows are read 32 inputs ahead (three planes: there are no registers for that, and three times the time)
-    uint4 x[AHEAD + 1][kTileRows][P];
-    auto read_rows = [&](uint4 (&to)[kTileRows][P], int of, int ks) {
+    uint4 x[AHEAD + 1][MT][P];
+    auto read_rows = [&](uint4 (&to)[MT][P], int of, int ks) {
 #pragma unroll
-        for (int m = 0; m < kTileRows; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int p = 0; p < P; ++p) to[m][p] = *reinterpret_cast<const uint4*>(lds + of * Plan::kRowsSlot + ((m * KS + ks) * P + p) * 1024 + 16 * ln);
+            for (int p = 0; p < P; ++p) to[m][p] = *reinterpret_cast<const uint4*>(lds + of * Plan::kRowsSlot + (((wm * MT + m) * KS + ks) * P + p) * 1024 + 16 * ln);
     };
     wait_vmem<Plan::later(-1)>();
     lds_barrier();
@@ -166,19 +197,10 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
     for (int part = 0; part < a.parts; ++part) {
         uint4 codes[NS];
         float scale[NS], zero[NS];
-        const char* sc = lds + Plan::kScales + codes_slot * Plan::kScalesSlot + wave * 768;
-        auto read_group = [&](int g) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int at = (ln & 15) * each + g;
-                const uint32_t bits = *reinterpret_cast<const uint16_t*>(sc + (at >> 5) * 256 + (s & 3) * 64 + 2 * (at & 31));
-                scale[s] = a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
-                zero[s] = a.w[GATED ? s & 1 : 0].zeros ? (float)*reinterpret_cast<const uint8_t*>(sc + 512 + (s & 3) * 64 + at) : 8.f;
-            }
-        };
+        const char* sc = lds + Plan::kScales + codes_slot * Plan::kScalesSlot + wn * 768;
 #pragma unroll
         for (int ks4 = 0; ks4 < 4; ++ks4) {
-            const int j = ks4 / KS, ks = ks4 % KS;
+            const int j = ks4 / KS, ks = ks4 % KS, g = ks4 / PER;
             if (ks == 0) {                       // a stage: it is here, and so is the next one when the barrier is behind us
                 if (j == 0) wait_vmem<Plan::later(0)>();
                 else if (j == 1) wait_vmem<Plan::later(1)>();
@@ -189,9 +211,17 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             }
             if (ks4 == 0) {
 #pragma unroll
-                for (int s = 0; s < NS; ++s) codes[s] = *reinterpret_cast<const uint4*>(lds + Plan::kCodes + codes_slot * Plan::kCodesSlot + (wave * NS + s) * 1024 + 16 * ln);
+                for (int s = 0; s < NS; ++s) codes[s] = *reinterpret_cast<const uint4*>(lds + Plan::kCodes + codes_slot * Plan::kCodesSlot + (wn * NS + s) * 1024 + 16 * ln);
             }
-            if (ks4 % per == 0) read_group(ks4 / per);
+            if (ks4 % PER == 0) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const int at = (ln & 15) * EACH + g;
+                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(sc + (at >> 5) * 256 + s * 64 + 2 * (at & 31));
+                    scale[s] = a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
+                    zero[s] = a.w[GATED ? s & 1 : 0].zeros ? (float)*reinterpret_cast<const uint8_t*>(sc + 512 + s * 64 + at) : 8.f;
+                }
+            }
             if constexpr (AHEAD) {
                 const int after = ks + 1 == KS ? (slot + 1 == Plan::kRing ? 0 : slot + 1) : slot;
                 read_rows(x[(ks4 + 1) & 1], after, (ks + 1) % KS);
@@ -201,40 +231,46 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
                 const uint32_t word = ks4 == 0 ? codes[s].x : ks4 == 1 ? codes[s].y : ks4 == 2 ? codes[s].z : codes[s].w;
                 const auto op = weights_operand<TYPE>(word, zero[s]);
 #pragma unroll
-                for (int m = 0; m < kTileRows; ++m)
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int p = P - 1; p >= 0; --p) acc[m][s] = product<TYPE>(x[ks4 & AHEAD][m][p], op, acc[m][s]);
+                    for (int p = P - 1; p >= 0; --p)
+                        acc[m][s] = product<TYPE>(x[ks4 & AHEAD][m][p], op, ks4 % PER == 0 && p == P - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[m][s]);
             }
-            if ((ks4 + 1) % per == 0) {
-                const bool counts = part * kPackInputs + ((ks4 / per) << a.shift) < a.K;    // (scales behind the last group are not used)
+            if ((ks4 + 1) % PER == 0) {
+                const bool counts = part * kPackInputs + g * (32 * PER) < a.K;    // (scales behind the last group are not used)
+                f32x4 X[MT];
+                if constexpr (SUMS) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        X[m] = *reinterpret_cast<const f32x4*>(lds + Plan::kSums + codes_slot * Plan::kSumsSlot + (wm * MT + m) * 256 + g * 64 + 16 * (ln >> 4));
+                }
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const float f = counts ? scale[s] : 0.f;
 #pragma unroll
-                    for (int m = 0; m < kTileRows; ++m) {
+                    for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[m][s][i] = fmaf(f, acc[m][s][i], y[m][s][i]);
-                        acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    }
+                        for (int i = 0; i < 4; ++i) y[m][s][i] = fmaf(f, SUMS ? fmaf(-zero[s], X[m][i], acc[m][s][i]) : acc[m][s][i], y[m][s][i]);
                 }
             }
             if (ks + 1 == KS) slot = slot + 1 == Plan::kRing ? 0 : slot + 1;
+            if constexpr (PER < 4) __builtin_amdgcn_sched_barrier(0);   // (several groups' sums at once have no registers)
         }
         codes_slot = codes_slot + 1 == 3 ? 0 : codes_slot + 1;
     }
-    wait_vmem<0>();
+    wait_vmem<0>();                              // (nothing may come into another workgroup's LDS)
 #pragma unroll
-    for (int m = 0; m < kTileRows; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int64_t n = (int64_t)(tile0 + nt) * kPackOutputs + (ln & 15);
             if (n >= a.N) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t row = (int64_t)(mt0 + m) * 16 + 4 * (ln >> 4) + i;
+                const int64_t row = (int64_t)(mt0 + wm * MT + m) * 16 + 4 * (ln >> 4) + i;
                 if (row >= a.M) continue;
                 if constexpr (GATED) put_result(a, row, n, activate(y[m][2 * nt][i], a.activation) * y[m][2 * nt + 1][i]);
-                else put_result(a, row, n, y[m][nt][i]);
+                else put_result(a, row, n, y[m][nt][i] + ((a.add ? added(a, row, n) : 0.f) + (a.bias ? a.bias[n] : 0.f)));
             }
         }
 }
