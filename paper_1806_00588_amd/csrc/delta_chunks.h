@@ -4,7 +4,7 @@
 //   out = scale (e Q S + A U),           A_ij = e^(c_i - c_j) q_i.k_j      for j <= i
 //   S <- e^(c_last) S + K^T (e^(c_last - c_j) u_j)_j
 //
-// What does not depend on the state -- T = (1 + L)^-1 diag(b), A, and K, Q, K^T, V in the order of the matrix operands -- is made for all chunks at once
+// What does not depend on the state -- T = (1 + L)^-1 diag(b), A, and K, Q, K^T in the order of the matrix operands -- is made for all chunks at once
 // by k_delta_prepare and goes through the workspace; k_delta_chain goes through a row's chunks in order.  The state's columns do not meet: a wave
 // has 16 of them in registers, four waves share what comes through LDS.
 //
@@ -19,7 +19,6 @@
 namespace lshbeam {
 
 constexpr int kChunk = 64;            // tokens
-constexpr int kStageBlocks = 8;       // operands of 1 KB that the waves of k_delta_chain wait for together
 
 // Row of row m of tile t: of two tiles, lane c's 4 + 4 rows are neighbours.
 __host__ __device__ constexpr int row_of(int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); }
@@ -28,17 +27,12 @@ __device__ __forceinline__ int place_of_row(int r) { return 4 * (r >> 3 & 3) + (
 
 // Operands of a chunk and head in the workspace, NK = ceil(k_dim / 32):
 //   for each 32 of k_dim: K and Q [4 tiles of tokens][planes]; then e and e^(c_last - c_j) [2][64] fp32; T [6][3], A [6][its planes]; K^T [2][2 NK tiles][planes]
-// in blocks of 1 KB, and V [64 columns at a time][parts of two blocks][4 tiles of columns][2].  k_delta_chain takes them in this order, V behind K and Q.  Of T and A those (tile of rows, 32 columns) that are not zero: (0, 0), (1, 0),
+// in blocks of 1 KB.  Of T and A those (tile of rows, 32 columns) that are not zero: (0, 0), (1, 0),
 // (2, 0), (2, 1), (3, 0), (3, 1).
 template <int TYPE, int NK> struct ChunkPlan {
     static constexpr int P = TYPE == kTypeBf16 ? 1 : TYPE == kTypeF16 ? 2 : 3;    // planes of K and Q
     static constexpr int PA = TYPE == kTypeF32 ? 3 : 2;                           // of A, and of what it meets
     static constexpr int kScalars = NK * 8 * P, kT = kScalars + 1, kA = kT + 18, kKt = kA + 6 * PA, kBlocks = kKt + 4 * NK * P;
-    static constexpr int kStages = (kBlocks + kStageBlocks - 1) / kStageBlocks;   // without V's
-    static constexpr int kVStages = TYPE == kTypeF32 ? 2 : 1;                     // V of 64 columns
-    static constexpr int kBeforeV = NK * P;                                       // stages before V's
-    static_assert(kScalars == kBeforeV * kStageBlocks && kStageBlocks == 8, "V's stages come between two others");
-    static constexpr size_t bytes(int Dv) { return ((size_t)kStages + (Dv + 63) / 64 * kVStages) * kStageBlocks * 1024; }
 };
 __host__ __device__ constexpr int block_of(int t, int s) { return t < 2 ? t : 2 * t - 2 + s; }
 
@@ -46,7 +40,7 @@ struct ChunkArgs {
     DeltaArgs d;
     char* room;                // workspace: [pairs][chunks of the segment] of pair_bytes
     size_t bytes;              // of a chunk
-    int64_t pair0;             // first pair of a row and a head of the launch
+    int64_t pair0, pairs;      // pairs of a row and a head of the launch
     int chunk0, chunks;        // the segment
     bool first;                // the state comes from the parent, else from state_out
 };
@@ -54,14 +48,17 @@ struct ChunkArgs {
 __device__ __forceinline__ f32x4 mfma_bf16(uint4 a, uint4 b, f32x4 acc) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
-// Products of planes i of a and j of b with i + j < ORDER, the smallest first.
-template <int ORDER, int PA, int PB> __device__ __forceinline__ f32x4 mfma_planes(const uint4 (&a)[PA], const uint4 (&b)[PB], f32x4 acc) {
+// N products of planes i of a and j of b with i + j < ORDER, the smallest first; one after the other of the N, each waiting for its own sum
+// alone (an instruction that adds to the one before it waits for that).
+template <int ORDER, int N, int PA, int PB> __device__ __forceinline__ void mfma_planes(const uint4 (&a)[N][PA], const uint4 (&b)[PB], f32x4 (&acc)[N]) {
 #pragma unroll
     for (int sum = ORDER - 1; sum >= 0; --sum)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
-            if (sum - i >= 0 && sum - i < PB) acc = mfma_bf16(a[i], b[sum - i], acc);
-    return acc;
+            if (sum - i >= 0 && sum - i < PB) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) acc[n] = mfma_bf16(a[n][i], b[sum - i], acc[n]);
+            }
 }
 
 constexpr int kMatrixPitch = 68;   // floats
@@ -79,7 +76,9 @@ __device__ __forceinline__ void put_tile(float* to, f32x4 v) {
     for (int i = 0; i < 4; ++i) to[(4 * (ln >> 4) + i) * kMatrixPitch + (ln & 15)] = v[i];
 }
 
-template <int TYPE, int NK> constexpr int kPrepareLds = ChunkPlan<TYPE, NK>::P * 4 * NK * 1024 + (2 * 64 * kMatrixPitch + 4 * 64) * 4;
+// LDS: the keys and later T in their place, L, small things.
+template <int TYPE, int NK> constexpr int kPrepareKeys = ChunkPlan<TYPE, NK>::P * 4 * NK * 1024 > 64 * kMatrixPitch * 4 ? ChunkPlan<TYPE, NK>::P * 4 * NK * 1024 : 64 * kMatrixPitch * 4;
+template <int TYPE, int NK> constexpr int kPrepareLds = kPrepareKeys<TYPE, NK> + (64 * kMatrixPitch + 3 * 64) * 4;
 
 // A workgroup of four waves for a chunk of a row and head.
 template <int TYPE, int NK>
@@ -88,9 +87,9 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
     constexpr int P = Plan::P;
     extern __shared__ __align__(16) char lds[];
     const DeltaArgs& a = ca.d;
-    float* L = reinterpret_cast<float*>(lds + P * 4 * NK * 1024);
-    float* T = L + 64 * kMatrixPitch;
-    float* chi = T + 64 * kMatrixPitch;
+    float* T = reinterpret_cast<float*>(lds);
+    float* L = reinterpret_cast<float*>(lds + kPrepareKeys<TYPE, NK>);
+    float* chi = L + 64 * kMatrixPitch;
     float *clo = chi + 64, *beta = clo + 64;
     const int64_t pair = ca.pair0 + blockIdx.x / (unsigned)ca.chunks;
     const int at = blockIdx.x % (unsigned)ca.chunks;
@@ -100,6 +99,18 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
     char* to = ca.room + (size_t)blockIdx.x * ca.bytes;
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), c = ln >> 4, m = ln & 15;
 
+    // queries of the wave's tile: asked for before anything waits
+    float xq[NK][8];
+    {
+        const int t = row_of(wave, m);
+        const int64_t q0 = r * a.qp.row + (int64_t)(t0 + t) * a.qp.token + hk * a.qp.head + 8 * c;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xq[s][i] = 0.f;
+            if (t < n && 32 * s + 8 * c < a.Dk) load_values<TYPE>(a.q, q0 + 32 * s, xq[s]);
+        }
+    }
     // the decays' sums, in 64 bits, kept as two numbers of 32
     if (wave == 0) {
         const int64_t i = ((int64_t)r * a.T + t0 + ln) * a.heads + h;
@@ -115,8 +126,9 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
         clo[ln] = (float)(sum - (double)(float)sum);
         beta[ln] = ln < n ? a.beta[i] : 0.f;
         float* scalars = reinterpret_cast<float*>(to + Plan::kScalars * 1024);
-        scalars[ln] = (float)exp(sum);
-        scalars[64 + ln] = (float)exp(last - sum);
+        const double rest = last - sum;          // (e^(h + l) = e^h (1 + l), l being some 2^-24 of h at most)
+        scalars[ln] = expf((float)sum) * (1.f + (float)(sum - (double)(float)sum));
+        scalars[64 + ln] = expf((float)rest) * (1.f + (float)(rest - (double)(float)rest));
     }
     // keys: planes as operands
     for (int u = threadIdx.x; u < kChunk * NK * 4; u += 256) {
@@ -131,7 +143,7 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
         for (int p = 0; p < P; ++p)
             *reinterpret_cast<uint4*>(lds + (((p * 4 + tile_of_row(t)) * NK + (piece >> 2)) * 64 + 16 * (piece & 3) + place_of_row(t)) * 16) = op[p];
     }
-    for (int i = threadIdx.x; i < 64 * kMatrixPitch; i += 256) { L[i] = 0.f; T[i] = 0.f; }
+    for (int i = threadIdx.x; i < 64 * kMatrixPitch; i += 256) L[i] = 0.f;
     __syncthreads();
 
     auto key = [&](int p, int t, int s) { return *reinterpret_cast<const uint4*>(lds + (((p * 4 + t) * NK + s) * 64 + ln) * 16); };
@@ -140,20 +152,16 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) kk[j] = qk[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int tiles = 2 * (wave >> 1) + 2;
-    for (int s = 0; s < NK; ++s) {
-        float x[8];
-        const int t = row_of(wave, m), d = 32 * s + 8 * c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        if (t < n && d < a.Dk) load_values<TYPE>(a.q, r * a.qp.row + (int64_t)(t0 + t) * a.qp.token + hk * a.qp.head + d, x);
-        uint4 q[P], k[P];
-        planes_of<P>(x, q);
+    for (int s = 0; s < NK; ++s) {
+        uint4 kq[2][P];
+        planes_of<P>(xq[s], kq[1]);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            k[p] = key(p, wave, s);
+            kq[0][p] = key(p, wave, s);
             char* block = to + (size_t)(s * 8 * P + wave * P + p) * 1024 + 16 * ln;
-            *reinterpret_cast<uint4*>(block) = k[p];
-            *reinterpret_cast<uint4*>(block + 4 * P * 1024) = q[p];
+            *reinterpret_cast<uint4*>(block) = kq[0][p];
+            *reinterpret_cast<uint4*>(block + 4 * P * 1024) = kq[1][p];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -161,8 +169,10 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
             uint4 other[P];
 #pragma unroll
             for (int p = 0; p < P; ++p) other[p] = key(p, j, s);
-            kk[j] = mfma_planes<3>(k, other, kk[j]);
-            qk[j] = mfma_planes<3>(q, other, qk[j]);
+            f32x4 both[2] = {kk[j], qk[j]};
+            mfma_planes<3>(kq, other, both);
+            kk[j] = both[0];
+            qk[j] = both[1];
         }
     }
 #pragma unroll
@@ -189,32 +199,8 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
         }
         *reinterpret_cast<uint4*>(to + (size_t)(Plan::kKt + b) * 1024 + 16 * ln) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    // values: 16-bit as they are, eight tokens of a column; fp32 four
-    const int groups = (a.Dv + 63) / 64;
-    char* values = to + (size_t)Plan::kStages * kStageBlocks * 1024;
-    for (int b = wave; b < groups * Plan::kVStages * kStageBlocks; b += 4) {
-        const int part = b / kStageBlocks % Plan::kVStages * 2 + (b & 1), tile = b / (kStageBlocks * Plan::kVStages) * 4 + (b >> 1 & 3);
-        const int col = 16 * tile + m;
-        if (16 * tile >= a.Dv) continue;
-        const int64_t from = r * a.vp.row + (int64_t)t0 * a.vp.token + h * a.vp.head + col;
-        uint32_t w[4];
-        if constexpr (TYPE == kTypeF32) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = row_of(part, 4 * c + i);
-                w[i] = t < n ? __float_as_uint(value_at<TYPE>(a.v, from + t * a.vp.token)) : 0u;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = 32 * part + 8 * c + i;
-                const uint32_t v = t < n ? (uint32_t)static_cast<const uint16_t*>(a.v)[from + t * a.vp.token] : 0u;
-                if (i & 1) w[i >> 1] |= v << 16;
-                else w[i >> 1] = v;
-            }
-        }
-        *reinterpret_cast<uint4*>(values + (size_t)b * 1024 + 16 * ln) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * kMatrixPitch; i += 256) T[i] = 0.f;
     __syncthreads();
 
     // (1 + L)^-1: blocks of 16 on the diagonal by substitution, a lane a column; blocks below them by X21 = -X22 L21 X11, twice
@@ -273,199 +259,244 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
     }
 }
 
-// Stages of k_delta_chain that are in LDS or on their way.
-constexpr int kRing = 8;
-constexpr int kChainLds = kRing * kStageBlocks * 1024;
+// LDS of k_delta_chain: K S and Q S of each wave's rows of the state; V - e K S, U, and e^(c_last - c_j) U as operands.  OVER: U lies over the sums.
+template <int PA, bool OVER> struct ChainLds {
+    static constexpr int kR = 4 * 8 * 1024, kU = OVER ? 0 : kR + 2 * 3 * 1024, kLast = kU + 2 * PA * 1024;
+    static constexpr int kBytes = OVER ? kR + 2 * 3 * 1024 : kLast + 2 * 3 * 1024;
+};
 
-// A workgroup of four waves for 64 columns of a row's and head's state.
-template <int TYPE, int NK>
-__global__ void __launch_bounds__(256) k_delta_chain(ChunkArgs ca) {
+// Planes of a tile's four values a lane: its half of the operand that two tiles make.
+template <int N> __device__ __forceinline__ void put_half(char* to, int tile, const f32x4& v) {
+    float x[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
+    uint4 op[N];
+    planes_of<N>(x, op);
+#pragma unroll
+    for (int p = 0; p < N; ++p) *reinterpret_cast<uint2*>(to + ((tile >> 1) * N + p) * 1024 + 16 * lane_id() + 8 * (tile & 1)) = make_uint2(op[p].x, op[p].y);
+}
+// One tile's sum of products of planes, in two accumulators (an instruction that adds to the one before it waits for that).
+template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(const uint4 (&a)[PA], const uint4 (&b)[PB], f32x4 (&acc)[2]) {
+    int turn = 0;
+#pragma unroll
+    for (int sum = ORDER - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (sum - i >= 0 && sum - i < PB) { acc[turn & 1] = mfma_bf16(a[i], b[sum - i], acc[turn & 1]); ++turn; }
+}
+
+// A workgroup of four waves for 16 columns of a row's and head's state.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what is made for
+// tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight to
+// registers, and asked for a chunk ahead.  Bound by the chain of a chunk's instructions: 16 heads of 128 x 128, 8192 tokens TIME us a chunk.  (Four waves with
+// columns of their own, operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk.)
+// AHEAD: chunks that operands are asked for ahead, for which a workgroup has half a CU or a whole one; 0: when they are needed.
+template <int TYPE, int NK, int AHEAD>
+__global__ void __launch_bounds__(256, AHEAD ? 1 : 2) k_delta_chain(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;
-    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2;
-    extern __shared__ __align__(16) char lds[];
+    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4, SETS = AHEAD ? AHEAD : 1;
+    using Lds = ChainLds<PA, AHEAD == 0>;
+    __shared__ __align__(16) char lds[Lds::kBytes];
     const DeltaArgs& a = ca.d;
-    const int64_t pairs = gridDim.x / (unsigned)a.slices;
-    const int64_t local = blockIdx.x % pairs, pair = ca.pair0 + local;     // (a head's workgroups on one XCD, if the pairs are a multiple of eight)
-    const int slice = (int)(blockIdx.x / pairs);
+    // workgroups go round the eight XCDs one by one: those of a pair follow each other on one of them, so that its operands come from there but once
+    const unsigned tiles = (unsigned)a.Dv >> 4, on_xcd = blockIdx.x >> 3;
+    const int64_t local = (int64_t)(on_xcd / tiles) * 8 + (blockIdx.x & 7), pair = ca.pair0 + local;
+    const int tile = (int)(on_xcd % tiles);
+    if (local >= ca.pairs) return;
     const int r = (int)(pair / a.heads), h = (int)(pair - (int64_t)r * a.heads);
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), c = ln >> 4, n = ln & 15;
     const int n_new = delta_new(a, r), begin = ca.chunk0 * kChunk;
     const int chunks = min(ca.chunks, (n_new - begin + kChunk - 1) / kChunk);
     if (!ca.first && chunks <= 0) return;
-    const int col = slice * kDeltaColumns + 16 * wave + n;
-    const bool live = slice * kDeltaColumns + 16 * wave < a.Dv;
+    const int col = 16 * tile + n;
     const int64_t size = (int64_t)a.Dk * a.Dv;
 
-    f32x4 S[2 * NK];
+    f32x4 S[MINE][2];
     const int parent = delta_parent(a, r);
     const float* from = ca.first ? a.state_in + (parent < 0 ? 0 : ((int64_t)parent * a.heads + h) * size) : a.state_out + pair * size;
-    const bool any = live && (!ca.first || parent >= 0);
+    const bool any = !ca.first || parent >= 0;
 #pragma unroll
-    for (int t = 0; t < 2 * NK; ++t)
+    for (int j = 0; j < MINE; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = row_of(t, 4 * c + i);
-            S[t][i] = any && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
-        }
-    // (the compiler's own wait for these loads: here, not with every stage)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int t = 0; t < 2 * NK; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(S[t][i]));
+            for (int i = 0; i < 4; ++i) {
+                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                S[j][t][i] = any && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
+            }
 
-    if (chunks > 0) {
-        constexpr int kStages = Plan::kStages + Plan::kVStages;
-        const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes;
-        int ask_chunk = 0, ask_stage = 0, ask_slot = 0, slot = 0;
-        auto ask = [&]() {                     // the next stage to its slot: two operands a wave
-            const char* of = room + (size_t)ask_chunk * ca.bytes;
-            const int v = ask_stage - Plan::kBeforeV;
-            if (v >= 0 && v < Plan::kVStages) of += ((size_t)Plan::kStages + slice * Plan::kVStages + v) * (kStageBlocks * 1024);
-            else of += (size_t)(v < 0 ? ask_stage : ask_stage - Plan::kVStages) * (kStageBlocks * 1024);
-            of += wave * 2048 + ln * 16;
-            char* to = lds + ask_slot * (kStageBlocks * 1024) + wave * 2048;
-            load_to_lds16(of, to);
-            load_to_lds16(of + 1024, to + 1024);
-            ask_slot = ask_slot + 1 == kRing ? 0 : ask_slot + 1;
-            if (++ask_stage == kStages) { ask_stage = 0; ask_chunk = min(ask_chunk + 1, chunks - 1); }   // (behind the end the last chunk once more)
-        };
-        const char* stage = lds;
-        auto next_stage = [&]() {
-            wait_vmem<2 * (kRing - 2)>();
-            lds_barrier();
-            stage = lds + slot * (kStageBlocks * 1024);
-            slot = slot + 1 == kRing ? 0 : slot + 1;
-            ask();
-        };
-        for (int i = 0; i < kRing - 1; ++i) ask();
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            auto block = [&](int b) {          // asked for one after the other
-                if (b % kStageBlocks == 0) next_stage();
-                return stage + b % kStageBlocks * 1024;
-            };
-            auto operand = [&](int b) { return *reinterpret_cast<const uint4*>(block(b) + 16 * ln); };
-            f32x4 ks[4], qs[4];
+    // Operands.  What a wave has no work for it asks for all the same (another's): the number of loads under way is known to the compiler then.
+    struct Operands {
+        uint4 kq[MINE][8][P], kt[MINE][4][P], tp[2][3], ap[2][PA];
+        f32x4 e, last;
+        float all;
+        typename WordOf<TYPE>::type v[4];
+    } sets[SETS];
+    const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes + 16 * ln;
+    const int64_t v_from = r * a.vp.row + h * a.vp.head + col;
+    auto block = [&](int chunk, int b) { return *reinterpret_cast<const uint4*>(room + (size_t)chunk * ca.bytes + (size_t)b * 1024); };
+    auto ask_kq = [&](Operands& to, int chunk) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) ks[t] = qs[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < MINE; ++j)
 #pragma unroll
-            for (int s = 0; s < NK; ++s) {
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int p = 0; p < P; ++p) to.kq[j][i][p] = block(chunk, (min(wave + 4 * j, NK - 1) * 8 + i) * P + p);
+    };
+    auto ask_values = [&](Operands& to, int chunk) {
+        const float* scalars = reinterpret_cast<const float*>(room - 16 * ln + (size_t)chunk * ca.bytes + Plan::kScalars * 1024);
+        to.e = *reinterpret_cast<const f32x4*>(scalars + row_of(wave, 4 * c));
+        to.last = *reinterpret_cast<const f32x4*>(scalars + 64 + row_of(wave, 4 * c));
+        to.all = scalars[63];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                                        // (tokens behind the last count as if they were it: T has zeros there)
+            const int token = min(begin + chunk * kChunk + row_of(wave, 4 * c + i), n_new - 1);
+            to.v[i] = static_cast<const typename WordOf<TYPE>::type*>(a.v)[v_from + token * a.vp.token];
+        }
+    };
+    auto ask_t = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) to.tp[s][p] = block(chunk, Plan::kT + 3 * block_of(wave, min(s, wave >> 1)) + p);
+    };
+    auto ask_a = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int p = 0; p < PA; ++p) to.ap[s][p] = block(chunk, Plan::kA + PA * block_of(wave, min(s, wave >> 1)) + p);
+    };
+    auto ask_kt = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                                      // [32 tokens][tile of the state's rows]
+#pragma unroll
+                for (int p = 0; p < P; ++p) to.kt[j][i][p] = block(chunk, Plan::kKt + ((i >> 1) * 2 * NK + 2 * min(wave + 4 * j, NK - 1) + (i & 1)) * P + p);
+    };
+    if (AHEAD && chunks > 0) {
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) {
+            const int chunk = min(i, chunks - 1);
+            ask_kq(sets[i], chunk); ask_values(sets[i], chunk); ask_t(sets[i], chunk); ask_a(sets[i], chunk); ask_kt(sets[i], chunk);
+        }
+    }
+
+    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+    f32x4* part = reinterpret_cast<f32x4*>(lds);
+    auto read = [&](int at, int b) { return *reinterpret_cast<const uint4*>(lds + at + b * 1024 + 16 * ln); };
+    auto work = [&](Operands& of, int chunk) __attribute__((always_inline)) {
+        const int after = min(chunk + AHEAD, chunks - 1);                    // (behind the end the last chunk once more)
+        if constexpr (!AHEAD) { ask_kq(of, chunk); ask_values(of, chunk); }
+        // K S and Q S: of the wave's rows of the state
+        f32x4 ks[4] = {none, none, none, none}, qs[4] = {none, none, none, none};
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (wave + 4 * j < NK) {
                 float x[8];
-                uint4 sp[3];
+                uint4 sp[3], op[4][P];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = S[2 * s + (i >> 2)][i & 3];
+                for (int i = 0; i < 8; ++i) x[i] = S[j][i >> 2][i & 3];
                 planes_of<3>(x, sp);
 #pragma unroll
-                for (int which = 0; which < 2; ++which)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        uint4 op[P];
+                    for (int p = 0; p < P; ++p) op[t][p] = of.kq[j][t][p];
+                mfma_planes<3>(op, sp, ks);
 #pragma unroll
-                        for (int p = 0; p < P; ++p) op[p] = operand(s * 8 * P + (which * 4 + t) * P + p);
-                        if (which == 0) ks[t] = mfma_planes<3>(op, sp, ks[t]);
-                        else qs[t] = mfma_planes<ORDER>(op, sp, qs[t]);
-                    }
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) op[t][p] = of.kq[j][4 + t][p];
+                mfma_planes<ORDER>(op, sp, qs);
             }
-            f32x4 v[4], e[4], last[4];
+        if constexpr (AHEAD) ask_kq(of, after);
+        else ask_t(of, chunk);
 #pragma unroll
-            for (int part = 0; part < 2 * Plan::kVStages; ++part) {
-                if (part % 2 == 0) next_stage();
-                const uint4 w = *reinterpret_cast<const uint4*>(stage + (2 * wave + part % 2) * 1024 + 16 * ln);
-                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        for (int t = 0; t < 4; ++t) { part[(wave * 8 + t) * 64 + ln] = ks[t]; part[(wave * 8 + 4 + t) * 64 + ln] = qs[t]; }
+        lds_barrier();
+        // V - e K S of the wave's tile of tokens
+        f32x4 k_sum = none, q_sum = none, v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (TYPE == kTypeF32) v[part][i] = __uint_as_float(words[i]);
-                    else {
-                        v[2 * part + (i >> 1)][2 * (i & 1)] = word_f32<TYPE>((uint16_t)(words[i] & 0xffffu));
-                        v[2 * part + (i >> 1)][2 * (i & 1) + 1] = word_f32<TYPE>((uint16_t)(words[i] >> 16));
-                    }
+        for (int w = 0; w < 4; ++w)
+            if (w < NK) k_sum += part[(w * 8 + wave) * 64 + ln];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[i]));
+        put_half<3>(lds + Lds::kR, wave, v);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (w < NK) q_sum += part[(w * 8 + 4 + wave) * 64 + ln];
+        q_sum *= of.e;
+        lds_barrier();
+        // U = T (V - e K S)
+        f32x4 two[2] = {none, none};
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s <= wave >> 1) {
+                const uint4 rp[3] = {read(Lds::kR, 3 * s), read(Lds::kR, 3 * s + 1), read(Lds::kR, 3 * s + 2)};
+                mfma_two<3>(of.tp[s], rp, two);
+            }
+        if constexpr (AHEAD) ask_t(of, after);
+        else { ask_a(of, chunk); ask_kt(of, chunk); }
+        const f32x4 u = two[0] + two[1];
+        put_half<PA>(lds + Lds::kU, wave, u);
+        put_half<3>(lds + Lds::kLast, wave, u * of.last);
+        const float decay = of.all;
+        if constexpr (AHEAD) ask_values(of, after);
+        lds_barrier();
+        // the state
+        uint4 lp[2][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) lp[s][p] = read(Lds::kLast, 3 * s + p);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (wave + 4 * j < NK) {
+                S[j][0] *= decay;
+                S[j][1] *= decay;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    uint4 op[2][P];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
+                    mfma_planes<3>(op, lp[s], S[j]);
                 }
             }
-            const float* scalars = reinterpret_cast<const float*>(block(Plan::kScalars));
+        if constexpr (AHEAD) ask_kt(of, after);
+        // out = scale (e Q S + A U)
+        two[0] = q_sum;
+        two[1] = none;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                e[t] = *reinterpret_cast<const f32x4*>(scalars + row_of(t, 4 * c));
-                last[t] = *reinterpret_cast<const f32x4*>(scalars + 64 + row_of(t, 4 * c));
+        for (int s = 0; s < 2; ++s)
+            if (s <= wave >> 1) {
+                uint4 up[PA];
+#pragma unroll
+                for (int p = 0; p < PA; ++p) up[p] = read(Lds::kU, PA * s + p);
+                mfma_two<ORDER>(of.ap[s], up, two);
             }
-            const float all = scalars[63];
-            // U = T (V - e K S)
-            uint4 rp[2][3];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = 2 * s + (i >> 2);
-                    x[i] = fmaf(-e[t][i & 3], ks[t][i & 3], v[t][i & 3]);
-                }
-                planes_of<3>(x, rp[s]);
-            }
-            f32x4 u[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                u[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s <= t >> 1; ++s) {
-                    uint4 op[3];
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) op[p] = operand(Plan::kT + 3 * block_of(t, s) + p);
-                    u[t] = mfma_planes<3>(op, rp[s], u[t]);
-                }
-            }
-            // out = scale (e Q S + A U), and what the state gets
-            uint4 up[2][PA], lp[2][3];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = u[2 * s + (i >> 2)][i & 3];
-                planes_of<PA>(x, up[s]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= last[2 * s + (i >> 2)][i & 3];
-                planes_of<3>(x, lp[s]);
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                f32x4 o;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = e[t][i] * qs[t][i];
-#pragma unroll
-                for (int s = 0; s <= t >> 1; ++s) {
-                    uint4 op[PA];
-#pragma unroll
-                    for (int p = 0; p < PA; ++p) op[p] = operand(Plan::kA + PA * block_of(t, s) + p);
-                    o = mfma_planes<ORDER>(op, up[s], o);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int token = begin + chunk * kChunk + row_of(t, 4 * c + i);
-                    if (live && token < n_new) put_value<TYPE>(a.out, r * a.op.row + (int64_t)token * a.op.token + h * a.op.head + col, a.scale * o[i]);
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < 2 * NK; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[t][i] *= all;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int t = 0; t < 2 * NK; ++t) {
-                    uint4 op[P];
-#pragma unroll
-                    for (int p = 0; p < P; ++p) op[p] = operand(Plan::kKt + (s * 2 * NK + t) * P + p);
-                    S[t] = mfma_planes<3>(op, lp[s], S[t]);
-                }
-        }
-        wait_vmem<0>();                        // (what was asked for behind the end must not come into another workgroup's LDS)
-    }
-    if (!live) return;
-    float* to = a.state_out + pair * size;
-#pragma unroll
-    for (int t = 0; t < 2 * NK; ++t)
+        if constexpr (AHEAD) ask_a(of, after);
+        else lds_barrier();                                                  // (the next sums go where U is)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int d = row_of(t, 4 * c + i);
-            if (d < a.Dk) to[(int64_t)d * a.Dv + col] = S[t][i];
+            const int token = begin + chunk * kChunk + row_of(wave, 4 * c + i);
+            if (token < n_new) put_value<TYPE>(a.out, r * a.op.row + (int64_t)token * a.op.token + h * a.op.head + col, a.scale * (two[0][i] + two[1][i]));
         }
+    };
+    for (int chunk = 0; chunk < chunks; chunk += SETS) {
+        work(sets[0], chunk);
+        if constexpr (SETS == 2) {
+            if (chunk + 1 < chunks) work(sets[SETS - 1], chunk + 1);
+        }
+    }
+    float* to = a.state_out + pair * size;
+#pragma unroll
+    for (int j = 0; j < MINE; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                if (d < a.Dk) to[(int64_t)d * a.Dv + col] = S[j][t][i];
+            }
 }
 
 }  // namespace lshbeam

@@ -148,7 +148,7 @@ bool delta_ok(const lsh_delta_params* p) {
 int64_t delta_slices(const lsh_delta_params* p) { return ceil_div(p->v_dim, kDeltaColumns); }
 int64_t delta_pairs(const lsh_delta_params* p) { return (int64_t)p->S * p->B * p->n_heads; }
 bool delta_fits(const lsh_delta_params* p) {
-    return delta_pairs(p) <= kMaxGrid && delta_pairs(p) * p->T <= (int64_t)1 << 26 && delta_pairs(p) * delta_slices(p) <= kMaxGrid;
+    return delta_pairs(p) <= kMaxGrid && delta_pairs(p) * p->T <= (int64_t)1 << 26 && ceil_div(delta_pairs(p), 8) * 8 * (p->v_dim / 16) <= kMaxGrid;
 }
 // Rows of more tokens than this go in chunks of 64.
 constexpr int kTokensMost = 32;
@@ -172,7 +172,7 @@ template <typename F> void for_dims(int32_t dim, F f) {   // f(std::integral_con
 ChunksPlan chunks_plan(const lsh_delta_params* p, int32_t dtype) {
     ChunksPlan w{};
     for_type(dtype, [&](auto type) {
-        for_dims(p->k_dim, [&](auto nk) { w.of_chunk = ChunkPlan<decltype(type)::value, decltype(nk)::value>::bytes(p->v_dim); });
+        for_dims(p->k_dim, [&](auto nk) { w.of_chunk = ChunkPlan<decltype(type)::value, decltype(nk)::value>::kBlocks * 1024; });
     });
     const int64_t most = std::max<int64_t>(1, kChunksRoom / w.of_chunk), all = ceil_div(p->T, kChunk);
     w.pairs = std::min(most, delta_pairs(p));
@@ -186,13 +186,16 @@ template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const 
     const int all = (int)ceil_div(p->T, kChunk);
     for (int64_t pair = 0; pair < delta_pairs(p); pair += w.pairs) {
         const int64_t pairs = std::min(w.pairs, delta_pairs(p) - pair);
-        a.pair0 = pair;
+        a.pair0 = pair; a.pairs = pairs;
         for (int chunk = 0; chunk < all; chunk += w.chunks) {
             a.chunk0 = chunk;
             a.chunks = std::min(w.chunks, all - chunk);
             a.first = chunk == 0;
             if (!launch_room<k_delta_prepare<TYPE, NK>>(dim3((unsigned)(pairs * a.chunks)), 256, kPrepareLds<TYPE, NK>, st, a)) return false;
-            if (!launch_room<k_delta_chain<TYPE, NK>>(dim3((unsigned)(pairs * d.slices)), 256, kChainLds, st, a)) return false;
+            const unsigned grid = (unsigned)(ceil_div(pairs, 8) * 8 * (p->v_dim / 16));
+            constexpr int kAhead = (NK + 3) / 4 * ChunkPlan<TYPE, NK>::P <= 2 ? 2 : 1;       // (what there are registers for)
+            if (grid <= 512) hipLaunchKernelGGL((k_delta_chain<TYPE, NK, kAhead>), dim3(grid), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0>), dim3(grid), dim3(256), 0, st, a);
         }
     }
     return true;
