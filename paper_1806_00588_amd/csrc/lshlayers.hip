@@ -38,10 +38,10 @@ bool quantize_args(const lsh_packed_params* p, const lsh_packed_weights* w, cons
     return ceil_div(a->units, 4) <= kMaxGrid;
 }
 
-// How few rows' products are divided among workgroups of eight waves.
+// How few rows' products are divided among workgroups.
 struct RowsPlan {
     int groups, rows, row_tiles;   // of rows
-    int streams;                   // tiles of a wave (gated: of both matrices)
+    int waves, streams;            // tiles of a wave (gated: of both matrices)
     int log_across, chunk, turns;
     int64_t sets;
     unsigned grid;                 // workgroups of a group of rows
@@ -55,24 +55,26 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     w.rows = (int)ceil_div(M, w.groups);
     w.row_tiles = (int)ceil_div(w.rows, 16);
     const int64_t tiles = tiles_of(p), parts = parts_of(p), planes = dtype == LSH_F32 ? 3 : 1;
-    // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in cycles -- a wave's tile some 300 a
-    // part, its rows' operands some 60 a part and plane, adding up and the results 1200 a round
+    w.waves = w.row_tiles == 1 && tiles * parts > 8 * 256 ? 16 : 8;
+    // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in units of 10 ns -- a wave's tile 40 a
+    // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 90 a round (fitted to 12 rows of fp32 x 40000 x 1000 in six
+    // divisions, 13.6 to 24.6 us, and bf16 x 4096 x 4096 in six, 8.3 to 15)
     int64_t best = INT64_MAX;
-    for (int each = 1; each <= (gated ? 2 : 4); each *= 2)
-        for (int lg = 0; (w.row_tiles * each << lg) <= kPackedWaves; ++lg) {
+    for (int each = 1; each <= (gated ? 1 : 2); each *= 2)
+        for (int lg = 0; (w.row_tiles * each << lg) <= w.waves; ++lg) {
             const int64_t sets = ceil_div(tiles, (int64_t)each << lg), rounds = ceil_div(sets * w.groups, 256), streams = gated ? 2 * each : each;
-            const int64_t cost = rounds * (ceil_div(parts, kPackedWaves >> lg) * w.row_tiles * (300 * streams + 60 * planes) + 1200);
+            const int64_t cost = rounds * (ceil_div(parts, w.waves >> lg) * w.row_tiles * ((planes == 3 ? 57 : 40) * streams + 10 * planes) + 90);
             if (cost < best) { best = cost; w.streams = (int)streams; w.log_across = lg; w.sets = sets; }
         }
-    const int deep = kPackedWaves >> w.log_across;
+    const int deep = w.waves >> w.log_across;
     w.grid = (unsigned)std::min<int64_t>(w.sets, std::max(1, 256 / w.groups));
     // all rows in LDS, or as many of their parts as there is room for
-    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1), join = 2 * packed_join(w.row_tiles, w.streams);
+    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1), join = 2 * packed_join(w.waves, w.row_tiles, w.streams);
     const int64_t chunks = ceil_div(parts, (int64_t)((kMaxDynLds - join) / of_part));
     int64_t chunk = ceil_div(parts, chunks);
     if (chunks > 1 && chunk > deep) chunk = chunk / deep * deep;
     w.chunk = (int)chunk;
-    w.turns = (int)ceil_div(ceil_div(chunk, deep), 2) * 2;
+    w.turns = (int)ceil_div(chunk, deep);
     w.join_at = (int)(chunk * of_part);
     w.lds = w.join_at + join;
     return w;
@@ -133,7 +135,7 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
         char* room = static_cast<char*>(workspace_dev);
         const TilesArgs t{a, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
         ok = launch_packed_tiles(x->dtype, tiles.wave_rows, tiles.streams, gated, t, st);
-    } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups), w.lds, st);
+    } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups), w.lds, st);
     if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
     return ok ? launched() : LSH_ERR_HIP;
 }

@@ -4,8 +4,9 @@
 // bf16 that add up to them, so every product is exact and nothing but the fp32 sums rounds.
 //
 // Few rows: two operations a weight and row, so the weights' bytes bound it.  The rows' operands are in LDS, made once where all of them fit; the weights come
-// straight to registers, two parts of a wave under way.  Eight waves of a workgroup are side by side along the outputs or share the inputs of the
-// same outputs among them, and workgroups go on to further outputs.
+// straight to registers, the next part of a wave while the others work.  The waves of a workgroup are side by side along the outputs or share the inputs of
+// the same outputs among them, and workgroups go on to further outputs.  16 waves of up to 16 rows hide what each waits for (12 rows x 40000 x 1000,
+// fp32: 13.6 us a launch, eight waves with two parts under way 17.4); eight for more rows, which have no registers for that, and for small matrices.
 #pragma once
 #include "packed.h"
 
@@ -31,20 +32,19 @@ struct PackedArgs {
     // of k_packed_rows
     int rows;                  // of a workgroup
     int log_across;            // log2 of the waves side by side along the outputs; the others share their inputs
-    int chunk, turns;          // parts whose rows are in LDS at a time, the most that a wave has of them (even)
+    int chunk, turns;          // parts whose rows are in LDS at a time, the most that a wave has of them
     int sets;                  // groups of tiles
     int join_at;               // where in LDS waves that share inputs add up
 };
 
 constexpr int kRowsPlanesF32 = 3;
 template <int TYPE> constexpr int kRowPlanes = TYPE == kTypeF32 ? kRowsPlanesF32 : 1;
-constexpr int kPackedWaves = 8, kLogWaves = 3;
 // LDS: operands of 32 inputs: [plane][of the chunk][c][row] 16 bytes, the c's 32 bytes apart so that four neighbouring lanes write to banks
 // of their own; sums of the rows' groups; twice (for one group of tiles and the next) what the waves that share inputs add up.
 constexpr int rows_of_c(int rows) { return rows * 16 + 32; }
 constexpr int packed_plane(int rows, int chunk) { return chunk * 4 * 4 * rows_of_c(rows); }
 constexpr int packed_sums(int row_tiles, int chunk) { return chunk * 4 * 16 * row_tiles * 4; }
-constexpr int packed_join(int row_tiles, int streams) { return kPackedWaves * row_tiles * streams * 1024; }
+constexpr int packed_join(int waves, int row_tiles, int streams) { return waves * row_tiles * streams * 1024; }
 
 template <int TYPE> struct OperandOf { using type = bf16x8; };
 template <> struct OperandOf<kTypeF16> { using type = f16x8; };
@@ -110,18 +110,18 @@ template <int PER> struct PackedPiece {
 };
 
 // MT: 16 rows each; NS: tiles of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
-template <int TYPE, int MT, int NS, int PER, bool GATED>
-__global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a) {
+template <int TYPE, int MT, int NS, int PER, bool GATED, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
     extern __shared__ __align__(16) char lds[];
     constexpr int NP = kRowPlanes<TYPE>, NT = GATED ? NS / 2 : NS, EACH = 4 / PER;
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), c = ln >> 4;
     const int wn = wave & ((1 << a.log_across) - 1), wk = wave >> a.log_across;
-    const int log_deep = kLogWaves - a.log_across, deep = 1 << log_deep;
+    const int log_deep = (WAVES == 16 ? 4 : 3) - a.log_across, deep = 1 << log_deep;
     const int m0 = blockIdx.y * a.rows, rows = min(a.rows, a.M - m0), of_c = rows_of_c(a.rows), plane = packed_plane(a.rows, a.chunk);
     float* sums = reinterpret_cast<float*>(lds + NP * plane);
     const int chunks = (a.parts + a.chunk - 1) / a.chunk;
 
-    // the next part of the wave: they are asked for in the order in which they are worked on, two ahead
+    // the next part of the wave: asked for as soon as the one before it has been worked on
     int ask_set = blockIdx.x, ask_chunk = 0, ask_turn = 0;
     auto ask = [&](PackedPiece<PER> (&to)[NS]) {
         const int part = min(ask_chunk * a.chunk + min((ask_turn << log_deep) + wk, a.chunk - 1), a.parts - 1);
@@ -146,9 +146,8 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
             if (++ask_chunk == chunks) { ask_chunk = 0; ask_set = min(ask_set + (int)gridDim.x, a.sets - 1); }   // (behind the end the last one once more)
         }
     };
-    PackedPiece<PER> piece[2][NS];
-    ask(piece[0]);
-    ask(piece[1]);
+    PackedPiece<PER> piece[NS];
+    ask(piece);
 
     f32x4 y[MT][NS];
     auto work = [&](const PackedPiece<PER> (&now)[NS], int part0, int p) {
@@ -191,7 +190,7 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
         }
     };
 
-    const int finishing = (MT * NT) << a.log_across;    // tiles of results, eight at most
+    const int finishing = (MT * NT) << a.log_across;    // tiles of results, no more than waves
     bool second = false;
     for (int set = blockIdx.x; set < a.sets; set += gridDim.x) {
 #pragma unroll
@@ -215,7 +214,7 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
             const int part0 = chunk * a.chunk, here = min(a.chunk, a.parts - part0);
             if (chunks > 1 || set == (int)blockIdx.x) {
                 __syncthreads();
-                for (int u = threadIdx.x; u < here * rows * 4; u += 64 * kPackedWaves) {
+                for (int u = threadIdx.x; u < here * rows * 4; u += 64 * WAVES) {
                     const int q = u >> 2, m = q % rows, p = q / rows, cc = u & 3;
                     float group = 0.f;
 #pragma unroll
@@ -242,12 +241,10 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
                 }
                 __syncthreads();
             }
-            for (int turn = 0; turn < a.turns; turn += 2) {
+            for (int turn = 0; turn < a.turns; ++turn) {
                 const int p = turn * deep + wk;
-                if (p < here) work(piece[0], part0, p);
-                ask(piece[0]);
-                if (p + deep < here) work(piece[1], part0, p + deep);
-                ask(piece[1]);
+                if (p < here) work(piece, part0, p);
+                ask(piece);
             }
         }
         auto finish = [&](f32x4 g, f32x4 u, int mt) {
@@ -258,7 +255,7 @@ __global__ void __launch_bounds__(64 * kPackedWaves) k_packed_rows(PackedArgs a)
             }
         };
         // waves that share inputs: their sums through LDS, each wave adds up a tile, in order
-        f32x4* join = reinterpret_cast<f32x4*>(lds + a.join_at + (second ? packed_join(MT, NS) : 0));
+        f32x4* join = reinterpret_cast<f32x4*>(lds + a.join_at + (second ? packed_join(WAVES, MT, NS) : 0));
         second = !second;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)

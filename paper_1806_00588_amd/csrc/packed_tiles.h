@@ -52,16 +52,17 @@ __global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, floa
 
 template <int TYPE, int MT, int NS> struct TilesPlan {     // MT: times 16 rows of a wave, a workgroup has twice that
     static constexpr int P = kRowPlanes<TYPE>;
-    static constexpr int KS = P == 1 || MT < 4 ? 2 : 1;              // times 32 inputs of a stage
+    static constexpr int KS = (P == 1 ? 2 : 1) * (MT < 4 ? 2 : 1);   // times 32 inputs of a stage
     static constexpr int kOf = 4 / KS;                               // stages of a part
-    static constexpr int kRing = P == 1 ? 5 : 4;                     // stages of rows in LDS, or on their way
+    static constexpr int kRing = P == 1 && MT == 4 ? 5 : 4;          // stages of rows in LDS, or on their way
+    static constexpr int kParts = (kRing - 2) / kOf + 2;             // parts of codes
     static constexpr int kRowsSlot = 2 * MT * KS * P * 1024;
     static constexpr int kRowsEach = 2 * MT * KS * P / kTileWaves;   // a wave's loads of rows
     static constexpr int kCodesEach = NS < 2 ? 1 : NS / 2;           // a wave's loads of codes
-    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kTileAcross * NS * 1024;         // parts: three
-    static constexpr int kScales = kCodes + 3 * kCodesSlot, kScalesSlot = kTileAcross * 768;
-    static constexpr int kSums = kScales + 3 * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? 2 * MT * 256 : 0;
-    static constexpr int kLds = kSums + 3 * kSumsSlot;
+    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kTileAcross * NS * 1024;
+    static constexpr int kScales = kCodes + kParts * kCodesSlot, kScalesSlot = kTileAcross * 768;
+    static constexpr int kSums = kScales + kParts * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? 2 * MT * 256 : 0;
+    static constexpr int kLds = kSums + kParts * kSumsSlot;
     static_assert(kLds <= (int)kMaxDynLds && kRowsEach * kTileWaves == 2 * MT * KS * P, "every wave asks for as much");
     // loads of a wave for the j-th stage of a part
     static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + 2 + kTileSums<TYPE> : 0); }
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
         if (++ask_in == OF) {                    // (behind the end the last part once more)
             ask_in = 0;
             ask_part = min(ask_part + 1, a.parts - 1);
-            ask_codes = ask_codes + 1 == 3 ? 0 : ask_codes + 1;
+            ask_codes = ask_codes + 1 == Plan::kParts ? 0 : ask_codes + 1;
         }
     };
     for (int i = 0; i < Plan::kRing - 1; ++i) ask();
@@ -256,7 +257,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             if (ks + 1 == KS) slot = slot + 1 == Plan::kRing ? 0 : slot + 1;
             if constexpr (PER < 4) __builtin_amdgcn_sched_barrier(0);   // (several groups' sums at once have no registers)
         }
-        codes_slot = codes_slot + 1 == 3 ? 0 : codes_slot + 1;
+        codes_slot = codes_slot + 1 == Plan::kParts ? 0 : codes_slot + 1;
     }
     wait_vmem<0>();                              // (nothing may come into another workgroup's LDS)
 #pragma unroll
