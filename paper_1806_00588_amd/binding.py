@@ -687,7 +687,7 @@ def cache_advance(cp: CacheParams, T: int, tables_in, lengths_in, tables_out, le
 def _rows(x, name, R, T, heads, D, dev):
     """lsh_rows of a tensor [R, T, heads, D] with any pitches."""
     t = _t().types.get(x.dtype)
-    if t is None or x.get_device() != dev or tuple(x.shape) != (R, T, heads, D):
+    if t is None or x.get_device() != dev or x.shape != (R, T, heads, D):
         raise ValueError(f"{name} must be {(R, T, heads, D)} on the current device, of {tuple(_t().types)}")
     row, token, head, one = x.stride()
     if one != 1:
@@ -777,7 +777,7 @@ class PackedWeights:
 def _matrix(x, name, shape, dev):
     """lsh_matrix of a tensor with contiguous rows."""
     t = _t().types.get(x.dtype)
-    if t is None or x.get_device() != dev or tuple(x.shape) != shape or (shape[1] > 1 and x.stride(1) != 1):
+    if t is None or x.get_device() != dev or x.shape != shape or (shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{name} must be {shape} with contiguous rows on the current device, of {tuple(_t().types)}")
     return _Matrix(t, x.stride(0) if shape[0] > 1 else shape[1])
 

@@ -301,7 +301,17 @@ lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const ls
             for_dims(p->k_dim, [&](auto nk) { ok = chunks_launch<kType, decltype(nk)::value>(p, a, w, static_cast<char*>(workspace_dev), st); });
             return;
         }
-        auto kernel = p->k_dim <= 64 ? k_delta_tokens<kType, 4> : p->k_dim <= 128 ? k_delta_tokens<kType, 8> : k_delta_tokens<kType, 16>;
+        const auto pick = [&](auto one) {
+            constexpr bool kOne = decltype(one)::value;
+            const int rows = p->k_dim / 16;
+            return rows <= 2   ? k_delta_tokens<kType, 2, kOne>
+                   : rows <= 4 ? k_delta_tokens<kType, 4, kOne>
+                   : rows <= 6 ? k_delta_tokens<kType, 6, kOne>
+                   : rows <= 8 ? k_delta_tokens<kType, 8, kOne>
+                   : rows <= 12 ? k_delta_tokens<kType, 12, kOne>
+                                : k_delta_tokens<kType, 16, kOne>;
+        };
+        auto kernel = p->T == 1 ? pick(std::true_type()) : pick(std::false_type());
         hipLaunchKernelGGL(kernel, dim3((unsigned)(delta_pairs(p) * a.slices)), dim3(256), 0, st, a);
     });
     if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
