@@ -60,20 +60,19 @@ __global__ void __launch_bounds__(256) k_packed_quantize(QuantArgs a) {
             for (int i = 0; i < 8; ++i) x[w][i] = row < a.N && k + i < a.K ? value_at<TYPE>(a.w, row * a.ld + k + i) : 0.f;
         }
     }
-    // smallest (with zeros), largest, and whether all is finite
+    // smallest (with zeros) and largest
     float lo[4], hi[4];
-    bool bad[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
+        float none = 0.f;                        // 0 times each: no 0 if one of them is not finite
         lo[w] = hi[w] = 0.f;
-        bad[w] = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             lo[w] = ZEROS ? fminf(lo[w], x[w][i]) : 0.f;
             hi[w] = fmaxf(hi[w], ZEROS ? x[w][i] : fabsf(x[w][i]));
-            bad[w] |= !(fabsf(x[w][i]) < INFINITY);
+            none = fmaf(x[w][i], 0.f, none);
         }
-        if (bad[w]) hi[w] = INFINITY;            // (says the same to the other lanes)
+        if (none != 0.f) hi[w] = INFINITY;       // (says the same to the other lanes)
         hi[w] = fmaxf(hi[w], dpp_f32<0xB1>(hi[w]));
         hi[w] = fmaxf(hi[w], dpp_f32<0x4E>(hi[w]));
         if (ZEROS) {
@@ -91,6 +90,7 @@ __global__ void __launch_bounds__(256) k_packed_quantize(QuantArgs a) {
         for (int w = 0; w < 4; ++w) { hi[w] = h[w]; lo[w] = l[w]; }
     }
     const int each = kPackInputs >> a.shift;
+    const bool edge = (tile + 1) * kPackOutputs > a.N || (part + 1) * kPackInputs > a.K;
     uint32_t words[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -109,24 +109,33 @@ __global__ void __launch_bounds__(256) k_packed_quantize(QuantArgs a) {
             zero = fminf(fmaxf(zero, 0.f), 15.f);
         }
         float q[8], off = 0.f;
+        if (f != 1.f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = x[w][i] * f * inv;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = x[w][i] * inv;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float at = x[w][i] * f * inv;
-            q[i] = rintf(at);
-            off = fmaxf(off, fabsf(at - q[i]));
+            const float whole = rintf(q[i]);
+            off = fmaxf(off, fabsf(q[i] - whole));
+            q[i] = whole;
         }
         if (off > 0.4999f && s > 0.f) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[i] = whole_near(x[w][i], s, q[i]);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __builtin_amdgcn_fmed3f(q[i] + zero, 0.f, 15.f);
+        if (edge || nan) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (nan || row >= a.N || part * kPackInputs + 32 * w + 8 * c + i >= a.K) q[i] = 0.f;
+        }
         uint32_t word = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t code = (uint32_t)fminf(fmaxf(q[i] + zero, 0.f), 15.f);
-            const int k = part * kPackInputs + 32 * w + 8 * c + i;
-            if (nan || row >= a.N || k >= a.K) code = 0;
-            word |= code << (8 * (i & 3) + 4 * (i >> 2));
-        }
+        for (int i = 0; i < 4; ++i) word = __builtin_amdgcn_cvt_pk_u8_f32(fmaf(q[i + 4], 16.f, q[i]), i, word);
         words[w] = word;
         const int per = 1 << (a.shift - 5);      // words of a group
         if (c == 0 && (w & (per - 1)) == 0) {
@@ -165,8 +174,18 @@ __global__ void __launch_bounds__(256) k_packed_values(QuantArgs a) {
         if (k + 8 <= a.K) {
             using T = typename WordOf<TYPE>::type;
             T t[8];
+            if constexpr (TYPE == kTypeBf16) {   // (nearest even, pairs at once)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) put_value<TYPE>(t, i, x[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 v = {x[2 * i], x[2 * i + 1]};
+                    const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+                    t[2 * i] = (T)(two & 0xffffu);
+                    t[2 * i + 1] = (T)(two >> 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) put_value<TYPE>(t, i, x[i]);
+            }
             T* to = static_cast<T*>(out) + row * a.ld + k;
 #pragma unroll
             for (int h = 0; h < (TYPE == kTypeF32 ? 2 : 1); ++h) {
