@@ -9,7 +9,7 @@ import numpy as np
 
 
 def place(n: int, k: int, parts: int):
-    """(byte, upper four bits?) of the code of output n, input k in an array of codes."""
+    """(byte, upper four bits?) of the code of output n, input k in an array of codes; numbers or arrays."""
     tile, part, c = n // 16, k // 128, k % 32 // 8
     word, i = k % 128 // 32, k % 8
     return ((((tile * parts + part) * 4 + c) * 16 + n % 16) * 4 + word) * 4 + i % 4, i >= 4
@@ -20,36 +20,29 @@ def pack(codes: np.ndarray) -> np.ndarray:
     N, K = codes.shape
     tiles, parts = -(-N // 16), -(-K // 128)
     out = np.zeros(tiles * parts * 1024, dtype=np.uint8)
-    for n in range(N):
-        for k in range(K):
-            at, upper = place(n, k, parts)
-            out[at] |= int(codes[n, k]) << (4 * upper)
+    at, upper = place(np.arange(N)[:, None], np.arange(K)[None, :], parts)
+    upper = np.broadcast_to(upper, at.shape)
+    out[at[~upper]] = codes[~upper]              # (no two in one place)
+    out[at[upper]] |= (codes[upper] << 4).astype(np.uint8)
     return out.reshape(tiles, parts, 4, 16, 16)
 
 
 def unpack(packed: np.ndarray, N: int, K: int) -> np.ndarray:
-    flat, parts = packed.reshape(-1), packed.shape[1]
-    out = np.empty((N, K), dtype=np.int64)
-    for n in range(N):
-        for k in range(K):
-            at, upper = place(n, k, parts)
-            out[n, k] = flat[at] >> (4 * upper) & 15
-    return out
+    at, upper = place(np.arange(N)[:, None], np.arange(K)[None, :], packed.shape[1])
+    return packed.reshape(-1)[at].astype(np.int64) >> 4 * upper & 15
 
 
 def of_groups(x: np.ndarray, to_shape, fill=0):
     """[N, groups] numbers as scales and zeros lie: [tiles, parts, 16, 128 / group]."""
-    tiles, parts, _, each = to_shape
     out = np.full(to_shape, fill, dtype=x.dtype)
-    for n in range(x.shape[0]):
-        for g in range(x.shape[1]):
-            out[n // 16, g // each, n % 16, g % each] = x[n, g]
+    n, g = np.arange(x.shape[0])[:, None], np.arange(x.shape[1])[None, :]
+    out[n // 16, g // to_shape[3], n % 16, g % to_shape[3]] = x
     return out
 
 
 def to_groups(x: np.ndarray, N: int, groups: int):
-    each = x.shape[3]
-    return np.array([[x[n // 16, g // each, n % 16, g % each] for g in range(groups)] for n in range(N)])
+    n, g = np.arange(N)[:, None], np.arange(groups)[None, :]
+    return x[n // 16, g // x.shape[3], n % 16, g % x.shape[3]]
 
 
 def quantize(w: np.ndarray, group: int, round16, zeros: bool):
