@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
 }
 
 // LDS of k_delta_chain: K S and Q S of each wave's rows of the state; V - e K S, U, and e^(c_last - c_j) U as operands.  OVER: U lies over the sums.
-template <int PA, bool OVER> struct ChainLds {
-    static constexpr int kR = 4 * 8 * 1024, kU = OVER ? 0 : kR + 2 * 3 * 1024, kLast = kU + 2 * PA * 1024;
-    static constexpr int kBytes = OVER ? kR + 2 * 3 * 1024 : kLast + 2 * 3 * 1024;
+template <int PA, bool OVER, int TILES> struct ChainLds {
+    static constexpr int kR = TILES * 4 * 8 * 1024, kU = OVER ? 0 : kR + TILES * 2 * 3 * 1024, kLast = kU + TILES * 2 * PA * 1024;
+    static constexpr int kBytes = OVER ? kR + TILES * 2 * 3 * 1024 : kLast + TILES * 2 * 3 * 1024;
 };
 
 // Planes of a tile's four values a lane: its half of the operand that two tiles make.
@@ -283,55 +283,64 @@ template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(co
             if (sum - i >= 0 && sum - i < PB) { acc[turn & 1] = mfma_bf16(a[i], b[sum - i], acc[turn & 1]); ++turn; }
 }
 
-// A workgroup of four waves for 16 columns of a row's and head's state.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what is made for
+// A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what is made for
 // tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight to
 // registers, and asked for a chunk ahead.  Bound by the chain of a chunk's instructions: 16 heads of 128 x 128, 8192 tokens TIME us a chunk.  (Four waves with
 // columns of their own, operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk.)
-// AHEAD: chunks that operands are asked for ahead, for which a workgroup has half a CU or a whole one; 0: when they are needed.
-template <int TYPE, int NK, int AHEAD>
-__global__ void __launch_bounds__(256, AHEAD ? 1 : 2) k_delta_chain(ChunkArgs ca) {
+// AHEAD: chunks that operands are asked for ahead, for which a workgroup has half a CU or a whole one; 0: when they are needed.  TILES: times 16 columns.
+template <int TYPE, int NK, int AHEAD, int TILES>
+__global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;
     constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4, SETS = AHEAD ? AHEAD : 1;
-    using Lds = ChainLds<PA, AHEAD == 0>;
+    constexpr bool OVER = TILES == 2;                      // (two workgroups a CU)
+    using Lds = ChainLds<PA, OVER, TILES>;
     __shared__ __align__(16) char lds[Lds::kBytes];
     const DeltaArgs& a = ca.d;
     // workgroups go round the eight XCDs one by one: those of a pair follow each other on one of them, so that its operands come from there but once
-    const unsigned tiles = (unsigned)a.Dv >> 4, on_xcd = blockIdx.x >> 3;
+    const unsigned tiles = (((unsigned)a.Dv >> 4) + TILES - 1) / TILES, on_xcd = blockIdx.x >> 3;
     const int64_t local = (int64_t)(on_xcd / tiles) * 8 + (blockIdx.x & 7), pair = ca.pair0 + local;
-    const int tile = (int)(on_xcd % tiles);
+    const int tile = (int)(on_xcd % tiles) * TILES;
     if (local >= ca.pairs) return;
     const int r = (int)(pair / a.heads), h = (int)(pair - (int64_t)r * a.heads);
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), c = ln >> 4, n = ln & 15;
     const int n_new = delta_new(a, r), begin = ca.chunk0 * kChunk;
     const int chunks = min(ca.chunks, (n_new - begin + kChunk - 1) / kChunk);
     if (!ca.first && chunks <= 0) return;
-    const int col = 16 * tile + n;
+    int col[TILES];            // (tiles behind the last: the last one once more, without results)
+    bool live[TILES];
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) {
+        live[k] = 16 * (tile + k) < a.Dv;
+        col[k] = min(16 * (tile + k), a.Dv - 16) + n;
+    }
     const int64_t size = (int64_t)a.Dk * a.Dv;
 
-    f32x4 S[MINE][2];
+    f32x4 S[TILES][MINE][2];
     const int parent = delta_parent(a, r);
     const float* from = ca.first ? a.state_in + (parent < 0 ? 0 : ((int64_t)parent * a.heads + h) * size) : a.state_out + pair * size;
     const bool any = !ca.first || parent >= 0;
 #pragma unroll
-    for (int j = 0; j < MINE; ++j)
+    for (int k = 0; k < TILES; ++k)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int j = 0; j < MINE; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
-                S[j][t][i] = any && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
-            }
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                    S[k][j][t][i] = any && d < a.Dk ? from[(int64_t)d * a.Dv + col[k]] : 0.f;
+                }
 
     // Operands.  What a wave has no work for it asks for all the same (another's): the number of loads under way is known to the compiler then.
     struct Operands {
         uint4 kq[MINE][8][P], kt[MINE][4][P], tp[2][3], ap[2][PA];
         f32x4 e, last;
         float all;
-        typename WordOf<TYPE>::type v[4];
+        typename WordOf<TYPE>::type v[TILES][4];
     } sets[SETS];
-    const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes + 16 * ln;
-    const int64_t v_from = r * a.vp.row + h * a.vp.head + col;
-    auto block = [&](int chunk, int b) { return *reinterpret_cast<const uint4*>(room + (size_t)chunk * ca.bytes + (size_t)b * 1024); };
+    const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes;       // (the same for all lanes, and stays in scalar registers)
+    const int64_t v_from = r * a.vp.row + h * a.vp.head;
+    auto block = [&](int chunk, int b) { return reinterpret_cast<const uint4*>(room + (size_t)chunk * ca.bytes + (size_t)b * 1024)[(unsigned)ln]; };
     auto ask_kq = [&](Operands& to, int chunk) {
 #pragma unroll
         for (int j = 0; j < MINE; ++j)
@@ -341,14 +350,15 @@ __global__ void __launch_bounds__(256, AHEAD ? 1 : 2) k_delta_chain(ChunkArgs ca
                 for (int p = 0; p < P; ++p) to.kq[j][i][p] = block(chunk, (min(wave + 4 * j, NK - 1) * 8 + i) * P + p);
     };
     auto ask_values = [&](Operands& to, int chunk) {
-        const float* scalars = reinterpret_cast<const float*>(room - 16 * ln + (size_t)chunk * ca.bytes + Plan::kScalars * 1024);
+        const float* scalars = reinterpret_cast<const float*>(room + (size_t)chunk * ca.bytes + Plan::kScalars * 1024);
         to.e = *reinterpret_cast<const f32x4*>(scalars + row_of(wave, 4 * c));
         to.last = *reinterpret_cast<const f32x4*>(scalars + 64 + row_of(wave, 4 * c));
         to.all = scalars[63];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                                        // (tokens behind the last count as if they were it: T has zeros there)
             const int token = min(begin + chunk * kChunk + row_of(wave, 4 * c + i), n_new - 1);
-            to.v[i] = static_cast<const typename WordOf<TYPE>::type*>(a.v)[v_from + token * a.vp.token];
+#pragma unroll
+            for (int k = 0; k < TILES; ++k) to.v[k][i] = static_cast<const typename WordOf<TYPE>::type*>(a.v)[v_from + token * a.vp.token + col[k]];
         }
     };
     auto ask_t = [&](Operands& to, int chunk) {
@@ -386,99 +396,126 @@ __global__ void __launch_bounds__(256, AHEAD ? 1 : 2) k_delta_chain(ChunkArgs ca
         const int after = min(chunk + AHEAD, chunks - 1);                    // (behind the end the last chunk once more)
         if constexpr (!AHEAD) { ask_kq(of, chunk); ask_values(of, chunk); }
         // K S and Q S: of the wave's rows of the state
-        f32x4 ks[4] = {none, none, none, none}, qs[4] = {none, none, none, none};
+        f32x4 ks[TILES][4], qs[TILES][4];
+#pragma unroll
+        for (int k = 0; k < TILES; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) ks[k][t] = qs[k][t] = none;
 #pragma unroll
         for (int j = 0; j < MINE; ++j)
             if (wave + 4 * j < NK) {
-                float x[8];
-                uint4 sp[3], op[4][P];
+                uint4 op[2][4][P];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = S[j][i >> 2][i & 3];
-                planes_of<3>(x, sp);
+                for (int t = 0; t < 8; ++t)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+                    for (int p = 0; p < P; ++p) op[t >> 2][t & 3][p] = of.kq[j][t][p];
 #pragma unroll
-                    for (int p = 0; p < P; ++p) op[t][p] = of.kq[j][t][p];
-                mfma_planes<3>(op, sp, ks);
+                for (int k = 0; k < TILES; ++k) {
+                    float x[8];
+                    uint4 sp[3];
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int p = 0; p < P; ++p) op[t][p] = of.kq[j][4 + t][p];
-                mfma_planes<ORDER>(op, sp, qs);
+                    for (int i = 0; i < 8; ++i) x[i] = S[k][j][i >> 2][i & 3];
+                    planes_of<3>(x, sp);
+                    mfma_planes<3>(op[0], sp, ks[k]);
+                    mfma_planes<ORDER>(op[1], sp, qs[k]);
+                }
             }
         if constexpr (AHEAD) ask_kq(of, after);
         else ask_t(of, chunk);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) { part[(wave * 8 + t) * 64 + ln] = ks[t]; part[(wave * 8 + 4 + t) * 64 + ln] = qs[t]; }
+        for (int k = 0; k < TILES; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) { part[((k * 4 + wave) * 8 + t) * 64 + ln] = ks[k][t]; part[((k * 4 + wave) * 8 + 4 + t) * 64 + ln] = qs[k][t]; }
         lds_barrier();
         // V - e K S of the wave's tile of tokens
-        f32x4 k_sum = none, q_sum = none, v;
+        f32x4 q_sum[TILES];
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (w < NK) k_sum += part[(w * 8 + wave) * 64 + ln];
+        for (int k = 0; k < TILES; ++k) {
+            f32x4 k_sum = none, v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[i]));
-        put_half<3>(lds + Lds::kR, wave, v);
+            for (int w = 0; w < 4; ++w)
+                if (w < NK) k_sum += part[((k * 4 + w) * 8 + wave) * 64 + ln];
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (w < NK) q_sum += part[(w * 8 + 4 + wave) * 64 + ln];
-        q_sum *= of.e;
+            for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[k][i]));
+            put_half<3>(lds + Lds::kR + k * (2 * 3 * 1024), wave, v);
+            q_sum[k] = none;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                if (w < NK) q_sum[k] += part[((k * 4 + w) * 8 + 4 + wave) * 64 + ln];
+            q_sum[k] *= of.e;
+        }
         lds_barrier();
         // U = T (V - e K S)
-        f32x4 two[2] = {none, none};
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (s <= wave >> 1) {
-                const uint4 rp[3] = {read(Lds::kR, 3 * s), read(Lds::kR, 3 * s + 1), read(Lds::kR, 3 * s + 2)};
-                mfma_two<3>(of.tp[s], rp, two);
-            }
+        for (int k = 0; k < TILES; ++k) {
+            f32x4 two[2] = {none, none};
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s <= wave >> 1) {
+                    const int at = Lds::kR + k * (2 * 3 * 1024);
+                    const uint4 rp[3] = {read(at, 3 * s), read(at, 3 * s + 1), read(at, 3 * s + 2)};
+                    mfma_two<3>(of.tp[s], rp, two);
+                }
+            const f32x4 u = two[0] + two[1];
+            put_half<PA>(lds + Lds::kU + k * (2 * PA * 1024), wave, u);
+            put_half<3>(lds + Lds::kLast + k * (2 * 3 * 1024), wave, u * of.last);
+        }
         if constexpr (AHEAD) ask_t(of, after);
         else { ask_a(of, chunk); ask_kt(of, chunk); }
-        const f32x4 u = two[0] + two[1];
-        put_half<PA>(lds + Lds::kU, wave, u);
-        put_half<3>(lds + Lds::kLast, wave, u * of.last);
         const float decay = of.all;
         if constexpr (AHEAD) ask_values(of, after);
         lds_barrier();
         // the state
-        uint4 lp[2][3];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int k = 0; k < TILES; ++k) {
+            uint4 lp[2][3];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) lp[s][p] = read(Lds::kLast, 3 * s + p);
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int j = 0; j < MINE; ++j)
-            if (wave + 4 * j < NK) {
-                S[j][0] *= decay;
-                S[j][1] *= decay;
+                for (int p = 0; p < 3; ++p) lp[s][p] = read(Lds::kLast + k * (2 * 3 * 1024), 3 * s + p);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    uint4 op[2][P];
+            for (int j = 0; j < MINE; ++j)
+                if (wave + 4 * j < NK) {
+                    S[k][j][0] *= decay;
+                    S[k][j][1] *= decay;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                    for (int s = 0; s < 2; ++s) {
+                        uint4 op[2][P];
 #pragma unroll
-                        for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
-                    mfma_planes<3>(op, lp[s], S[j]);
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
+                        mfma_planes<3>(op, lp[s], S[k][j]);
+                    }
                 }
-            }
+        }
         if constexpr (AHEAD) ask_kt(of, after);
         // out = scale (e Q S + A U)
-        two[0] = q_sum;
-        two[1] = none;
+        f32x4 o[TILES][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (s <= wave >> 1) {
-                uint4 up[PA];
+        for (int k = 0; k < TILES; ++k) {
+            o[k][0] = q_sum[k];
+            o[k][1] = none;
 #pragma unroll
-                for (int p = 0; p < PA; ++p) up[p] = read(Lds::kU, PA * s + p);
-                mfma_two<ORDER>(of.ap[s], up, two);
-            }
+            for (int s = 0; s < 2; ++s)
+                if (s <= wave >> 1) {
+                    uint4 up[PA];
+#pragma unroll
+                    for (int p = 0; p < PA; ++p) up[p] = read(Lds::kU + k * (2 * PA * 1024), PA * s + p);
+                    mfma_two<ORDER>(of.ap[s], up, o[k]);
+                }
+        }
         if constexpr (AHEAD) ask_a(of, after);
-        else lds_barrier();                                                  // (the next sums go where U is)
+        if constexpr (OVER) lds_barrier();                                   // (the next sums go where U is)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int token = begin + chunk * kChunk + row_of(wave, 4 * c + i);
-            if (token < n_new) put_value<TYPE>(a.out, r * a.op.row + (int64_t)token * a.op.token + h * a.op.head + col, a.scale * (two[0][i] + two[1][i]));
+            if (token < n_new) {
+                const int64_t at = r * a.op.row + (int64_t)token * a.op.token + h * a.op.head;
+#pragma unroll
+                for (int k = 0; k < TILES; ++k)
+                    if (live[k]) put_value<TYPE>(a.out, at + col[k], a.scale * (o[k][0][i] + o[k][1][i]));
+            }
         }
     };
     for (int chunk = 0; chunk < chunks; chunk += SETS) {
@@ -489,14 +526,16 @@ __global__ void __launch_bounds__(256, AHEAD ? 1 : 2) k_delta_chain(ChunkArgs ca
     }
     float* to = a.state_out + pair * size;
 #pragma unroll
-    for (int j = 0; j < MINE; ++j)
+    for (int k = 0; k < TILES; ++k)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int j = 0; j < MINE; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
-                if (d < a.Dk) to[(int64_t)d * a.Dv + col] = S[j][t][i];
-            }
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                    if (live[k] && d < a.Dk) to[(int64_t)d * a.Dv + col[k]] = S[k][j][t][i];
+                }
 }
 
 }  // namespace lshbeam

@@ -80,10 +80,10 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     return w;
 }
 
-// More rows: 64 or 128 of them and 64, 128 or 256 outputs a workgroup, whatever makes the least work of the rounds of 256 workgroups (a part of 64 x 256
-// results some 1000 cycles on the matrix cores, and some 500 for the rest of it).
+// More rows: 64 or 128 of them and 64, 128 or 256 outputs a workgroup, whatever makes the least work of the rounds of 256 workgroups.
 struct TilesLaunch {
-    int wave_rows, streams, row_tiles, row_groups;   // wave_rows: times 16
+    bool deep;                 // 64 rows
+    int streams, row_tiles, row_groups;
     int64_t sets;
     size_t rows, room;         // the rows as operands; and their groups' sums
 };
@@ -91,13 +91,14 @@ bool takes_tiles(int32_t M) { return M > kFewRows; }
 TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     TilesLaunch w{};
     w.row_tiles = (int)ceil_div(M, 16);
+    // (a part of 16 x 16 results of a wave some 16 ns on the matrix cores and beside them, of three planes 48; 250 for the rest of it)
     int64_t best = INT64_MAX;
-    for (int rows = 4; rows >= 2; rows -= 2)
-        for (int streams = 4; streams >= (gated || rows == 4 ? 2 : 1); streams /= 2) {
-            if (rows * streams == 16 && p->group == 32) continue;     // (four groups of a part: no registers for them)
-            const int64_t groups = ceil_div(w.row_tiles, 2 * rows), sets = ceil_div(tiles_of(p), kTileAcross * (gated ? streams / 2 : streams));
-            const int64_t cost = ceil_div(groups * sets, 256) * (rows * streams * (dtype == LSH_F32 ? 3 : 1) * 125 + 500);
-            if (cost < best) { best = cost; w.wave_rows = rows; w.streams = streams; w.row_groups = (int)groups; w.sets = sets; }
+    for (int deep = 0; deep < 2; ++deep)
+        for (int streams = 4; streams >= (gated || !deep ? 2 : 1); streams /= 2) {
+            if (streams == 4 && (deep || p->group == 32)) continue;     // (no LDS for twice as many codes; no registers for four groups of a part)
+            const int64_t groups = ceil_div(w.row_tiles, deep ? 4 : 8), sets = ceil_div(tiles_of(p), kTileAcross * (gated ? streams / 2 : streams));
+            const int64_t cost = ceil_div(groups * sets, 256) * (4 * streams * (dtype == LSH_F32 ? 48 : 16) + 250) / (deep ? 2 : 1);
+            if (cost < best) { best = cost; w.deep = deep != 0; w.streams = streams; w.row_groups = (int)groups; w.sets = sets; }
         }
     const size_t units = (size_t)w.row_tiles * parts_of(p);
     w.rows = units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
@@ -134,7 +135,7 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     if (many) {
         char* room = static_cast<char*>(workspace_dev);
         const TilesArgs t{a, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
-        ok = launch_packed_tiles(x->dtype, tiles.wave_rows, tiles.streams, gated, t, st);
+        ok = launch_packed_tiles(x->dtype, tiles.deep, tiles.streams, gated, t, st);
     } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups), w.lds, st);
     if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
     return ok ? launched() : LSH_ERR_HIP;
@@ -194,10 +195,10 @@ template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const 
             a.chunks = std::min(w.chunks, all - chunk);
             a.first = chunk == 0;
             if (!launch_room<k_delta_prepare<TYPE, NK>>(dim3((unsigned)(pairs * a.chunks)), 256, kPrepareLds<TYPE, NK>, st, a)) return false;
-            const unsigned grid = (unsigned)(ceil_div(pairs, 8) * 8 * (p->v_dim / 16));
+            const auto grid = [&](int tiles) { return dim3((unsigned)(ceil_div(pairs, 8) * 8 * ceil_div(p->v_dim / 16, tiles))); };
             constexpr int kAhead = (NK + 3) / 4 * ChunkPlan<TYPE, NK>::P <= 2 ? 2 : 1;       // (what there are registers for)
-            if (grid <= 512) hipLaunchKernelGGL((k_delta_chain<TYPE, NK, kAhead>), dim3(grid), dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0>), dim3(grid), dim3(256), 0, st, a);
+            if (grid(1).x <= 512) hipLaunchKernelGGL((k_delta_chain<TYPE, NK, kAhead, 1>), grid(1), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0, 2>), grid(2), dim3(256), 0, st, a);
         }
     }
     return true;

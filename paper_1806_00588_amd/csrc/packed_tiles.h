@@ -3,7 +3,8 @@
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
 // blocks of 1 KB, straight to LDS.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
 // converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
-// that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.
+// that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.  Up to 64 rows: the two waves with the same
+// outputs take turns with the parts instead of sharing the rows, so that no weight is converted twice, and add up at the end.
 // (128 x 64 and four waves, with accumulators in the other 256, which only the matrix instructions reach: 2048 x 8192 x 8192 in fp16 541 us, moves being
 // most of it.)
 #pragma once
@@ -50,22 +51,27 @@ __global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, floa
     }
 }
 
-template <int TYPE, int MT, int NS> struct TilesPlan {     // MT: times 16 rows of a wave, a workgroup has twice that
+// MT: times 16 rows of a wave; NS: its tiles of outputs; DEEP: the two waves with the same outputs have the same rows and every second part, else other
+// rows and the same parts.
+template <int TYPE, int MT, int NS, bool DEEP> struct TilesPlan {
     static constexpr int P = kRowPlanes<TYPE>;
-    static constexpr int KS = (P == 1 ? 2 : 1) * (MT < 4 ? 2 : 1);   // times 32 inputs of a stage
+    static constexpr int kHalves = DEEP ? 2 : 1, kRows = DEEP ? MT : 2 * MT;             // parts at a time; times 16 rows of a workgroup
+    static constexpr int KS = P == 1 ? 2 : 1;                        // times 32 inputs of a stage
     static constexpr int kOf = 4 / KS;                               // stages of a part
-    static constexpr int kRing = P == 1 && MT == 4 ? 5 : 4;          // stages of rows in LDS, or on their way
-    static constexpr int kParts = (kRing - 2) / kOf + 2;             // parts of codes
-    static constexpr int kRowsSlot = 2 * MT * KS * P * 1024;
-    static constexpr int kRowsEach = 2 * MT * KS * P / kTileWaves;   // a wave's loads of rows
-    static constexpr int kCodesEach = NS < 2 ? 1 : NS / 2;           // a wave's loads of codes
-    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kTileAcross * NS * 1024;
-    static constexpr int kScales = kCodes + kParts * kCodesSlot, kScalesSlot = kTileAcross * 768;
-    static constexpr int kSums = kScales + kParts * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? 2 * MT * 256 : 0;
+    static constexpr int kRing = P == 1 ? 5 : 4;                     // stages of rows in LDS, or on their way
+    static constexpr int kParts = (kRing - 2) / kOf + 2;             // turns of codes
+    static constexpr int kRowsSlot = kHalves * kRows * KS * P * 1024;
+    static constexpr int kRowsEach = kRowsSlot / 1024 / kTileWaves;  // a wave's loads of rows
+    static constexpr int kCodesOf = kTileAcross * NS * kHalves, kCodesEach = kCodesOf < kTileWaves ? 1 : kCodesOf / kTileWaves;   // blocks of codes; a wave's loads
+    static constexpr int kScalesEach = DEEP ? 3 : 2;
+    static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kCodesOf * 1024;
+    static constexpr int kScales = kCodes + kParts * kCodesSlot, kScalesSlot = kTileAcross * kHalves * 768;
+    static constexpr int kSums = kScales + kParts * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? kTileWaves * 256 : 0;
     static constexpr int kLds = kSums + kParts * kSumsSlot;
-    static_assert(kLds <= (int)kMaxDynLds && kRowsEach * kTileWaves == 2 * MT * KS * P, "every wave asks for as much");
-    // loads of a wave for the j-th stage of a part
-    static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + 2 + kTileSums<TYPE> : 0); }
+    static_assert(kLds <= (int)kMaxDynLds && kRowsEach * kTileWaves * 1024 == kRowsSlot && kHalves * kRows == kTileWaves, "every wave asks for as much");
+    static_assert(!DEEP || kTileAcross * MT * NS * 1024 <= kCodes, "the sums of one half have room");
+    // loads of a wave for the j-th stage of a turn
+    static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + kScalesEach + kTileSums<TYPE> : 0); }
     // ... that may be under way when stage j begins: all but those for it and the next one
     static constexpr int later(int j) {
         int n = 0;
@@ -107,72 +113,86 @@ struct TilesArgs {
 };
 
 // NS: tiles of 16 outputs of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
-template <int TYPE, int MT, int NS, int PER, bool GATED>
+template <int TYPE, int MT, int NS, int PER, bool GATED, bool DEEP>
 __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t) {
-    using Plan = TilesPlan<TYPE, MT, NS>;
-    constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS, EACH = 4 / PER;
+    using Plan = TilesPlan<TYPE, MT, NS, DEEP>;
+    constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS, EACH = 4 / PER, HALVES = Plan::kHalves;
     constexpr bool SUMS = kTileSums<TYPE>;
     extern __shared__ __align__(16) char lds[];
     const PackedArgs& a = t.p;
-    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), wn = wave % kTileAcross, wm = wave / kTileAcross;
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), wn = wave % kTileAcross, wm = DEEP ? 0 : wave / kTileAcross, wk = DEEP ? wave / kTileAcross : 0;
     // workgroups go round the eight XCDs one by one; an XCD gets neighbouring ones: four along the outputs, then along the rows
     const int total = t.row_groups * t.sets, each_xcd = (total + 7) / 8;
     const int u = (int)(blockIdx.x & 7) * each_xcd + (int)(blockIdx.x >> 3);
     if (u >= total || (int)(blockIdx.x >> 3) >= each_xcd) return;
     const int band = u / (4 * t.row_groups), wide = min(4, t.sets - 4 * band), in_band = u - band * 4 * t.row_groups;
     const int group = in_band / wide, set = 4 * band + in_band % wide;
-    const int tile0 = (set * kTileAcross + wn) * NT, mt0 = group * 2 * MT;
+    const int tile0 = (set * kTileAcross + wn) * NT, mt0 = group * Plan::kRows;
     // stream s of the waves with outputs w: matrix, tile's first part
     auto unit_of = [&](int w, int s) { return (int64_t)min((set * kTileAcross + w) * NT + (GATED ? s >> 1 : s), a.tiles - 1) * a.parts; };
 
+    // (what is asked for of a half's part: from the part's place on)
     const char* rows_from[Plan::kRowsEach];      // of 16 rows those of a stage lie side by side
+    const char* codes_from[Plan::kCodesEach];
+    int rows_half[Plan::kRowsEach], codes_half[Plan::kCodesEach];
 #pragma unroll
     for (int i = 0; i < Plan::kRowsEach; ++i) {
-        const int b = wave * Plan::kRowsEach + i;
-        rows_from[i] = t.x + (int64_t)min(mt0 + b / (KS * P), t.row_tiles - 1) * a.parts * (4 * P * 1024) + b % (KS * P) * 1024 + 16 * ln;
+        const int b = wave * Plan::kRowsEach + i, mt = b / (KS * P);
+        rows_half[i] = mt / Plan::kRows;
+        rows_from[i] = t.x + (int64_t)min(mt0 + mt % Plan::kRows, t.row_tiles - 1) * a.parts * (4 * P * 1024) + b % (KS * P) * 1024 + 16 * ln;
     }
-    const char* sums_from = t.sums + (int64_t)min(mt0 + wave % (2 * MT), t.row_tiles - 1) * a.parts * (EACH * 64) + 4 * min(ln, EACH * 16 - 1);
-    const char* codes_from[Plan::kCodesEach];
 #pragma unroll
     for (int i = 0; i < Plan::kCodesEach; ++i) {
-        const int s = (wave * Plan::kCodesEach + i) % (kTileAcross * NS);
-        codes_from[i] = reinterpret_cast<const char*>(a.w[GATED ? s & 1 : 0].codes) + unit_of(s / NS, s % NS) * kPackBytes + 16 * ln;
+        const int s = (wave * Plan::kCodesEach + i) % Plan::kCodesOf, of = s % (kTileAcross * NS);
+        codes_half[i] = s / (kTileAcross * NS);
+        codes_from[i] = reinterpret_cast<const char*>(a.w[GATED ? of & 1 : 0].codes) + unit_of(of / NS, of % NS) * kPackBytes + 16 * ln;
     }
-    // scales (the first four waves) and zeros of the wave's streams, 4 bytes a lane: 16 lanes a stream, scales twice that
+    const int sums_half = wave / Plan::kRows % HALVES;
+    const char* sums_from = t.sums + (int64_t)min(mt0 + wave % Plan::kRows, t.row_tiles - 1) * a.parts * (EACH * 64) + 4 * min(ln, EACH * 16 - 1);
+    // scales and zeros of the wave's streams, 4 bytes a lane: 16 lanes a stream, scales twice that.  Waves with the same part share the work: the first
+    // four ask for the scales, the others for the zeros
     const int mine = min(ln >> 4, NS - 1);
     const PackedRef& my = a.w[GATED ? mine & 1 : 0];
-    const char* scales_from[2];
-    int scales_step;
+    const char* scales_from[3];
+    int scales_step[3];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (wm == 0 || !my.zeros) {
-            scales_step = 32 * EACH;
-            scales_from[i] = reinterpret_cast<const char*>(my.scales) + unit_of(wn, mine) * scales_step + 4 * min((ln & 15) + 16 * i, 8 * EACH - 1);
+    for (int i = 0; i < 3; ++i) {
+        if (i < 2 || !my.zeros) {
+            scales_step[i] = 32 * EACH;
+            scales_from[i] = reinterpret_cast<const char*>(my.scales) + unit_of(wn, mine) * scales_step[i] + 4 * min((ln & 15) + 16 * (i & 1), 8 * EACH - 1);
         } else {
-            scales_step = 16 * EACH;
-            scales_from[i] = reinterpret_cast<const char*>(my.zeros) + unit_of(wn, mine) * scales_step + 4 * min(ln & 15, 4 * EACH - 1);
+            scales_step[i] = 16 * EACH;
+            scales_from[i] = reinterpret_cast<const char*>(my.zeros) + unit_of(wn, mine) * scales_step[i] + 4 * min(ln & 15, 4 * EACH - 1);
         }
     }
 
-    int ask_part = 0, ask_in = 0, ask_slot = 0, ask_codes = 0;
+    const int turns = (a.parts + HALVES - 1) / HALVES;
+    int ask_turn = 0, ask_in = 0, ask_slot = 0, ask_codes = 0;
+    auto part_of = [&](int half) { return (int64_t)min(ask_turn * HALVES + half, a.parts - 1); };
     auto ask = [&]() {
 #pragma unroll
         for (int i = 0; i < Plan::kRowsEach; ++i)
-            load_to_lds16(rows_from[i] + ((int64_t)ask_part * 4 + ask_in * KS) * (P * 1024), lds + ask_slot * Plan::kRowsSlot + (wave * Plan::kRowsEach + i) * 1024);
+            load_to_lds16(rows_from[i] + (part_of(rows_half[i]) * 4 + ask_in * KS) * (P * 1024), lds + ask_slot * Plan::kRowsSlot + (wave * Plan::kRowsEach + i) * 1024);
         if (ask_in == 0) {
 #pragma unroll
             for (int i = 0; i < Plan::kCodesEach; ++i)
-                load_to_lds16(codes_from[i] + (int64_t)ask_part * kPackBytes,
-                              lds + Plan::kCodes + ask_codes * Plan::kCodesSlot + (wave * Plan::kCodesEach + i) % (kTileAcross * NS) * 1024);
-            char* to = lds + Plan::kScales + ask_codes * Plan::kScalesSlot + wn * 768 + wm * 512;
-            load_to_lds4(scales_from[0] + (int64_t)ask_part * scales_step, to);
-            load_to_lds4(scales_from[1] + (int64_t)ask_part * scales_step, to + (wm == 0 ? 256 : 0));
-            if constexpr (SUMS) load_to_lds4(sums_from + (int64_t)ask_part * (EACH * 64), lds + Plan::kSums + ask_codes * Plan::kSumsSlot + wave % (2 * MT) * 256);
+                load_to_lds16(codes_from[i] + part_of(codes_half[i]) * kPackBytes,
+                              lds + Plan::kCodes + ask_codes * Plan::kCodesSlot + (wave * Plan::kCodesEach + i) % Plan::kCodesOf * 1024);
+            char* to = lds + Plan::kScales + ask_codes * Plan::kScalesSlot + (wk * kTileAcross + wn) * 768;
+            if (DEEP || wm == 0) {
+                load_to_lds4(scales_from[0] + part_of(wk) * scales_step[0], to);
+                load_to_lds4(scales_from[1] + part_of(wk) * scales_step[1], to + 256);
+            } else {
+                load_to_lds4(scales_from[2] + part_of(wk) * scales_step[2], to + 512);
+                load_to_lds4(scales_from[2] + part_of(wk) * scales_step[2], to + 512);   // (as many loads as the other waves')
+            }
+            if constexpr (DEEP) load_to_lds4(scales_from[2] + part_of(wk) * scales_step[2], to + 512);
+            if constexpr (SUMS) load_to_lds4(sums_from + part_of(sums_half) * (EACH * 64), lds + Plan::kSums + ask_codes * Plan::kSumsSlot + wave * 256);
         }
         ask_slot = ask_slot + 1 == Plan::kRing ? 0 : ask_slot + 1;
         if (++ask_in == OF) {                    // (behind the end the last part once more)
             ask_in = 0;
-            ask_part = min(ask_part + 1, a.parts - 1);
+            ask_turn = min(ask_turn + 1, turns - 1);
             ask_codes = ask_codes + 1 == Plan::kParts ? 0 : ask_codes + 1;
         }
     };
@@ -190,15 +210,16 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int p = 0; p < P; ++p) to[m][p] = *reinterpret_cast<const uint4*>(lds + of * Plan::kRowsSlot + (((wm * MT + m) * KS + ks) * P + p) * 1024 + 16 * ln);
+            for (int p = 0; p < P; ++p) to[m][p] = *reinterpret_cast<const uint4*>(lds + of * Plan::kRowsSlot + ((((wk * Plan::kRows + wm * MT + m) * KS + ks) * P + p) * 1024) + 16 * ln);
     };
     wait_vmem<Plan::later(-1)>();
     lds_barrier();
     if constexpr (AHEAD) read_rows(x[0], 0, 0);
-    for (int part = 0; part < a.parts; ++part) {
+    for (int turn = 0; turn < turns; ++turn) {
+        const int part = turn * HALVES + wk;
         uint4 codes[NS];
         float scale[NS], zero[NS];
-        const char* sc = lds + Plan::kScales + codes_slot * Plan::kScalesSlot + wn * 768;
+        const char* sc = lds + Plan::kScales + codes_slot * Plan::kScalesSlot + (wk * kTileAcross + wn) * 768;
 #pragma unroll
         for (int ks4 = 0; ks4 < 4; ++ks4) {
             const int j = ks4 / KS, ks = ks4 % KS, g = ks4 / PER;
@@ -212,7 +233,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             }
             if (ks4 == 0) {
 #pragma unroll
-                for (int s = 0; s < NS; ++s) codes[s] = *reinterpret_cast<const uint4*>(lds + Plan::kCodes + codes_slot * Plan::kCodesSlot + (wn * NS + s) * 1024 + 16 * ln);
+                for (int s = 0; s < NS; ++s) codes[s] = *reinterpret_cast<const uint4*>(lds + Plan::kCodes + codes_slot * Plan::kCodesSlot + ((wk * kTileAcross + wn) * NS + s) * 1024 + 16 * ln);
             }
             if (ks4 % PER == 0) {
 #pragma unroll
@@ -243,7 +264,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
                 if constexpr (SUMS) {
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
-                        X[m] = *reinterpret_cast<const f32x4*>(lds + Plan::kSums + codes_slot * Plan::kSumsSlot + (wm * MT + m) * 256 + g * 64 + 16 * (ln >> 4));
+                        X[m] = *reinterpret_cast<const f32x4*>(lds + Plan::kSums + codes_slot * Plan::kSumsSlot + (wk * Plan::kRows + wm * MT + m) * 256 + g * 64 + 16 * (ln >> 4));
                 }
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
@@ -260,6 +281,21 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
         codes_slot = codes_slot + 1 == Plan::kParts ? 0 : codes_slot + 1;
     }
     wait_vmem<0>();                              // (nothing may come into another workgroup's LDS)
+    if constexpr (DEEP) {                        // the second half's sums to the first
+        lds_barrier();
+        f32x4* join = reinterpret_cast<f32x4*>(lds) + wn * MT * NS * 64 + ln;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                if (wk == 1) join[(m * NS + s) * 64] = y[m][s];
+        lds_barrier();
+        if (wk == 1) return;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) y[m][s] += join[(m * NS + s) * 64];
+    }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll

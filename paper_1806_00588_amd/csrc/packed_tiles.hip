@@ -7,33 +7,35 @@
 namespace lshbeam {
 namespace {
 
-template <int TYPE, int MT, int NS, bool GATED> bool launch(const TilesArgs& a, hipStream_t st) {
+template <int TYPE, int NS, bool GATED, bool DEEP> bool launch(const TilesArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)((a.row_groups * (int64_t)a.sets + 7) / 8 * 8));
-    constexpr size_t lds = TilesPlan<TYPE, MT, NS>::kLds;
-    if constexpr (MT * NS < 16) {
-        if (a.p.shift == 5) return launch_room<k_packed_tiles<TYPE, MT, NS, 1, GATED>>(grid, 64 * kTileWaves, lds, st, a);
+    constexpr size_t lds = TilesPlan<TYPE, 4, NS, DEEP>::kLds;
+    if constexpr (NS < 4) {
+        if (a.p.shift == 5) return launch_room<k_packed_tiles<TYPE, 4, NS, 1, GATED, DEEP>>(grid, 64 * kTileWaves, lds, st, a);
     }
-    if (a.p.shift == 6) return launch_room<k_packed_tiles<TYPE, MT, NS, 2, GATED>>(grid, 64 * kTileWaves, lds, st, a);
-    return launch_room<k_packed_tiles<TYPE, MT, NS, 4, GATED>>(grid, 64 * kTileWaves, lds, st, a);
+    if (a.p.shift == 6) return launch_room<k_packed_tiles<TYPE, 4, NS, 2, GATED, DEEP>>(grid, 64 * kTileWaves, lds, st, a);
+    return launch_room<k_packed_tiles<TYPE, 4, NS, 4, GATED, DEEP>>(grid, 64 * kTileWaves, lds, st, a);
 }
-template <int TYPE, int MT> bool launch(int streams, bool gated, const TilesArgs& a, hipStream_t st) {
-    if (gated) return streams == 2 ? launch<TYPE, MT, 2, true>(a, st) : launch<TYPE, MT, 4, true>(a, st);
-    if constexpr (MT == 2) {
-        if (streams == 1) return launch<TYPE, MT, 1, false>(a, st);
+template <int TYPE, bool DEEP> bool launch(int streams, bool gated, const TilesArgs& a, hipStream_t st) {
+    if constexpr (DEEP) {
+        if (gated) return launch<TYPE, 2, true, true>(a, st);
+        return streams == 1 ? launch<TYPE, 1, false, true>(a, st) : launch<TYPE, 2, false, true>(a, st);
+    } else {
+        if (gated) return streams == 2 ? launch<TYPE, 2, true, false>(a, st) : launch<TYPE, 4, true, false>(a, st);
+        return streams == 2 ? launch<TYPE, 2, false, false>(a, st) : launch<TYPE, 4, false, false>(a, st);
     }
-    return streams == 2 ? launch<TYPE, MT, 2, false>(a, st) : launch<TYPE, MT, 4, false>(a, st);
 }
 
 }  // namespace
 
-bool launch_packed_tiles(int32_t dtype, int wave_rows, int streams, bool gated, const TilesArgs& a, hipStream_t st) {
+bool launch_packed_tiles(int32_t dtype, bool deep, int streams, bool gated, const TilesArgs& a, hipStream_t st) {
     bool ok = false;
     for_type(dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
         const int64_t units = (int64_t)a.row_tiles * a.p.parts;
         hipLaunchKernelGGL(k_packed_lay<kType>, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, st, a.p, const_cast<char*>(a.x),
                            reinterpret_cast<float*>(const_cast<char*>(a.sums)), units);
-        ok = wave_rows == 4 ? launch<kType, 4>(streams, gated, a, st) : launch<kType, 2>(streams, gated, a, st);
+        ok = deep ? launch<kType, true>(streams, gated, a, st) : launch<kType, false>(streams, gated, a, st);
     });
     return ok;
 }

@@ -93,6 +93,17 @@ def test_prompts(T, Dk, Dv, dtype):
     check(rng, 1, 1, T, 3, 3, Dk, Dv, dtype, fresh=True, keys="alike")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("S,H,Hk,T,Dk,Dv", [(30, 6, 2, 130, 32, 48), (9, 20, 20, 70, 64, 80), (50, 3, 1, 40, 16, 64), (17, 4, 4, 100, 128, 128), (6, 12, 3, 66, 192, 144),
+                                            (11, 5, 5, 96, 256, 160)])
+def test_many_rows_and_heads(S, H, Hk, T, Dk, Dv, dtype):
+    """More workgroups than the chip takes at once: 32 columns each, some of them behind the last."""
+    rng = np.random.default_rng(S + T)
+    n_new = np.round(T * rng.random(S) ** 1.5).astype(int)
+    n_new[-1] = T
+    check(rng, S, 1, T, H, Hk, Dk, Dv, dtype, n_new=n_new)
+
+
 @pytest.mark.parametrize("T", [1, 70])
 def test_parents_and_counts_out_of_range(T):
     rng = np.random.default_rng(T)
