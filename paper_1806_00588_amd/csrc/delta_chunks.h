@@ -283,10 +283,13 @@ template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(co
             if (sum - i >= 0 && sum - i < PB) { acc[turn & 1] = mfma_bf16(a[i], b[sum - i], acc[turn & 1]); ++turn; }
 }
 
-// A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what is made for
-// tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight to
-// registers, and asked for a chunk ahead.  Bound by the chain of a chunk's instructions: 16 heads of 128 x 128, 8192 tokens TIME us a chunk.  (Four waves with
-// columns of their own, operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk.)
+// A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what
+// is made for tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight
+// to registers.  Bound by the chain of a chunk: some 400 instructions a wave and tile of columns, 45 of them matrix ones, four phases that wait for each other.
+// 16 heads of 128 x 128 in bf16, 128 workgroups: 1.95 us a chunk, operands asked for two chunks ahead (one: 2.15).  (Four waves with columns of their own,
+// operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk, and a wave alone on its CU 4.5.)
+// Where there are more than 512 workgroups of 16 columns, 32 columns and two workgroups a CU that ask when they need it: 144 heads of 96 x 160 in fp16,
+// up to 700 tokens, 71 to 83 us; 16 columns 65 to 95, asking ahead 74 to 82.
 // AHEAD: chunks that operands are asked for ahead, for which a workgroup has half a CU or a whole one; 0: when they are needed.  TILES: times 16 columns.
 template <int TYPE, int NK, int AHEAD, int TILES>
 __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {

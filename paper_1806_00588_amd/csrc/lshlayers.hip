@@ -47,6 +47,7 @@ struct RowsPlan {
     unsigned grid;                 // workgroups of a group of rows
     size_t lds;
     int join_at;
+    int splits, split_parts;       // of the inputs
 };
 constexpr int kFewRows = 32;
 RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
@@ -57,24 +58,35 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     const int64_t tiles = tiles_of(p), parts = parts_of(p), planes = dtype == LSH_F32 ? 3 : 1;
     w.waves = w.row_tiles == 1 && tiles * parts > 8 * 256 ? 16 : 8;
     // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in units of 10 ns -- a wave's tile 40 a
-    // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 90 a round (fitted to 12 rows of fp32 x 40000 x 1000 in six
-    // divisions, 13.6 to 24.6 us, and bf16 x 4096 x 4096 in six, 8.3 to 15)
+    // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 90 a round, rows to LDS 1 for 400 bytes of operands, in every round
+    // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 in six divisions, 13.6 to 24.6 us, bf16 x 4096 x 4096 in six, 8.3 to 15, and
+    // to 96 rows of these, 42)
+    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1);
     int64_t best = INT64_MAX;
     for (int each = 1; each <= (gated ? 1 : 2); each *= 2)
         for (int lg = 0; (w.row_tiles * each << lg) <= w.waves; ++lg) {
             const int64_t sets = ceil_div(tiles, (int64_t)each << lg), rounds = ceil_div(sets * w.groups, 256), streams = gated ? 2 * each : each;
-            const int64_t cost = rounds * (ceil_div(parts, w.waves >> lg) * w.row_tiles * ((planes == 3 ? 57 : 40) * streams + 10 * planes) + 90);
+            const bool stay = parts * of_part + 2 * packed_join(w.waves, w.row_tiles, (int)streams) <= kMaxDynLds;
+            const int64_t cost = rounds * (ceil_div(parts, w.waves >> lg) * w.row_tiles * ((planes == 3 ? 57 : 40) * streams + 10 * planes) + 90) +
+                                 (stay ? 1 : rounds) * w.rows * parts * planes * 256 / 400;
             if (cost < best) { best = cost; w.streams = (int)streams; w.log_across = lg; w.sets = sets; }
         }
     const int deep = w.waves >> w.log_across;
-    w.grid = (unsigned)std::min<int64_t>(w.sets, std::max(1, 256 / w.groups));
+    // few workgroups that go through many parts: the parts are split (a launch more, some 3 us; 16 rows x 1000 x 16384 in fp16 25.9 -> 13.1 us)
+    const int64_t turns = ceil_div(parts, deep), wide = w.sets * w.groups;
+    w.split_parts = (int)parts;
+    if (turns >= 6 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 2, 256 / wide)) * deep);
+    w.splits = (int)ceil_div(parts, w.split_parts);
+    const int64_t of_split = w.split_parts;
     // all rows in LDS, or as many of their parts as there is room for
-    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1), join = 2 * packed_join(w.waves, w.row_tiles, w.streams);
-    const int64_t chunks = ceil_div(parts, (int64_t)((kMaxDynLds - join) / of_part));
-    int64_t chunk = ceil_div(parts, chunks);
+    const size_t join = 2 * packed_join(w.waves, w.row_tiles, w.streams);
+    const int64_t chunks = ceil_div(of_split, (int64_t)((kMaxDynLds - join) / of_part));
+    int64_t chunk = ceil_div(of_split, chunks);
     if (chunks > 1 && chunk > deep) chunk = chunk / deep * deep;
     w.chunk = (int)chunk;
     w.turns = (int)ceil_div(chunk, deep);
+    // (who has all rows goes on to further outputs)
+    w.grid = (unsigned)(chunks > 1 ? w.sets : std::min<int64_t>(w.sets, std::max(1, 256 / w.groups)));
     w.join_at = (int)(chunk * of_part);
     w.lds = w.join_at + join;
     return w;
@@ -85,9 +97,15 @@ struct TilesLaunch {
     bool deep;                 // 64 rows
     int streams, row_tiles, row_groups;
     int64_t sets;
+    int splits, split_parts;   // of the inputs
     size_t rows, room;         // the rows as operands; and their groups' sums
 };
-bool takes_tiles(int32_t M) { return M > kFewRows; }
+// Small matrices are not worth laying out the rows first (4096 x 4096 in bf16, 64 rows: k_packed_rows 18.3 us, k_packed_tiles 23.3; 16384 x 4096 gated, 32 and 40
+// rows: 30.6 and 56 against 31.7 and 33.6; 40000 x 1000 in fp32, 16, 17 and 32 rows: 17 and 44 and 58 against 41 and 40 and 43), unless their rows do not
+// stay in LDS (1000 x 16384 in fp16, 64 and 96 rows: 33 and 57 against 22).
+bool takes_tiles(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
+    return M > 128 || (M > (dtype == LSH_F32 ? 16 : kFewRows) && tiles_of(p) * parts_of(p) * (gated ? 2 : 1) >= 16384) || (M > kFewRows && parts_of(p) > 48);
+}
 TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     TilesLaunch w{};
     w.row_tiles = (int)ceil_div(M, 16);
@@ -100,9 +118,13 @@ TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, boo
             const int64_t cost = ceil_div(groups * sets, 256) * (4 * streams * (dtype == LSH_F32 ? 48 : 16) + 250) / (deep ? 2 : 1);
             if (cost < best) { best = cost; w.deep = deep != 0; w.streams = streams; w.row_groups = (int)groups; w.sets = sets; }
         }
+    const int64_t halves = w.deep ? 2 : 1, turns = ceil_div(parts_of(p), halves), wide = w.sets * w.row_groups;
+    w.split_parts = (int)(turns * halves);
+    if (turns >= 12 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 4, 256 / wide)) * halves);
+    w.splits = (int)ceil_div(parts_of(p), w.split_parts);
     const size_t units = (size_t)w.row_tiles * parts_of(p);
     w.rows = units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
-    w.room = w.rows + units * 64 * (kPackInputs / p->group);
+    w.room = round_up(w.rows + units * 64 * (kPackInputs / p->group));
     return w;
 }
 
@@ -114,10 +136,10 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
         !aligned(bias_dev, 4) || (add_dev && (add_ld < p->N || !aligned(add_dev, type_bytes(out->dtype)))) || !workspace_dev || !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
     if (workspace_bytes < lsh_packed_workspace_bytes(p, M)) return LSH_ERR_WORKSPACE_TOO_SMALL;
-    const bool many = takes_tiles(M);
+    const bool many = takes_tiles(p, M, x->dtype, gated);
     const RowsPlan w = rows_plan(p, M, x->dtype, gated);
     const TilesLaunch tiles = tiles_plan(p, M, x->dtype, gated);
-    if (many ? ceil_div((int64_t)tiles.row_tiles * parts_of(p), 4) > kMaxGrid || tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 2)
+    if (many ? ceil_div((int64_t)tiles.row_tiles * parts_of(p), 4) > kMaxGrid || tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 4)
         return LSH_ERR_UNSUPPORTED;
     PackedArgs a{};
     a.M = M; a.N = p->N; a.K = p->K; a.tiles = (int)tiles_of(p); a.parts = (int)parts_of(p);
@@ -130,13 +152,20 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     a.out = out_dev; a.ld_out = out->ld; a.out_type = out->dtype == LSH_F32 ? kTypeF32 : out->dtype == LSH_BF16 ? kTypeBf16 : kTypeF16;
     a.activation = activation;
     a.rows = w.rows; a.log_across = w.log_across; a.chunk = w.chunk; a.turns = w.turns; a.sets = (int)w.sets; a.join_at = w.join_at;
+    a.splits = many ? tiles.splits : w.splits; a.split_parts = many ? tiles.split_parts : w.split_parts;
+    char* room = static_cast<char*>(workspace_dev);
+    a.partial = reinterpret_cast<float*>(room + (many ? tiles.room : 0));
     const hipStream_t st = (hipStream_t)hip_stream;
     bool ok = false;
     if (many) {
-        char* room = static_cast<char*>(workspace_dev);
         const TilesArgs t{a, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
         ok = launch_packed_tiles(x->dtype, tiles.deep, tiles.streams, gated, t, st);
-    } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups), w.lds, st);
+    } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups, (unsigned)w.splits), w.lds, st);
+    if (ok && a.splits > 1) {
+        const unsigned grid = (unsigned)ceil_div((int64_t)M * p->N, 256);
+        if (gated) hipLaunchKernelGGL(k_packed_join<true>, dim3(grid), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(k_packed_join<false>, dim3(grid), dim3(256), 0, st, a);
+    }
     if (!ok) (void)hipGetLastError();   // (reported here, not by the caller's next call)
     return ok ? launched() : LSH_ERR_HIP;
 }
@@ -153,8 +182,9 @@ int64_t delta_pairs(const lsh_delta_params* p) { return (int64_t)p->S * p->B * p
 bool delta_fits(const lsh_delta_params* p) {
     return delta_pairs(p) <= kMaxGrid && delta_pairs(p) * p->T <= (int64_t)1 << 26 && ceil_div(delta_pairs(p), 8) * 8 * (p->v_dim / 16) <= kMaxGrid;
 }
-// Rows of more tokens than this go in chunks of 64.
-constexpr int kTokensMost = 32;
+// Rows of more tokens than this go in chunks of 64 (16 pairs of 128 x 128, bf16, 8 and 16 tokens: token after token 12.6 and 21.7 us, a chunk 17.5; 512 pairs,
+// 16 and 24 tokens: 45 and 61 against 55).
+int most_tokens(const lsh_delta_params* p) { return delta_pairs(p) * delta_slices(p) <= 256 ? 12 : 20; }
 
 // The chunks' operands take turns in the workspace: as many pairs of a row and a head and as many of their chunks at a time as have room.
 struct ChunksPlan {
@@ -238,7 +268,15 @@ lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weight
 
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) {
     if (!packed_ok(p) || M < 1 || M > kMaxRows) return 0;
-    return takes_tiles(M) ? std::max<size_t>(256, tiles_plan(p, M, LSH_F32, false).room) : 256;
+    size_t bytes = 256;          // for rows of any type, of one matrix or two
+    for (int32_t dtype : {LSH_F32, LSH_BF16})
+        for (bool gated : {false, true}) {
+            const bool many = takes_tiles(p, M, dtype, gated);
+            const TilesLaunch tiles = tiles_plan(p, M, dtype, gated);
+            const int splits = many ? tiles.splits : rows_plan(p, M, dtype, gated).splits;
+            bytes = std::max(bytes, (many ? tiles.room : 0) + (splits > 1 ? (size_t)splits * (gated ? 2 : 1) * M * p->N * sizeof(float) : 0));
+        }
+    return bytes;
 }
 
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
@@ -258,7 +296,7 @@ lsh_status lsh_packed_gated(const lsh_packed_params* p, const lsh_packed_weights
 size_t lsh_delta_workspace_bytes(const lsh_delta_params* p) {
     if (!delta_ok(p) || !delta_fits(p)) return 0;
     size_t bytes = 256;
-    if (p->T > kTokensMost)
+    if (p->T > most_tokens(p))
         for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16}) bytes = std::max(bytes, chunks_plan(p, dtype).bytes);
     return bytes;
 }
@@ -297,7 +335,7 @@ lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const ls
     bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
-        if (p->T > kTokensMost) {
+        if (p->T > most_tokens(p)) {
             const ChunksPlan w = chunks_plan(p, q_rows->dtype);
             for_dims(p->k_dim, [&](auto nk) { ok = chunks_launch<kType, decltype(nk)::value>(p, a, w, static_cast<char*>(workspace_dev), st); });
             return;

@@ -29,6 +29,9 @@ struct PackedArgs {
     int64_t ld_out;
     int out_type;
     int activation;
+    // few outputs of many inputs: these are split among workgroups, whose sums k_packed_join adds up
+    int splits, split_parts;
+    float* partial;            // [splits][matrix][M, N]
     // of k_packed_rows
     int rows;                  // of a workgroup
     int log_across;            // log2 of the waves side by side along the outputs; the others share their inputs
@@ -103,6 +106,27 @@ __device__ __forceinline__ void put_result(const PackedArgs& a, int64_t m, int64
     else put_value<kTypeF16>(a.out, at, y);
 }
 
+// A part of a result's sum.
+template <bool GATED> __device__ __forceinline__ void put_partial(const PackedArgs& a, int split, int64_t m, int64_t n, float g, float u) {
+    float* to = a.partial + ((int64_t)split * (GATED ? 2 : 1) * a.M + m) * a.N + n;
+    to[0] = g;
+    if (GATED) to[(int64_t)a.M * a.N] = u;
+}
+// The parts' sums, added up in order, to results.  A thread for each.
+template <bool GATED> __global__ void __launch_bounds__(256) k_packed_join(PackedArgs a) {
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, size = (int64_t)a.M * a.N;
+    if (at >= size) return;
+    const int64_t m = at / a.N, n = at - m * a.N;
+    float g = 0.f, u = 0.f;
+    for (int i = 0; i < a.splits; ++i) {
+        const float* from = a.partial + (int64_t)i * (GATED ? 2 : 1) * size + at;
+        g += from[0];
+        if (GATED) u += from[size];
+    }
+    if constexpr (GATED) put_result(a, m, n, activate(g, a.activation) * u);
+    else put_result(a, m, n, g + ((a.add ? added(a, m, n) : 0.f) + (a.bias ? a.bias[n] : 0.f)));
+}
+
 // What a wave asks of a tile's part: codes, its output's scales and zeros.
 template <int PER> struct PackedPiece {
     uint4 codes;
@@ -119,12 +143,13 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
     const int log_deep = (WAVES == 16 ? 4 : 3) - a.log_across, deep = 1 << log_deep;
     const int m0 = blockIdx.y * a.rows, rows = min(a.rows, a.M - m0), of_c = rows_of_c(a.rows), plane = packed_plane(a.rows, a.chunk);
     float* sums = reinterpret_cast<float*>(lds + NP * plane);
-    const int chunks = (a.parts + a.chunk - 1) / a.chunk;
+    const int from_part = blockIdx.z * a.split_parts, parts = min(a.split_parts, a.parts - from_part);
+    const int chunks = (parts + a.chunk - 1) / a.chunk;
 
     // the next part of the wave: asked for as soon as the one before it has been worked on
     int ask_set = blockIdx.x, ask_chunk = 0, ask_turn = 0;
     auto ask = [&](PackedPiece<PER> (&to)[NS]) {
-        const int part = min(ask_chunk * a.chunk + min((ask_turn << log_deep) + wk, a.chunk - 1), a.parts - 1);
+        const int part = from_part + min(ask_chunk * a.chunk + min((ask_turn << log_deep) + wk, a.chunk - 1), parts - 1);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int tile = min(((ask_set << a.log_across) + wn) * NT + (GATED ? s >> 1 : s), a.tiles - 1);
@@ -202,7 +227,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
         const int64_t n = ((int64_t)((set << a.log_across) + of) * NT + nt) * kPackOutputs + (ln & 15);
         const bool mine = wave < finishing && n < a.N;
         f32x4 plus = {0.f, 0.f, 0.f, 0.f};
-        if (!GATED && mine) {
+        if (!GATED && mine && a.splits == 1) {
             const float b = a.bias ? a.bias[n] : 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -211,7 +236,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
             }
         }
         for (int chunk = 0; chunk < chunks; ++chunk) {
-            const int part0 = chunk * a.chunk, here = min(a.chunk, a.parts - part0);
+            const int part0 = from_part + chunk * a.chunk, here = min(a.chunk, parts - chunk * a.chunk);
             if (chunks > 1 || set == (int)blockIdx.x) {
                 __syncthreads();
                 for (int u = threadIdx.x; u < here * rows * 4; u += 64 * WAVES) {
@@ -251,7 +276,9 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int m = 16 * mt + 4 * c + i;
-                if (m < rows) put_result(a, m0 + m, n, GATED ? activate(g[i], a.activation) * u[i] : g[i] + plus[i]);
+                if (m >= rows) continue;
+                if (a.splits > 1) put_partial<GATED>(a, blockIdx.z, m0 + m, n, g[i], u[i]);
+                else put_result(a, m0 + m, n, GATED ? activate(g[i], a.activation) * u[i] : g[i] + plus[i]);
             }
         };
         // waves that share inputs: their sums through LDS, each wave adds up a tile, in order

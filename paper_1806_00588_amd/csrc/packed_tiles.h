@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
         }
     }
 
-    const int turns = (a.parts + HALVES - 1) / HALVES;
-    int ask_turn = 0, ask_in = 0, ask_slot = 0, ask_codes = 0;
+    const int first_turn = blockIdx.y * (a.split_parts / HALVES), turns = min((a.parts + HALVES - 1) / HALVES, first_turn + a.split_parts / HALVES);
+    int ask_turn = first_turn, ask_in = 0, ask_slot = 0, ask_codes = 0;
     auto part_of = [&](int half) { return (int64_t)min(ask_turn * HALVES + half, a.parts - 1); };
     auto ask = [&]() {
 #pragma unroll
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
     wait_vmem<Plan::later(-1)>();
     lds_barrier();
     if constexpr (AHEAD) read_rows(x[0], 0, 0);
-    for (int turn = 0; turn < turns; ++turn) {
+    for (int turn = first_turn; turn < turns; ++turn) {
         const int part = turn * HALVES + wk;
         uint4 codes[NS];
         float scale[NS], zero[NS];
@@ -252,12 +252,14 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             for (int s = 0; s < NS; ++s) {
                 const uint32_t word = ks4 == 0 ? codes[s].x : ks4 == 1 ? codes[s].y : ks4 == 2 ? codes[s].z : codes[s].w;
                 const auto op = weights_operand<TYPE>(word, zero[s]);
+                __builtin_amdgcn_s_setprio(1);      // (the two waves of a SIMD one behind the other: 1 to 3 %)
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int p = P - 1; p >= 0; --p)
                         acc[m][s] = product<TYPE>(x[ks4 & AHEAD][m][p], op, ks4 % PER == 0 && p == P - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[m][s]);
             }
+            __builtin_amdgcn_s_setprio(0);
             if ((ks4 + 1) % PER == 0) {
                 const bool counts = part * kPackInputs + g * (32 * PER) < a.K;    // (scales behind the last group are not used)
                 f32x4 X[MT];
@@ -306,7 +308,8 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             for (int i = 0; i < 4; ++i) {
                 const int64_t row = (int64_t)(mt0 + wm * MT + m) * 16 + 4 * (ln >> 4) + i;
                 if (row >= a.M) continue;
-                if constexpr (GATED) put_result(a, row, n, activate(y[m][2 * nt][i], a.activation) * y[m][2 * nt + 1][i]);
+                if (a.splits > 1) put_partial<GATED>(a, blockIdx.y, row, n, y[m][GATED ? 2 * nt : nt][i], y[m][GATED ? 2 * nt + 1 : nt][i]);
+                else if constexpr (GATED) put_result(a, row, n, activate(y[m][2 * nt][i], a.activation) * y[m][2 * nt + 1][i]);
                 else put_result(a, row, n, y[m][nt][i] + ((a.add ? added(a, row, n) : 0.f) + (a.bias ? a.bias[n] : 0.f)));
             }
         }

@@ -8,7 +8,7 @@ namespace lshbeam {
 namespace {
 
 template <int TYPE, int NS, bool GATED, bool DEEP> bool launch(const TilesArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((a.row_groups * (int64_t)a.sets + 7) / 8 * 8));
+    const dim3 grid((unsigned)((a.row_groups * (int64_t)a.sets + 7) / 8 * 8), (unsigned)a.p.splits);
     constexpr size_t lds = TilesPlan<TYPE, 4, NS, DEEP>::kLds;
     if constexpr (NS < 4) {
         if (a.p.shift == 5) return launch_room<k_packed_tiles<TYPE, 4, NS, 1, GATED, DEEP>>(grid, 64 * kTileWaves, lds, st, a);

@@ -192,6 +192,26 @@ def test_linear_of_every_type_and_group(M, N, K, dtype, zeros, group):
     check_linear(rng, M, Weights(rng, N, K, group, "bf16" if zeros else "f16", zeros), dtype, dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 64, 16000), (16, 100, 7000), (32, 33, 16384), (40, 200, 4500), (130, 70, 3333), (300, 64, 5000)])
+def test_few_outputs_of_many_inputs(M, N, K, dtype):
+    """The inputs are split among workgroups and their sums added up by another launch."""
+    rng = np.random.default_rng(M + K)
+    for i, group in enumerate((32, 128)):
+        w = Weights(rng, N, K, group, zeros=i == 0)
+        check_linear(rng, M, w, dtype, ("f32", dtype)[i], bias=i == 0, add=("in place", None)[i], pitch=3 * i)
+    check_gated(rng, M, N, K, 64, dtype, "gelu")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(33, 17000, 2100), (64, 9000, 4200), (129, 700, 900), (257, 300, 260)])
+def test_matrices_of_every_launch(M, N, K, dtype):
+    """64 rows and 128 rows a workgroup, of matrices that are large enough, and of any with more rows."""
+    rng = np.random.default_rng(M + K)
+    for i, group in enumerate((32, 128)):
+        check_linear(rng, M, Weights(rng, N, K, group, ("f16", "bf16")[i], zeros=i == 1), dtype, dtype)
+
+
 def test_linear_results_do_not_depend_on_the_run():
     import torch
     from paper_1806_00588_amd import binding
