@@ -413,7 +413,8 @@ size_t lsh_delta_workspace_bytes(const lsh_delta_params* p);
  *   u = beta (v - e^decay H^T k),   H <- e^decay H + k u^T,   out = scale H^T q
  *   q_dev, k_dev        [R, T, n_k_heads, k_dim] with pitches, v_dev [R, T, n_heads, v_dim], out_dev the same; all of one type (fp32, bf16 or
  *                       fp16), no two of out's heads on each other and none on an input
- *   decay_dev, beta_dev fp32 [R, T, n_heads]
+ *   decay_dev, beta_dev fp32 [R, T, n_heads]; decays are meant to be 0 or less, -infinity too.  Above it, where those of a row's 64 successive
+ *                       tokens come to more than 88 (e^88 is the last that fp32 has), its results may be infinities or NaN
  *   state_in_dev        fp32 [R, n_heads, k_dim, v_dim], or NULL: all rows begin with zeros
  *   parents_dev         int32 [S, B] (out_beam of a selection), or NULL: row s*B + b begins with the state of row s*B + parents[r], with zeros
  *                       where that is outside 0 .. B-1.  So states need not be moved (lsh_beam_advance) before

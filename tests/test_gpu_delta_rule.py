@@ -104,6 +104,16 @@ def test_many_rows_and_heads(S, H, Hk, T, Dk, Dv, dtype):
     check(rng, S, 1, T, H, Hk, Dk, Dv, dtype, n_new=n_new)
 
 
+@pytest.mark.parametrize("S,T", [(23, 200), (42, 130)])
+def test_operands_that_take_turns_in_the_workspace(S, T):
+    """460 and 840 pairs of a row and a head, a chunk's operands of 325 KB each: a chunk at a time, and a part of the pairs."""
+    rng = np.random.default_rng(S)
+    n_new = rng.integers(0, T + 1, S)
+    n_new[:3] = T, 64, 65
+    check(rng, S, 1, T, 20, 1, 256, 16, "f32", n_new=n_new, in_place=S == 23)
+    check(rng, S // 2, 2, T, 20, 1, 256, 16, "f32", parents=rng.integers(-1, 2, S // 2 * 2))
+
+
 @pytest.mark.parametrize("T", [1, 70])
 def test_parents_and_counts_out_of_range(T):
     rng = np.random.default_rng(T)
@@ -139,6 +149,49 @@ def test_strong_and_no_decay(T):
     tol = 2.0 ** -24 * 16 * np.sqrt((T + 1) * 96) * size
     assert np.all(np.abs(in_64(to) - after) <= tol[:, :, None])
     assert np.all(np.abs(in_64(out) - want) <= tol[:, None])
+
+
+@pytest.mark.parametrize("T", [1, 7, 150])
+def test_beta_up_to_two_and_growing_states(T):
+    """A beta of 2 turns a column round along the key, still not making it longer.  A decay of 0.02 makes it longer by e^(0.02 T) at most: what was rounded
+    grows as the column itself does, whose largest length the tolerance has."""
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(T)
+    for grow in (False, True):
+        q, k, v, decay, beta, state = scene(rng, 1, 2, T, 2, 2, 64, 48, "f32", keys="alike")
+        beta = np.float32(beta * 2).astype(np.float64) if not grow else beta
+        beta[0, :, 0] = 1 if grow else 2
+        if grow:
+            decay[:] = np.float32(0.02)
+        want, after, size = layers.delta_rule(q, k, v, decay, beta, state, 1.0)
+        dp = binding.delta_params(1, 2, T, 2, 2, 64, 48, 1.0)
+        to, out = torch.empty(2, 2, 64, 48, device="cuda"), torch.empty(2, T, 2, 48, device="cuda")
+        binding.delta_rule(dp, *(on_gpu(x) for x in (q, k, v, decay, beta, state)), to, workspace(binding.delta_workspace_bytes(dp)), out)
+        tol = 2.0 ** -24 * 16 * np.sqrt((T + 1) * 128) * size
+        assert np.all(np.abs(in_64(to) - after) <= tol[:, :, None])
+        assert np.all(np.abs(in_64(out) - want) <= tol[:, None])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [1, 9, 150])
+def test_nothing_behind_the_last_token_is_used(T, dtype):
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(T)
+    n_new = np.array([T, T // 2, 0, min(T, 65)])
+    q, k, v, decay, beta, state = scene(rng, 4, 1, T, 2, 1, 48, 64, dtype)
+    dp = binding.delta_params(4, 1, T, 2, 1, 48, 64, 1.0)
+    ws, n, got = workspace(binding.delta_workspace_bytes(dp)), torch.from_numpy(n_new.astype(np.int32)).cuda(), []
+    for bad in (False, True):
+        for r in range(4):
+            if bad:
+                for x in (q, k, v, decay, beta):
+                    x[r, n_new[r]:] = np.nan
+        to, out = torch.zeros(4, 2, 48, 64, device="cuda"), torch.zeros(4, T, 2, 64, device="cuda", dtype=torch_type(dtype))
+        binding.delta_rule(dp, *(on_gpu(x, dtype) for x in (q, k, v)), *(on_gpu(x) for x in (decay, beta, state)), to, ws, out, n_new=n)
+        got.append((to, out))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and bool(torch.isfinite(got[1][0]).all())
 
 
 @pytest.mark.parametrize("T", [1, 20, 150])
