@@ -158,7 +158,8 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     const hipStream_t st = (hipStream_t)hip_stream;
     bool ok = false;
     if (many) {
-        const TilesArgs t{a, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
+        const bool as_they_are = x->dtype == LSH_F16 && p->K % kPackInputs == 0 && x->ld % 8 == 0 && aligned(x_dev, 16);   // (16 bytes at a time)
+        const TilesArgs t{a, as_they_are, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
         ok = launch_packed_tiles(x->dtype, tiles.deep, tiles.streams, gated, t, st);
     } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups, (unsigned)w.splits), w.lds, st);
     if (ok && a.splits > 1) {

@@ -1,7 +1,9 @@
 // Many rows times weights of 4 bits: y[m, n] = sum_g scale[n, g] sum_{k in g} x[m, k] (code[n, k] - zero[n, g]).
 //
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
-// blocks of 1 KB, straight to LDS.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
+// blocks of 1 KB, straight to LDS.  Rows of fp16, of which nothing has to be made before (bf16: the sums of groups), come from where they lie if
+// 16 bytes of them are always neighbours and in place: 40 rows x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 306.  (bf16 too, the sums being products with 1: what is saved,
+// 4.7 us for 40 rows x 4096, these take.)  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
 // converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
 // that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.  Up to 64 rows: the two waves with the same
 // outputs take turns with the parts instead of sharing the rows, so that no weight is converted twice, and add up at the end.
@@ -106,6 +108,7 @@ template <int TYPE> __device__ __forceinline__ typename OperandOf<TYPE>::type we
 
 struct TilesArgs {
     PackedArgs p;
+    bool as_they_are;          // rows are loaded from where they lie, 16 bytes a lane
     const char* x;             // k_packed_lay's blocks, and its sums
     const char* sums;
     int row_tiles;             // 16 rows each
@@ -117,7 +120,7 @@ template <int TYPE, int MT, int NS, int PER, bool GATED, bool DEEP>
 __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t) {
     using Plan = TilesPlan<TYPE, MT, NS, DEEP>;
     constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS, EACH = 4 / PER, HALVES = Plan::kHalves;
-    constexpr bool SUMS = kTileSums<TYPE>;
+    constexpr bool SUMS = kTileSums<TYPE>, AS_THEY_ARE = TYPE == kTypeF16;
     extern __shared__ __align__(16) char lds[];
     const PackedArgs& a = t.p;
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), wn = wave % kTileAcross, wm = DEEP ? 0 : wave / kTileAcross, wk = DEEP ? wave / kTileAcross : 0;
@@ -139,8 +142,11 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
     for (int i = 0; i < Plan::kRowsEach; ++i) {
         const int b = wave * Plan::kRowsEach + i, mt = b / (KS * P);
         rows_half[i] = mt / Plan::kRows;
-        rows_from[i] = t.x + (int64_t)min(mt0 + mt % Plan::kRows, t.row_tiles - 1) * a.parts * (4 * P * 1024) + b % (KS * P) * 1024 + 16 * ln;
+        const int tile = mt0 + mt % Plan::kRows, in_stage = b % (KS * P);
+        if (AS_THEY_ARE && t.as_they_are) rows_from[i] = static_cast<const char*>(a.x) + (int64_t)min(16 * tile + (ln & 15), a.M - 1) * a.ldx * 2 + in_stage * 64 + 16 * (ln >> 4);
+        else rows_from[i] = t.x + (int64_t)min(tile, t.row_tiles - 1) * a.parts * (4 * P * 1024) + in_stage * 1024 + 16 * ln;
     }
+    const int rows_step = AS_THEY_ARE && t.as_they_are ? 64 : P * 1024;               // from 32 inputs to the next
 #pragma unroll
     for (int i = 0; i < Plan::kCodesEach; ++i) {
         const int s = (wave * Plan::kCodesEach + i) % Plan::kCodesOf, of = s % (kTileAcross * NS);
@@ -172,7 +178,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
     auto ask = [&]() {
 #pragma unroll
         for (int i = 0; i < Plan::kRowsEach; ++i)
-            load_to_lds16(rows_from[i] + (part_of(rows_half[i]) * 4 + ask_in * KS) * (P * 1024), lds + ask_slot * Plan::kRowsSlot + (wave * Plan::kRowsEach + i) * 1024);
+            load_to_lds16(rows_from[i] + (part_of(rows_half[i]) * 4 + ask_in * KS) * rows_step, lds + ask_slot * Plan::kRowsSlot + (wave * Plan::kRowsEach + i) * 1024);
         if (ask_in == 0) {
 #pragma unroll
             for (int i = 0; i < Plan::kCodesEach; ++i)

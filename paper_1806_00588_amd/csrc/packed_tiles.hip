@@ -33,7 +33,7 @@ bool launch_packed_tiles(int32_t dtype, bool deep, int streams, bool gated, cons
     for_type(dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
         const int64_t units = (int64_t)a.row_tiles * a.p.parts;
-        hipLaunchKernelGGL(k_packed_lay<kType>, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, st, a.p, const_cast<char*>(a.x),
+        if (!a.as_they_are) hipLaunchKernelGGL(k_packed_lay<kType>, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, st, a.p, const_cast<char*>(a.x),
                            reinterpret_cast<float*>(const_cast<char*>(a.sums)), units);
         ok = deep ? launch<kType, true>(streams, gated, a, st) : launch<kType, false>(streams, gated, a, st);
     });

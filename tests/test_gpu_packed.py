@@ -212,6 +212,24 @@ def test_matrices_of_every_launch(M, N, K, dtype):
         check_linear(rng, M, Weights(rng, N, K, group, ("f16", "bf16")[i], zeros=i == 1), dtype, dtype)
 
 
+@pytest.mark.parametrize("M,N,K", [(40, 100, 6400), (64, 17000, 2176), (129, 700, 128), (300, 270, 1024)])
+def test_rows_from_where_they_lie(M, N, K):
+    """fp16: rows with a pitch of whole 16 bytes, with another one, and from an address between, have the same results bit for bit."""
+    import torch
+    from paper_1806_00588_amd import binding
+    rng = np.random.default_rng(M + K)
+    w = Weights(rng, N, K, 64, zeros=True)
+    check_linear(rng, M, w, "f16", "f16", pitch=8)
+    x = on_gpu(rows_of(rng, M, K, "f16"), "f16")
+    ws, outs = workspace(binding.packed_workspace_bytes(w.pp, M)), []
+    for pitch, begin in ((0, 0), (24, 8), (3, 0), (8, 1)):
+        held = torch.full((M, K + pitch), float("nan"), dtype=torch.float16, device="cuda")
+        held[:, begin:begin + K] = x
+        outs.append(torch.empty(M, N, device="cuda"))
+        binding.packed_linear(w.pp, w.on_gpu, held[:, begin:begin + K], ws, outs[-1])
+    assert all(torch.equal(outs[0], out) for out in outs[1:])
+
+
 def test_linear_results_do_not_depend_on_the_run():
     import torch
     from paper_1806_00588_amd import binding
