@@ -286,7 +286,7 @@ template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(co
 // A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what
 // is made for tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight
 // to registers.  Bound by the chain of a chunk: some 400 instructions a wave and tile of columns, 45 of them matrix ones, four phases that wait for each other.
-// 16 heads of 128 x 128 in bf16, 128 workgroups: 1.95 us a chunk, operands asked for two chunks ahead (one: 2.15).  (Four waves with columns of their own,
+// 16 heads of 128 x 128 in bf16, 128 workgroups: 1.95 us a chunk, operands asked for two chunks ahead (one: 2.15); k_delta_apart 1.74.  (Four waves with columns of their own,
 // operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk, and a wave alone on its CU 4.5.)
 // Where there are more than 512 workgroups of 16 columns, 32 columns and two workgroups a CU that ask when they need it: 144 heads of 96 x 160 in fp16,
 // up to 700 tokens, 71 to 83 us; 16 columns 65 to 95, asking ahead 74 to 82.
@@ -539,6 +539,235 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
                     const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
                     if (live[k] && d < a.Dk) to[(int64_t)d * a.Dv + col[k]] = S[k][j][t][i];
                 }
+}
+
+// Eight waves for 16 columns: four of them as in k_delta_chain, which have the state and make U, and four that make the results, a tile of tokens each, while
+// the others go on: these give the state's planes and U to them through LDS, so that Q S, A U and the results are out of the chunk's chain.  16 heads of
+// 128 x 128 in bf16, 8192 tokens: 224 us, 1.74 a chunk (k_delta_chain 252).  A workgroup has a CU for itself; of more than two rounds of them k_delta_chain is quicker
+// (144 heads of 96 x 160 in fp16, 700 tokens: with what comes before 196 us, this 226).
+template <int TYPE, int NK, int AHEAD>
+__global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
+    using Plan = ChunkPlan<TYPE, NK>;
+    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4;
+    // LDS: K S of each wave's rows of the state; the state; V - e K S, U, and e^(c_last - c_j) U as operands
+    constexpr int kState = 4 * 4 * 1024, kR = kState + NK * ORDER * 1024, kU = kR + 2 * 3 * 1024, kLast = kU + 2 * PA * 1024;
+    __shared__ __align__(16) char lds[kLast + 2 * 3 * 1024];
+    const DeltaArgs& a = ca.d;
+    const unsigned tiles = (unsigned)a.Dv >> 4, on_xcd = blockIdx.x >> 3;
+    const int64_t local = (int64_t)(on_xcd / tiles) * 8 + (blockIdx.x & 7), pair = ca.pair0 + local;
+    if (local >= ca.pairs) return;
+    const int r = (int)(pair / a.heads), h = (int)(pair - (int64_t)r * a.heads);
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()) & 3, ln = lane_id(), c = ln >> 4, n = ln & 15;
+    const bool results = __builtin_amdgcn_readfirstlane(wave_id()) >= 4;
+    const int n_new = delta_new(a, r), begin = ca.chunk0 * kChunk, col = 16 * (int)(on_xcd % tiles) + n;
+    const int chunks = min(ca.chunks, (n_new - begin + kChunk - 1) / kChunk);
+    if (!ca.first && chunks <= 0) return;
+    const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes;       // (the same for all lanes, and stays in scalar registers)
+    auto block = [&](int chunk, int b) { return reinterpret_cast<const uint4*>(room + (size_t)chunk * ca.bytes + (size_t)b * 1024)[(unsigned)ln]; };
+    auto scalars = [&](int chunk) { return reinterpret_cast<const float*>(room + (size_t)chunk * ca.bytes + Plan::kScalars * 1024); };
+    auto read = [&](int at, int b) { return *reinterpret_cast<const uint4*>(lds + at + b * 1024 + 16 * ln); };
+    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+
+    if (results) {
+        struct Operands { uint4 q[NK][P], ap[2][PA]; f32x4 e; } sets[AHEAD];
+        auto ask_q = [&](Operands& to, int chunk) {
+#pragma unroll
+            for (int s = 0; s < NK; ++s)
+#pragma unroll
+                for (int p = 0; p < P; ++p) to.q[s][p] = block(chunk, (s * 8 + 4 + wave) * P + p);
+            to.e = *reinterpret_cast<const f32x4*>(scalars(chunk) + row_of(wave, 4 * c));
+        };
+        auto ask_a = [&](Operands& to, int chunk) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int p = 0; p < PA; ++p) to.ap[s][p] = block(chunk, Plan::kA + PA * block_of(wave, min(s, wave >> 1)) + p);
+        };
+        if (chunks > 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) { ask_q(sets[i], min(i, chunks - 1)); ask_a(sets[i], min(i, chunks - 1)); }
+        }
+        auto work = [&](Operands& of, int chunk) __attribute__((always_inline)) {
+            const int after = min(chunk + AHEAD, chunks - 1);                // (behind the end the last chunk once more)
+            lds_barrier();
+            f32x4 o[2] = {none, none};
+#pragma unroll
+            for (int s = 0; s < NK; ++s) {
+                uint4 sp[ORDER];
+#pragma unroll
+                for (int p = 0; p < ORDER; ++p) sp[p] = read(kState, s * ORDER + p);
+                mfma_two<ORDER>(of.q[s], sp, o);
+            }
+            o[0] = (o[0] + o[1]) * of.e;
+            o[1] = none;
+            ask_q(of, after);
+            lds_barrier();
+            lds_barrier();
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s <= wave >> 1) {
+                    uint4 up[PA];
+#pragma unroll
+                    for (int p = 0; p < PA; ++p) up[p] = read(kU, PA * s + p);
+                    mfma_two<ORDER>(of.ap[s], up, o);
+                }
+            ask_a(of, after);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int token = begin + chunk * kChunk + row_of(wave, 4 * c + i);
+                if (token < n_new) put_value<TYPE>(a.out, r * a.op.row + (int64_t)token * a.op.token + h * a.op.head + col, a.scale * (o[0][i] + o[1][i]));
+            }
+        };
+        for (int chunk = 0; chunk < chunks; chunk += AHEAD) {
+            work(sets[0], chunk);
+            if (AHEAD == 2 && chunk + 1 < chunks) work(sets[AHEAD - 1], chunk + 1);
+        }
+        return;
+    }
+
+    const int64_t size = (int64_t)a.Dk * a.Dv;
+    const int parent = delta_parent(a, r);
+    const float* from = ca.first ? a.state_in + (parent < 0 ? 0 : ((int64_t)parent * a.heads + h) * size) : a.state_out + pair * size;
+    const bool any = !ca.first || parent >= 0;
+    f32x4 S[MINE][2];
+#pragma unroll
+    for (int j = 0; j < MINE; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                S[j][t][i] = any && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
+            }
+    // (what a wave has no work for it asks for all the same, another's: the number of loads under way is known to the compiler then)
+    struct Operands {
+        uint4 k[MINE][4][P], kt[MINE][4][P], tp[2][3];
+        f32x4 e, last;
+        float all;
+        typename WordOf<TYPE>::type v[4];
+    } sets[AHEAD];
+    const int64_t v_from = r * a.vp.row + h * a.vp.head + col;
+    auto ask_k = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int p = 0; p < P; ++p) to.k[j][i][p] = block(chunk, (min(wave + 4 * j, NK - 1) * 8 + i) * P + p);
+    };
+    auto ask_values = [&](Operands& to, int chunk) {
+        to.e = *reinterpret_cast<const f32x4*>(scalars(chunk) + row_of(wave, 4 * c));
+        to.last = *reinterpret_cast<const f32x4*>(scalars(chunk) + 64 + row_of(wave, 4 * c));
+        to.all = scalars(chunk)[63];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                                        // (tokens behind the last count as if they were it: T has zeros there)
+            const int token = min(begin + chunk * kChunk + row_of(wave, 4 * c + i), n_new - 1);
+            to.v[i] = static_cast<const typename WordOf<TYPE>::type*>(a.v)[v_from + token * a.vp.token];
+        }
+    };
+    auto ask_t = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) to.tp[s][p] = block(chunk, Plan::kT + 3 * block_of(wave, min(s, wave >> 1)) + p);
+    };
+    auto ask_kt = [&](Operands& to, int chunk) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                                      // [32 tokens][tile of the state's rows]
+#pragma unroll
+                for (int p = 0; p < P; ++p) to.kt[j][i][p] = block(chunk, Plan::kKt + ((i >> 1) * 2 * NK + 2 * min(wave + 4 * j, NK - 1) + (i & 1)) * P + p);
+    };
+    if (chunks > 0) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int chunk = min(i, chunks - 1);
+            ask_k(sets[i], chunk); ask_values(sets[i], chunk); ask_t(sets[i], chunk); ask_kt(sets[i], chunk);
+        }
+    }
+    f32x4* part = reinterpret_cast<f32x4*>(lds);
+    auto work = [&](Operands& of, int chunk) __attribute__((always_inline)) {
+        const int after = min(chunk + AHEAD, chunks - 1);
+        // K S of the wave's rows of the state, and these for the results
+        f32x4 ks[4] = {none, none, none, none};
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (wave + 4 * j < NK) {
+                float x[8];
+                uint4 sp[3];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = S[j][i >> 2][i & 3];
+                planes_of<3>(x, sp);
+#pragma unroll
+                for (int p = 0; p < ORDER; ++p) *reinterpret_cast<uint4*>(lds + kState + ((wave + 4 * j) * ORDER + p) * 1024 + 16 * ln) = sp[p];
+                mfma_planes<3>(of.k[j], sp, ks);
+            }
+        ask_k(of, after);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) part[(wave * 4 + t) * 64 + ln] = ks[t];
+        lds_barrier();
+        // V - e K S of the wave's tile of tokens
+        f32x4 k_sum = none, v;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (w < NK) k_sum += part[(w * 4 + wave) * 64 + ln];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[i]));
+        put_half<3>(lds + kR, wave, v);
+        lds_barrier();
+        // U = T (V - e K S)
+        f32x4 two[2] = {none, none};
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s <= wave >> 1) {
+                const uint4 rp[3] = {read(kR, 3 * s), read(kR, 3 * s + 1), read(kR, 3 * s + 2)};
+                mfma_two<3>(of.tp[s], rp, two);
+            }
+        const f32x4 u = two[0] + two[1];
+        put_half<PA>(lds + kU, wave, u);
+        put_half<3>(lds + kLast, wave, u * of.last);
+        const float decay = of.all;
+        ask_t(of, after);
+        ask_values(of, after);
+        lds_barrier();
+        // the state
+        uint4 lp[2][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) lp[s][p] = read(kLast, 3 * s + p);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (wave + 4 * j < NK) {
+                S[j][0] *= decay;
+                S[j][1] *= decay;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    uint4 op[2][P];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
+                    mfma_planes<3>(op, lp[s], S[j]);
+                }
+            }
+        ask_kt(of, after);
+    };
+    for (int chunk = 0; chunk < chunks; chunk += AHEAD) {
+        work(sets[0], chunk);
+        if (AHEAD == 2 && chunk + 1 < chunks) work(sets[AHEAD - 1], chunk + 1);
+    }
+    float* to = a.state_out + pair * size;
+#pragma unroll
+    for (int j = 0; j < MINE; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = row_of(2 * (wave + 4 * j) + t, 4 * c + i);
+                if (d < a.Dk) to[(int64_t)d * a.Dv + col] = S[j][t][i];
+            }
 }
 
 }  // namespace lshbeam

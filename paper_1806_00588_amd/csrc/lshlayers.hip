@@ -227,9 +227,11 @@ template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const 
             a.first = chunk == 0;
             if (!launch_room<k_delta_prepare<TYPE, NK>>(dim3((unsigned)(pairs * a.chunks)), 256, kPrepareLds<TYPE, NK>, st, a)) return false;
             const auto grid = [&](int tiles) { return dim3((unsigned)(ceil_div(pairs, 8) * 8 * ceil_div(p->v_dim / 16, tiles))); };
-            constexpr int kAhead = (NK + 3) / 4 * ChunkPlan<TYPE, NK>::P <= 2 ? 2 : 1;       // (what there are registers for)
-            if (grid(1).x <= 512) hipLaunchKernelGGL((k_delta_chain<TYPE, NK, kAhead, 1>), grid(1), dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0, 2>), grid(2), dim3(256), 0, st, a);
+            constexpr int kMine = (NK + 3) / 4 * ChunkPlan<TYPE, NK>::P;      // (what there are registers for)
+            if (grid(1).x <= 512) {
+                if constexpr (kMine <= 3) hipLaunchKernelGGL((k_delta_apart<TYPE, NK, kMine == 1 ? 2 : 1>), grid(1), dim3(512), 0, st, a);
+                else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 1, 1>), grid(1), dim3(256), 0, st, a);
+            } else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0, 2>), grid(2), dim3(256), 0, st, a);
         }
     }
     return true;

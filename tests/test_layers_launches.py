@@ -66,7 +66,7 @@ def test_every_delta_rule_fits_the_chip(record):
         # (pairs of launches, as many as the workspace's turns)
         assert got["status"] == 0 and (len(got["launches"]) == 1 if kw["T"] <= 12 else len(got["launches"]) % 2 == 0 or kw["T"] <= 20), (kw, got)
         for grid, threads, lds in got["launches"]:
-            assert lds < LDS and threads == 256 and 0 < grid < 1 << 24, (kw, got)
+            assert lds < LDS and threads in (256, 512) and 0 < grid and grid * threads < 1 << 32, (kw, got)
         chunks += len(got["launches"]) > 1
     assert chunks > 100
 
