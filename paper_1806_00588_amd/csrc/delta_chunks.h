@@ -286,15 +286,15 @@ template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(co
 // A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what
 // is made for tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight
 // to registers.  Bound by the chain of a chunk: some 400 instructions a wave and tile of columns, 45 of them matrix ones, four phases that wait for each other.
-// 16 heads of 128 x 128 in bf16, 128 workgroups: 1.95 us a chunk, operands asked for two chunks ahead (one: 2.15); k_delta_apart 1.74.  (Four waves with columns of their own,
+// 16 heads of 128 x 128 in bf16, 128 workgroups, operands asked for a chunk ahead: 2.15 us a chunk; k_delta_apart 1.74.  (Four waves with columns of their own,
 // operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk, and a wave alone on its CU 4.5.)
 // Where there are more than 512 workgroups of 16 columns, 32 columns and two workgroups a CU that ask when they need it: 144 heads of 96 x 160 in fp16,
 // up to 700 tokens, 71 to 83 us; 16 columns 65 to 95, asking ahead 74 to 82.
-// AHEAD: chunks that operands are asked for ahead, for which a workgroup has half a CU or a whole one; 0: when they are needed.  TILES: times 16 columns.
-template <int TYPE, int NK, int AHEAD, int TILES>
+// AHEAD: operands are asked for a chunk ahead, for which a workgroup has a CU for itself, or when they are needed.  TILES: times 16 columns.
+template <int TYPE, int NK, bool AHEAD, int TILES>
 __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;
-    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4, SETS = AHEAD ? AHEAD : 1;
+    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4;
     constexpr bool OVER = TILES == 2;                      // (two workgroups a CU)
     using Lds = ChainLds<PA, OVER, TILES>;
     __shared__ __align__(16) char lds[Lds::kBytes];
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
         f32x4 e, last;
         float all;
         typename WordOf<TYPE>::type v[TILES][4];
-    } sets[SETS];
+    } set;
     const char* room = ca.room + (size_t)local * ca.chunks * ca.bytes;       // (the same for all lanes, and stays in scalar registers)
     const int64_t v_from = r * a.vp.row + h * a.vp.head;
     auto block = [&](int chunk, int b) { return reinterpret_cast<const uint4*>(room + (size_t)chunk * ca.bytes + (size_t)b * 1024)[(unsigned)ln]; };
@@ -384,13 +384,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 #pragma unroll
                 for (int p = 0; p < P; ++p) to.kt[j][i][p] = block(chunk, Plan::kKt + ((i >> 1) * 2 * NK + 2 * min(wave + 4 * j, NK - 1) + (i & 1)) * P + p);
     };
-    if (AHEAD && chunks > 0) {
-#pragma unroll
-        for (int i = 0; i < SETS; ++i) {
-            const int chunk = min(i, chunks - 1);
-            ask_kq(sets[i], chunk); ask_values(sets[i], chunk); ask_t(sets[i], chunk); ask_a(sets[i], chunk); ask_kt(sets[i], chunk);
-        }
-    }
+    if (AHEAD && chunks > 0) { ask_kq(set, 0); ask_values(set, 0); ask_t(set, 0); ask_a(set, 0); ask_kt(set, 0); }
 
     const f32x4 none = {0.f, 0.f, 0.f, 0.f};
     f32x4* part = reinterpret_cast<f32x4*>(lds);
@@ -521,12 +515,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
             }
         }
     };
-    for (int chunk = 0; chunk < chunks; chunk += SETS) {
-        work(sets[0], chunk);
-        if constexpr (SETS == 2) {
-            if (chunk + 1 < chunks) work(sets[SETS - 1], chunk + 1);
-        }
-    }
+    for (int chunk = 0; chunk < chunks; ++chunk) work(set, chunk);
     float* to = a.state_out + pair * size;
 #pragma unroll
     for (int k = 0; k < TILES; ++k)
@@ -543,8 +532,9 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 
 // Eight waves for 16 columns: four of them as in k_delta_chain, which have the state and make U, and four that make the results, a tile of tokens each, while
 // the others go on: these give the state's planes and U to them through LDS, so that Q S, A U and the results are out of the chunk's chain.  16 heads of
-// 128 x 128 in bf16, 8192 tokens: 224 us, 1.74 a chunk (k_delta_chain 252).  A workgroup has a CU for itself; of more than two rounds of them k_delta_chain is quicker
+// 128 x 128 in bf16, 8192 tokens: 224 us, 1.74 a chunk (k_delta_chain 252; keys and queries straight from where they lie, rows a few KB apart, 254).  A workgroup has a CU for itself; of more than two rounds of them k_delta_chain is quicker
 // (144 heads of 96 x 160 in fp16, 700 tokens: with what comes before 196 us, this 226).
+// AHEAD: chunks that operands are asked for ahead, what there are registers for.
 template <int TYPE, int NK, int AHEAD>
 __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;

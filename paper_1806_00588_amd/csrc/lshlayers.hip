@@ -230,8 +230,8 @@ template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const 
             constexpr int kMine = (NK + 3) / 4 * ChunkPlan<TYPE, NK>::P;      // (what there are registers for)
             if (grid(1).x <= 512) {
                 if constexpr (kMine <= 3) hipLaunchKernelGGL((k_delta_apart<TYPE, NK, kMine == 1 ? 2 : 1>), grid(1), dim3(512), 0, st, a);
-                else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 1, 1>), grid(1), dim3(256), 0, st, a);
-            } else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, 0, 2>), grid(2), dim3(256), 0, st, a);
+                else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, true, 1>), grid(1), dim3(256), 0, st, a);
+            } else hipLaunchKernelGGL((k_delta_chain<TYPE, NK, false, 2>), grid(2), dim3(256), 0, st, a);
         }
     }
     return true;

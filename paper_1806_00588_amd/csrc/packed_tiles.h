@@ -2,7 +2,8 @@
 //
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
 // blocks of 1 KB, straight to LDS.  Rows of fp16, of which nothing has to be made before (bf16: the sums of groups), come from where they lie if
-// 16 bytes of them are always neighbours and in place: 40 rows x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 306.  (bf16 too, the sums being products with 1: what is saved,
+// 16 bytes of them are always neighbours and in place: 40 rows x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 300 in
+// a graph (launched one by one 290, both).  (bf16 too, the sums being products with 1: what is saved,
 // 4.7 us for 40 rows x 4096, these take.)  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
 // converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
 // that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.  Up to 64 rows: the two waves with the same
