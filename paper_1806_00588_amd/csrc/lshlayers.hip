@@ -58,7 +58,7 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     const int64_t tiles = tiles_of(p), parts = parts_of(p), planes = dtype == LSH_F32 ? 3 : 1;
     w.waves = w.row_tiles == 1 && tiles * parts > 8 * 256 ? 16 : 8;
     // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in units of 10 ns -- a wave's tile 40 a
-    // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 90 a round, rows to LDS 1 for 400 bytes of operands, in every round
+    // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 65 a round, rows to LDS 1 for 400 bytes of operands, in every round
     // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 in six divisions, 13.6 to 24.6 us, bf16 x 4096 x 4096 in six, 8.3 to 15, and
     // to 96 rows of these, 42)
     const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1);
@@ -67,7 +67,7 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
         for (int lg = 0; (w.row_tiles * each << lg) <= w.waves; ++lg) {
             const int64_t sets = ceil_div(tiles, (int64_t)each << lg), rounds = ceil_div(sets * w.groups, 256), streams = gated ? 2 * each : each;
             const bool stay = parts * of_part + 2 * packed_join(w.waves, w.row_tiles, (int)streams) <= kMaxDynLds;
-            const int64_t cost = rounds * (ceil_div(parts, w.waves >> lg) * w.row_tiles * ((planes == 3 ? 57 : 40) * streams + 10 * planes) + 90) +
+            const int64_t cost = rounds * (ceil_div(parts, w.waves >> lg) * w.row_tiles * ((planes == 3 ? 57 : 40) * streams + 10 * planes) + 65) +
                                  (stay ? 1 : rounds) * w.rows * parts * planes * 256 / 400;
             if (cost < best) { best = cost; w.streams = (int)streams; w.log_across = lg; w.sets = sets; }
         }
@@ -102,9 +102,9 @@ struct TilesLaunch {
 };
 // Small matrices are not worth laying out the rows first (4096 x 4096 in bf16, 64 rows: k_packed_rows 18.3 us, k_packed_tiles 23.3; 16384 x 4096 gated, 32 and 40
 // rows: 30.6 and 56 against 31.7 and 33.6; 40000 x 1000 in fp32, 16, 17 and 32 rows: 17 and 44 and 58 against 41 and 40 and 43), unless their rows do not
-// stay in LDS (1000 x 16384 in fp16, 64 and 96 rows: 33 and 57 against 22).
+// stay in LDS (1000 x 16384 in fp16, 24, 32, 64 and 96 rows: 17.6 and 20.3 and 33 and 57 against 16, 16, 17 and 20, of rows that are laid out 20 to 22).
 bool takes_tiles(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
-    return M > 128 || (M > (dtype == LSH_F32 ? 16 : kFewRows) && tiles_of(p) * parts_of(p) * (gated ? 2 : 1) >= 16384) || (M > kFewRows && parts_of(p) > 48);
+    return M > 128 || (M > (dtype == LSH_F32 ? 16 : kFewRows) && tiles_of(p) * parts_of(p) * (gated ? 2 : 1) >= 16384) || (M > (dtype == LSH_F16 ? 24 : kFewRows) && parts_of(p) > 48);
 }
 TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     TilesLaunch w{};
@@ -272,7 +272,7 @@ lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weight
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) {
     if (!packed_ok(p) || M < 1 || M > kMaxRows) return 0;
     size_t bytes = 256;          // for rows of any type, of one matrix or two
-    for (int32_t dtype : {LSH_F32, LSH_BF16})
+    for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16})
         for (bool gated : {false, true}) {
             const bool many = takes_tiles(p, M, dtype, gated);
             const TilesLaunch tiles = tiles_plan(p, M, dtype, gated);
