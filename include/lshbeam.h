@@ -420,8 +420,8 @@ size_t lsh_delta_workspace_bytes(const lsh_delta_params* p);
  *                       where that is outside 0 .. B-1.  So states need not be moved (lsh_beam_advance) before
  *   n_new_dev           int32 [R], each 0 .. T, or NULL: T.  Behind a row's last token nothing is read, and what stands in out stays
  *   state_out_dev       fp32 as state_in: the states afterwards.  It may be state_in itself if parents is NULL; else the two do not overlap
- * States, sums and everything between the inputs and out are fp32 or more (products of 32-bit numbers as sums of bf16 products that leave out
- * some 2^-24 of them; of results of 16 bits 2^-16).  Many tokens of a row go in chunks of 64: what is not finite in a token makes the results of its row
+ * States, sums and everything between the inputs and out are fp32 or more, whatever the type of the inputs (products of 32-bit numbers as sums of bf16
+ * products that leave out at most 2^-24 of them, of either sign).  Many tokens of a row go in chunks of 64: what is not finite in a token makes the results of its row
  * and head NaN from the chunk's first token on, not from its own.  Other rows and heads are not reached.
  * Addresses of the states are multiples of 16 bytes. */
 lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,

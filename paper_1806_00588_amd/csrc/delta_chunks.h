@@ -8,9 +8,10 @@
 // by k_delta_prepare and goes through the workspace; k_delta_chain goes through a row's chunks in order.  The state's columns do not meet: a wave
 // has 16 of them in registers, four waves share what comes through LDS.
 //
-// v_mfma_f32_16x16x32_bf16 everywhere, numbers of 32 bits as three planes of bf16 that add up to them (keys of 16 bits: one plane of bf16, two for
-// fp16), with the products of planes down to 2^-16 of the first, so that what is left out is 2^-24 of a product; of results of 16 bits
-// down to 2^-8, 2^-16 left out, a sixteenth of their own rounding at least.  A result D of an instruction has rows 4 c + i in lane (n, c), an
+// v_mfma_f32_16x16x32_bf16 everywhere, numbers of 32 bits as three planes of bf16 that add up to them (queries and keys of 16 bits: one plane of bf16,
+// two for fp16), whatever the results' type.  A plane is what the ones before it leave, rounded to nearest: at most 2^-8 and 2^-17 of the number, of either
+// sign.  Of the products of planes those of a second and a third, and of two thirds, are left out: 2^-24 of a product at most, 2^-28 in the mean, as
+// often of one sign as of the other.  A result D of an instruction has rows 4 c + i in lane (n, c), an
 // operand rows 8 c + j: rows of the K, Q and T operands are in the order row_of below, so that two results' registers are the next
 // product's operand as they are, and nothing is exchanged between lanes.
 #pragma once
@@ -26,13 +27,12 @@ __device__ __forceinline__ int tile_of_row(int r) { return 2 * (r >> 5) + (r >> 
 __device__ __forceinline__ int place_of_row(int r) { return 4 * (r >> 3 & 3) + (r & 3); }
 
 // Operands of a chunk and head in the workspace, NK = ceil(k_dim / 32):
-//   for each 32 of k_dim: K and Q [4 tiles of tokens][planes]; then e and e^(c_last - c_j) [2][64] fp32; T [6][3], A [6][its planes]; K^T [2][2 NK tiles][planes]
+//   for each 32 of k_dim: K and Q [4 tiles of tokens][planes]; then e and e^(c_last - c_j) [2][64] fp32; T and A [6][3]; K^T [2][2 NK tiles][planes]
 // in blocks of 1 KB.  Of T and A those (tile of rows, 32 columns) that are not zero: (0, 0), (1, 0),
 // (2, 0), (2, 1), (3, 0), (3, 1).
 template <int TYPE, int NK> struct ChunkPlan {
     static constexpr int P = TYPE == kTypeBf16 ? 1 : TYPE == kTypeF16 ? 2 : 3;    // planes of K and Q
-    static constexpr int PA = TYPE == kTypeF32 ? 3 : 2;                           // of A, and of what it meets
-    static constexpr int kScalars = NK * 8 * P, kT = kScalars + 1, kA = kT + 18, kKt = kA + 6 * PA, kBlocks = kKt + 4 * NK * P;
+    static constexpr int kScalars = NK * 8 * P, kT = kScalars + 1, kA = kT + 18, kKt = kA + 18, kBlocks = kKt + 4 * NK * P;
 };
 __host__ __device__ constexpr int block_of(int t, int s) { return t < 2 ? t : 2 * t - 2 + s; }
 
@@ -48,11 +48,29 @@ struct ChunkArgs {
 __device__ __forceinline__ f32x4 mfma_bf16(uint4 a, uint4 b, f32x4 acc) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
-// N products of planes i of a and j of b with i + j < ORDER, the smallest first; one after the other of the N, each waiting for its own sum
-// alone (an instruction that adds to the one before it waits for that).
-template <int ORDER, int N, int PA, int PB> __device__ __forceinline__ void mfma_planes(const uint4 (&a)[N][PA], const uint4 (&b)[PB], f32x4 (&acc)[N]) {
+// Eight values as NP operands that add up to them: each the bf16 nearest to what is left (from 3.39e38 on, which is that type's largest, infinite).
+template <int NP> __device__ __forceinline__ void near_planes(const float (&x)[8], uint4 (&out)[NP]) {
+    float rest[8];
 #pragma unroll
-    for (int sum = ORDER - 1; sum >= 0; --sum)
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 v = {rest[2 * i], rest[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+            if (p + 1 < NP) { rest[2 * i] -= __uint_as_float(w[i] << 16); rest[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u); }
+        }
+        out[p] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// N products of planes i of a and j of b with i + j < 3, the smallest first; one after the other of the N, each waiting for its own sum
+// alone (an instruction that adds to the one before it waits for that).
+template <int N, int PA, int PB> __device__ __forceinline__ void mfma_planes(const uint4 (&a)[N][PA], const uint4 (&b)[PB], f32x4 (&acc)[N]) {
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
             if (sum - i >= 0 && sum - i < PB) {
@@ -138,7 +156,7 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
         for (int i = 0; i < 8; ++i) x[i] = 0.f;
         if (t < n && 8 * piece < a.Dk) load_values<TYPE>(a.k, r * a.kp.row + (int64_t)(t0 + t) * a.kp.token + hk * a.kp.head + 8 * piece, x);
         uint4 op[P];
-        planes_of<P>(x, op);
+        near_planes<P>(x, op);
 #pragma unroll
         for (int p = 0; p < P; ++p)
             *reinterpret_cast<uint4*>(lds + (((p * 4 + tile_of_row(t)) * NK + (piece >> 2)) * 64 + 16 * (piece & 3) + place_of_row(t)) * 16) = op[p];
@@ -155,7 +173,7 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
         uint4 kq[2][P];
-        planes_of<P>(xq[s], kq[1]);
+        near_planes<P>(xq[s], kq[1]);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             kq[0][p] = key(p, wave, s);
@@ -170,7 +188,7 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
 #pragma unroll
             for (int p = 0; p < P; ++p) other[p] = key(p, j, s);
             f32x4 both[2] = {kk[j], qk[j]};
-            mfma_planes<3>(kq, other, both);
+            mfma_planes(kq, other, both);
             kk[j] = both[0];
             qk[j] = both[1];
         }
@@ -245,39 +263,39 @@ __global__ void __launch_bounds__(256) k_delta_prepare(ChunkArgs ca) {
     for (int s = 0; s <= wave >> 1; ++s) {
         const int b = block_of(wave, s), from = row_of(wave, m) * kMatrixPitch + 32 * s + 8 * c;
         float x[8];
-        uint4 tp[3], ap[Plan::PA];
+        uint4 tp[3], ap[3];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = T[from + i] * beta[32 * s + 8 * c + i];
-        planes_of<3>(x, tp);
+        near_planes<3>(x, tp);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = L[from + i];
-        planes_of<Plan::PA>(x, ap);
+        near_planes<3>(x, ap);
 #pragma unroll
         for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(to + (size_t)(Plan::kT + 3 * b + p) * 1024 + 16 * ln) = tp[p];
 #pragma unroll
-        for (int p = 0; p < Plan::PA; ++p) *reinterpret_cast<uint4*>(to + (size_t)(Plan::kA + Plan::PA * b + p) * 1024 + 16 * ln) = ap[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(to + (size_t)(Plan::kA + 3 * b + p) * 1024 + 16 * ln) = ap[p];
     }
 }
 
 // LDS of k_delta_chain: K S and Q S of each wave's rows of the state; V - e K S, U, and e^(c_last - c_j) U as operands.  OVER: U lies over the sums.
-template <int PA, bool OVER, int TILES> struct ChainLds {
-    static constexpr int kR = TILES * 4 * 8 * 1024, kU = OVER ? 0 : kR + TILES * 2 * 3 * 1024, kLast = kU + TILES * 2 * PA * 1024;
+template <bool OVER, int TILES> struct ChainLds {
+    static constexpr int kR = TILES * 4 * 8 * 1024, kU = OVER ? 0 : kR + TILES * 2 * 3 * 1024, kLast = kU + TILES * 2 * 3 * 1024;
     static constexpr int kBytes = OVER ? kR + TILES * 2 * 3 * 1024 : kLast + TILES * 2 * 3 * 1024;
 };
 
 // Planes of a tile's four values a lane: its half of the operand that two tiles make.
-template <int N> __device__ __forceinline__ void put_half(char* to, int tile, const f32x4& v) {
-    float x[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
-    uint4 op[N];
-    planes_of<N>(x, op);
+__device__ __forceinline__ void put_half(char* to, int tile, const f32x4& v) {
+    const float x[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
+    uint4 op[3];
+    near_planes<3>(x, op);
 #pragma unroll
-    for (int p = 0; p < N; ++p) *reinterpret_cast<uint2*>(to + ((tile >> 1) * N + p) * 1024 + 16 * lane_id() + 8 * (tile & 1)) = make_uint2(op[p].x, op[p].y);
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(to + ((tile >> 1) * 3 + p) * 1024 + 16 * lane_id() + 8 * (tile & 1)) = make_uint2(op[p].x, op[p].y);
 }
 // One tile's sum of products of planes, in two accumulators (an instruction that adds to the one before it waits for that).
-template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(const uint4 (&a)[PA], const uint4 (&b)[PB], f32x4 (&acc)[2]) {
+template <int PA, int PB> __device__ __forceinline__ void mfma_two(const uint4 (&a)[PA], const uint4 (&b)[PB], f32x4 (&acc)[2]) {
     int turn = 0;
 #pragma unroll
-    for (int sum = ORDER - 1; sum >= 0; --sum)
+    for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
             if (sum - i >= 0 && sum - i < PB) { acc[turn & 1] = mfma_bf16(a[i], b[sum - i], acc[turn & 1]); ++turn; }
@@ -294,9 +312,9 @@ template <int ORDER, int PA, int PB> __device__ __forceinline__ void mfma_two(co
 template <int TYPE, int NK, bool AHEAD, int TILES>
 __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;
-    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4;
+    constexpr int P = Plan::P, MINE = (NK + 3) / 4;
     constexpr bool OVER = TILES == 2;                      // (two workgroups a CU)
-    using Lds = ChainLds<PA, OVER, TILES>;
+    using Lds = ChainLds<OVER, TILES>;
     __shared__ __align__(16) char lds[Lds::kBytes];
     const DeltaArgs& a = ca.d;
     // workgroups go round the eight XCDs one by one: those of a pair follow each other on one of them, so that its operands come from there but once
@@ -336,7 +354,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 
     // Operands.  What a wave has no work for it asks for all the same (another's): the number of loads under way is known to the compiler then.
     struct Operands {
-        uint4 kq[MINE][8][P], kt[MINE][4][P], tp[2][3], ap[2][PA];
+        uint4 kq[MINE][8][P], kt[MINE][4][P], tp[2][3], ap[2][3];
         f32x4 e, last;
         float all;
         typename WordOf<TYPE>::type v[TILES][4];
@@ -374,7 +392,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int p = 0; p < PA; ++p) to.ap[s][p] = block(chunk, Plan::kA + PA * block_of(wave, min(s, wave >> 1)) + p);
+            for (int p = 0; p < 3; ++p) to.ap[s][p] = block(chunk, Plan::kA + 3 * block_of(wave, min(s, wave >> 1)) + p);
     };
     auto ask_kt = [&](Operands& to, int chunk) {
 #pragma unroll
@@ -412,9 +430,9 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
                     uint4 sp[3];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = S[k][j][i >> 2][i & 3];
-                    planes_of<3>(x, sp);
-                    mfma_planes<3>(op[0], sp, ks[k]);
-                    mfma_planes<ORDER>(op[1], sp, qs[k]);
+                    near_planes<3>(x, sp);
+                    mfma_planes(op[0], sp, ks[k]);
+                    mfma_planes(op[1], sp, qs[k]);
                 }
             }
         if constexpr (AHEAD) ask_kq(of, after);
@@ -434,7 +452,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
                 if (w < NK) k_sum += part[((k * 4 + w) * 8 + wave) * 64 + ln];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[k][i]));
-            put_half<3>(lds + Lds::kR + k * (2 * 3 * 1024), wave, v);
+            put_half(lds + Lds::kR + k * (2 * 3 * 1024), wave, v);
             q_sum[k] = none;
 #pragma unroll
             for (int w = 0; w < 4; ++w)
@@ -451,11 +469,11 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
                 if (s <= wave >> 1) {
                     const int at = Lds::kR + k * (2 * 3 * 1024);
                     const uint4 rp[3] = {read(at, 3 * s), read(at, 3 * s + 1), read(at, 3 * s + 2)};
-                    mfma_two<3>(of.tp[s], rp, two);
+                    mfma_two(of.tp[s], rp, two);
                 }
             const f32x4 u = two[0] + two[1];
-            put_half<PA>(lds + Lds::kU + k * (2 * PA * 1024), wave, u);
-            put_half<3>(lds + Lds::kLast + k * (2 * 3 * 1024), wave, u * of.last);
+            put_half(lds + Lds::kU + k * (2 * 3 * 1024), wave, u);
+            put_half(lds + Lds::kLast + k * (2 * 3 * 1024), wave, u * of.last);
         }
         if constexpr (AHEAD) ask_t(of, after);
         else { ask_a(of, chunk); ask_kt(of, chunk); }
@@ -482,7 +500,7 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
                             for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
-                        mfma_planes<3>(op, lp[s], S[k][j]);
+                        mfma_planes(op, lp[s], S[k][j]);
                     }
                 }
         }
@@ -496,10 +514,10 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (s <= wave >> 1) {
-                    uint4 up[PA];
+                    uint4 up[3];
 #pragma unroll
-                    for (int p = 0; p < PA; ++p) up[p] = read(Lds::kU + k * (2 * PA * 1024), PA * s + p);
-                    mfma_two<ORDER>(of.ap[s], up, o[k]);
+                    for (int p = 0; p < 3; ++p) up[p] = read(Lds::kU + k * (2 * 3 * 1024), 3 * s + p);
+                    mfma_two(of.ap[s], up, o[k]);
                 }
         }
         if constexpr (AHEAD) ask_a(of, after);
@@ -538,9 +556,9 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 template <int TYPE, int NK, int AHEAD>
 __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
     using Plan = ChunkPlan<TYPE, NK>;
-    constexpr int P = Plan::P, PA = Plan::PA, ORDER = TYPE == kTypeF32 ? 3 : 2, MINE = (NK + 3) / 4;
+    constexpr int P = Plan::P, MINE = (NK + 3) / 4;
     // LDS: K S of each wave's rows of the state; the state; V - e K S, U, and e^(c_last - c_j) U as operands
-    constexpr int kState = 4 * 4 * 1024, kR = kState + NK * ORDER * 1024, kU = kR + 2 * 3 * 1024, kLast = kU + 2 * PA * 1024;
+    constexpr int kState = 4 * 4 * 1024, kR = kState + NK * 3 * 1024, kU = kR + 2 * 3 * 1024, kLast = kU + 2 * 3 * 1024;
     __shared__ __align__(16) char lds[kLast + 2 * 3 * 1024];
     const DeltaArgs& a = ca.d;
     const unsigned tiles = (unsigned)a.Dv >> 4, on_xcd = blockIdx.x >> 3;
@@ -559,7 +577,7 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
     const f32x4 none = {0.f, 0.f, 0.f, 0.f};
 
     if (results) {
-        struct Operands { uint4 q[NK][P], ap[2][PA]; f32x4 e; } sets[AHEAD];
+        struct Operands { uint4 q[NK][P], ap[2][3]; f32x4 e; } sets[AHEAD];
         auto ask_q = [&](Operands& to, int chunk) {
 #pragma unroll
             for (int s = 0; s < NK; ++s)
@@ -571,7 +589,7 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int p = 0; p < PA; ++p) to.ap[s][p] = block(chunk, Plan::kA + PA * block_of(wave, min(s, wave >> 1)) + p);
+                for (int p = 0; p < 3; ++p) to.ap[s][p] = block(chunk, Plan::kA + 3 * block_of(wave, min(s, wave >> 1)) + p);
         };
         if (chunks > 0) {
 #pragma unroll
@@ -583,10 +601,10 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
             f32x4 o[2] = {none, none};
 #pragma unroll
             for (int s = 0; s < NK; ++s) {
-                uint4 sp[ORDER];
+                uint4 sp[3];
 #pragma unroll
-                for (int p = 0; p < ORDER; ++p) sp[p] = read(kState, s * ORDER + p);
-                mfma_two<ORDER>(of.q[s], sp, o);
+                for (int p = 0; p < 3; ++p) sp[p] = read(kState, s * 3 + p);
+                mfma_two(of.q[s], sp, o);
             }
             o[0] = (o[0] + o[1]) * of.e;
             o[1] = none;
@@ -596,10 +614,10 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (s <= wave >> 1) {
-                    uint4 up[PA];
+                    uint4 up[3];
 #pragma unroll
-                    for (int p = 0; p < PA; ++p) up[p] = read(kU, PA * s + p);
-                    mfma_two<ORDER>(of.ap[s], up, o);
+                    for (int p = 0; p < 3; ++p) up[p] = read(kU, 3 * s + p);
+                    mfma_two(of.ap[s], up, o);
                 }
             ask_a(of, after);
 #pragma unroll
@@ -688,10 +706,10 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
                 uint4 sp[3];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = S[j][i >> 2][i & 3];
-                planes_of<3>(x, sp);
+                near_planes<3>(x, sp);
 #pragma unroll
-                for (int p = 0; p < ORDER; ++p) *reinterpret_cast<uint4*>(lds + kState + ((wave + 4 * j) * ORDER + p) * 1024 + 16 * ln) = sp[p];
-                mfma_planes<3>(of.k[j], sp, ks);
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(lds + kState + ((wave + 4 * j) * 3 + p) * 1024 + 16 * ln) = sp[p];
+                mfma_planes(of.k[j], sp, ks);
             }
         ask_k(of, after);
 #pragma unroll
@@ -704,7 +722,7 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
             if (w < NK) k_sum += part[(w * 4 + wave) * 64 + ln];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = fmaf(-of.e[i], k_sum[i], word_f32<TYPE>(of.v[i]));
-        put_half<3>(lds + kR, wave, v);
+        put_half(lds + kR, wave, v);
         lds_barrier();
         // U = T (V - e K S)
         f32x4 two[2] = {none, none};
@@ -712,11 +730,11 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
         for (int s = 0; s < 2; ++s)
             if (s <= wave >> 1) {
                 const uint4 rp[3] = {read(kR, 3 * s), read(kR, 3 * s + 1), read(kR, 3 * s + 2)};
-                mfma_two<3>(of.tp[s], rp, two);
+                mfma_two(of.tp[s], rp, two);
             }
         const f32x4 u = two[0] + two[1];
-        put_half<PA>(lds + kU, wave, u);
-        put_half<3>(lds + kLast, wave, u * of.last);
+        put_half(lds + kU, wave, u);
+        put_half(lds + kLast, wave, u * of.last);
         const float decay = of.all;
         ask_t(of, after);
         ask_values(of, after);
@@ -739,7 +757,7 @@ __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
                         for (int p = 0; p < P; ++p) op[t][p] = of.kt[j][2 * s + t][p];
-                    mfma_planes<3>(op, lp[s], S[j]);
+                    mfma_planes(op, lp[s], S[j]);
                 }
             }
         ask_kt(of, after);
