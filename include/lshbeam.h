@@ -380,8 +380,8 @@ size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M);
  *   bias_dev   fp32 [N], or NULL
  *   add_dev    [M, N] of out's type, with pitch add_ld, or NULL; it may be out itself (same address and pitch)
  *   out        [M, N] of any of the three types, on none of the inputs but add
- * Codes enter the products as they are, whatever x's type; products and sums are fp32, a group's scale and zero are applied to its sum,
- * the result is rounded once.  A row with a NaN or an infinity gives NaN (or infinities), and no other row does. */
+ * Codes less their zeros enter the products, which are exact whatever x's type; a group's sum is fp32, its scale is applied to that, the sum of
+ * groups is fp32 and rounded once.  A row with a NaN or an infinity gives NaN (or infinities), and no other row does. */
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
                              const float* bias_dev, const void* add_dev, int64_t add_ld, void* workspace_dev, size_t workspace_bytes,
                              void* out_dev, const lsh_matrix* out, void* hip_stream);

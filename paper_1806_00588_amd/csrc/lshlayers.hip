@@ -61,7 +61,7 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 65 a round, rows to LDS 1 for 400 bytes of operands, in every round
     // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 in six divisions, 13.6 to 24.6 us, bf16 x 4096 x 4096 in six, 8.3 to 15, and
     // to 96 rows of these, 42)
-    const size_t of_part = planes * packed_plane(w.rows, 1) + packed_sums(w.row_tiles, 1);
+    const size_t of_part = planes * packed_plane(w.rows, 1);
     int64_t best = INT64_MAX;
     for (int each = 1; each <= (gated ? 1 : 2); each *= 2)
         for (int lg = 0; (w.row_tiles * each << lg) <= w.waves; ++lg) {
@@ -98,7 +98,7 @@ struct TilesLaunch {
     int streams, row_tiles, row_groups;
     int64_t sets;
     int splits, split_parts;   // of the inputs
-    size_t rows, room;         // the rows as operands; and their groups' sums
+    size_t room;               // the rows as operands
 };
 // Small matrices are not worth laying out the rows first (4096 x 4096 in bf16, 64 rows: k_packed_rows 18.3 us, k_packed_tiles 23.3; 16384 x 4096 gated, 32 and 40
 // rows: 30.6 and 56 against 31.7 and 33.6; 40000 x 1000 in fp32, 16, 17 and 32 rows: 17 and 44 and 58 against 41 and 40 and 43), unless their rows do not
@@ -123,8 +123,7 @@ TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, boo
     if (turns >= 12 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 4, 256 / wide)) * halves);
     w.splits = (int)ceil_div(parts_of(p), w.split_parts);
     const size_t units = (size_t)w.row_tiles * parts_of(p);
-    w.rows = units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1);
-    w.room = round_up(w.rows + units * 64 * (kPackInputs / p->group));
+    w.room = round_up(units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1));
     return w;
 }
 
@@ -158,8 +157,8 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     const hipStream_t st = (hipStream_t)hip_stream;
     bool ok = false;
     if (many) {
-        const bool as_they_are = x->dtype == LSH_F16 && p->K % kPackInputs == 0 && x->ld % 8 == 0 && aligned(x_dev, 16);   // (16 bytes at a time)
-        const TilesArgs t{a, as_they_are, room, room + tiles.rows, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
+        const bool as_they_are = x->dtype != LSH_F32 && p->K % kPackInputs == 0 && x->ld % 8 == 0 && aligned(x_dev, 16);   // (16 bytes at a time)
+        const TilesArgs t{a, as_they_are, room, tiles.row_tiles, tiles.row_groups, (int)tiles.sets};
         ok = launch_packed_tiles(x->dtype, tiles.deep, tiles.streams, gated, t, st);
     } else ok = launch_packed_rows(x->dtype, w.row_tiles, w.waves, w.streams, gated, a, dim3(w.grid, (unsigned)w.groups, (unsigned)w.splits), w.lds, st);
     if (ok && a.splits > 1) {

@@ -1,7 +1,9 @@
 // Rows times weights of 4 bits (lsh_packed_linear, lsh_packed_gated):
-//   y[m, n] = sum_k x[m, k] (code[n, k] - zero[n, g]) scale[n, g] = sum_g scale[n, g] (sum_{k in g} x[m, k] code[n, k] - zero[n, g] X[m, g])
-// with X[m, g] the sum of a row's inputs of group g.  Codes 0 .. 15 are exact in bf16 and fp16, rows of fp32 are taken apart into three planes of
-// bf16 that add up to them, so every product is exact and nothing but the fp32 sums rounds.
+//   y[m, n] = sum_k x[m, k] (code[n, k] - zero[n, g]) scale[n, g] = sum_g scale[n, g] sum_{k in g} x[m, k] (code[n, k] - zero[n, g])
+// code - zero is exact in bf16 and fp16, rows of fp32 are taken apart into three planes of bf16 that add up to them, so every product is exact and
+// nothing but the fp32 sums rounds.  A conversion of eight codes is 11 instructions in fp16, else 19, and 13 where no matrix has zeros.  (The codes as they are,
+// and the zero times the sum of a group's inputs taken off afterwards, is one of 7, but of two terms that are many times their difference where a row's inputs
+// have one sign.)
 //
 // Few rows: two operations a weight and row, so the weights' bytes bound it.  The rows' operands are in LDS, made once where all of them fit; the weights come
 // straight to registers, the next part of a wave while the others work.  The waves of a workgroup are side by side along the outputs or share the inputs of
@@ -43,26 +45,44 @@ struct PackedArgs {
 constexpr int kRowsPlanesF32 = 3;
 template <int TYPE> constexpr int kRowPlanes = TYPE == kTypeF32 ? kRowsPlanesF32 : 1;
 // LDS: operands of 32 inputs: [plane][of the chunk][c][row] 16 bytes, the c's 32 bytes apart so that four neighbouring lanes write to banks
-// of their own; sums of the rows' groups; twice (for one group of tiles and the next) what the waves that share inputs add up.
+// of their own; twice (for one group of tiles and the next) what the waves that share inputs add up.
 constexpr int rows_of_c(int rows) { return rows * 16 + 32; }
 constexpr int packed_plane(int rows, int chunk) { return chunk * 4 * 4 * rows_of_c(rows); }
-constexpr int packed_sums(int row_tiles, int chunk) { return chunk * 4 * 16 * row_tiles * 4; }
 constexpr int packed_join(int waves, int row_tiles, int streams) { return waves * row_tiles * streams * 1024; }
 
 template <int TYPE> struct OperandOf { using type = bf16x8; };
 template <> struct OperandOf<kTypeF16> { using type = f16x8; };
 
-// Eight codes, as they are, as an operand.
-template <int TYPE> __device__ __forceinline__ typename OperandOf<TYPE>::type codes_operand(uint32_t word) {
-    const uint32_t lo = word & 0x0f0f0f0fu, hi = word >> 4 & 0x0f0f0f0fu;
-    if constexpr (TYPE == kTypeF16) {
-        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, true);
-        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, true);
-        return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-    } else {
+// Is there a conversion of its own for zeros of 8?
+template <int TYPE> constexpr bool kEights = TYPE != kTypeF16;
+// Eight codes less their zero, exactly, as an operand.
+template <int TYPE, bool EIGHT> __device__ __forceinline__ typename OperandOf<TYPE>::type weights_operand(uint32_t word, float zero) {
+    if constexpr (EIGHT) {
+        // code - 8 of all eight at once: its sign, and its size, 0 .. 8; a byte of both is an e4m3 number
+        const uint32_t negative = ~word & 0x88888888u, one = negative >> 3, size = ((word & 0x77777777u) ^ (negative - one)) + one;
+        const uint32_t lo = (size & 0x0f0f0f0fu) | (negative << 4 & 0xf0f0f0f0u), hi = (size >> 4 & 0x0f0f0f0fu) | (negative & 0xf0f0f0f0u);
         const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, true);
         const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, true);
         return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+    }
+    const uint32_t lo = word & 0x0f0f0f0fu, hi = word >> 4 & 0x0f0f0f0fu;
+    if constexpr (TYPE == kTypeF16) {
+        const _Float16 z = (_Float16)zero;
+        const f16x2 zz = {z, z};
+        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, false) - zz, b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, true) - zz;
+        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, false) - zz, d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, true) - zz;
+        return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+    } else {
+        bf16x8 op;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 v = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)(i & 2 ? hi : lo), true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)(i & 2 ? hi : lo), false);
+            const f32x2 w = {fmaf(v.x, 512.f, -zero), fmaf(v.y, 512.f, -zero)};
+            const bf16x2 b = __builtin_convertvector(w, bf16x2);
+            op[2 * i] = b.x;
+            op[2 * i + 1] = b.y;
+        }
+        return op;
     }
 }
 template <int TYPE> __device__ __forceinline__ f32x4 product(uint4 x, typename OperandOf<TYPE>::type w, f32x4 acc) {
@@ -78,13 +98,6 @@ template <int TYPE> __device__ __forceinline__ void row_operand(const float (&x)
         for (int i = 0; i < 4; ++i) b[i] = (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i])) | (uint32_t)__half_as_ushort(__float2half_rn(x[2 * i + 1])) << 16;
         op[0] = make_uint4(b[0], b[1], b[2], b[3]);
     } else planes_of<kRowPlanes<TYPE>>(x, op);
-}
-
-// The sum of the 32 values of four neighbouring lanes.
-__device__ __forceinline__ float quad_sum(const float (&x)[8]) {
-    float of = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-    of += dpp_f32<0xB1>(of);
-    return of + dpp_f32<0x4E>(of);
 }
 
 __device__ __forceinline__ float activate(float z, int kind) {
@@ -133,8 +146,8 @@ template <int PER> struct PackedPiece {
     uint32_t scales[PER == 1 ? 2 : 1], zeros;
 };
 
-// MT: 16 rows each; NS: tiles of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
-template <int TYPE, int MT, int NS, int PER, bool GATED, int WAVES>
+// MT: 16 rows each; NS: tiles of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group; EIGHT: no matrix has zeros.
+template <int TYPE, int MT, int NS, int PER, bool GATED, int WAVES, bool EIGHT>
 __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
     extern __shared__ __align__(16) char lds[];
     constexpr int NP = kRowPlanes<TYPE>, NT = GATED ? NS / 2 : NS, EACH = 4 / PER;
@@ -142,7 +155,6 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
     const int wn = wave & ((1 << a.log_across) - 1), wk = wave >> a.log_across;
     const int log_deep = (WAVES == 16 ? 4 : 3) - a.log_across, deep = 1 << log_deep;
     const int m0 = blockIdx.y * a.rows, rows = min(a.rows, a.M - m0), of_c = rows_of_c(a.rows), plane = packed_plane(a.rows, a.chunk);
-    float* sums = reinterpret_cast<float*>(lds + NP * plane);
     const int from_part = blockIdx.z * a.split_parts, parts = min(a.split_parts, a.parts - from_part);
     const int chunks = (parts + a.chunk - 1) / a.chunk;
 
@@ -188,7 +200,8 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
                     x[mt][i] = *reinterpret_cast<const uint4*>(at + i * plane + w * (4 * of_c) + 16 * min(16 * mt + (ln & 15), rows - 1));
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                const auto op = codes_operand<TYPE>(w == 0 ? now[s].codes.x : w == 1 ? now[s].codes.y : w == 2 ? now[s].codes.z : now[s].codes.w);
+                const float zero = !EIGHT && a.w[GATED ? s & 1 : 0].zeros ? (float)(now[s].zeros >> (8 * (w / PER)) & 0xffu) : 8.f;
+                const auto op = weights_operand<TYPE, EIGHT>(w == 0 ? now[s].codes.x : w == 1 ? now[s].codes.y : w == 2 ? now[s].codes.z : now[s].codes.w, zero);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -198,18 +211,14 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
             if ((w + 1) % PER != 0) continue;
             const int g = w / PER;
             const bool counts = (part0 + p) * kPackInputs + g * (32 * PER) < a.K;     // (scales behind the last group are not used)
-            f32x4 X[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) X[mt] = *reinterpret_cast<const f32x4*>(sums + (p * EACH + g) * (16 * MT) + 16 * mt + 4 * c);
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const uint32_t bits = PER == 1 ? now[s].scales[PER == 1 ? g >> 1 : 0] >> (16 * (g & 1)) & 0xffffu : now[s].scales[0] >> (16 * g) & 0xffffu;
                 const float sc = !counts ? 0.f : a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
-                const float zero = a.w[GATED ? s & 1 : 0].zeros ? (float)(now[s].zeros >> (8 * g) & 0xffu) : 8.f;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[mt][s][i] = fmaf(sc, fmaf(-zero, X[mt][i], acc[mt][s][i]), y[mt][s][i]);
+                    for (int i = 0; i < 4; ++i) y[mt][s][i] = fmaf(sc, acc[mt][s][i], y[mt][s][i]);
             }
             if constexpr (PER == 1 && MT * NS == 8) __builtin_amdgcn_sched_barrier(0);   // (several groups' sums at once have no registers)
         }
@@ -241,7 +250,6 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
                 __syncthreads();
                 for (int u = threadIdx.x; u < here * rows * 4; u += 64 * WAVES) {
                     const int q = u >> 2, m = q % rows, p = q / rows, cc = u & 3;
-                    float group = 0.f;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const int k = (part0 + p) * kPackInputs + 32 * w + 8 * cc;
@@ -257,11 +265,6 @@ __global__ void __launch_bounds__(64 * WAVES) k_packed_rows(PackedArgs a) {
                         char* to = lds + ((p * 4 + w) * 4 + cc) * of_c + m * 16;
 #pragma unroll
                         for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(to + i * plane) = op[i];
-                        group += quad_sum(x);
-                        if ((w + 1) % PER == 0) {
-                            if (cc == 0) sums[(p * EACH + w / PER) * (16 * MT) + m] = group;
-                            group = 0.f;
-                        }
                     }
                 }
                 __syncthreads();

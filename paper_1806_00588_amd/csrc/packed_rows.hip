@@ -7,10 +7,16 @@
 namespace lshbeam {
 namespace {
 
+template <int TYPE, int MT, int NS, bool GATED, int WAVES, bool EIGHT> bool launch(const PackedArgs& a, dim3 grid, size_t lds, hipStream_t st) {
+    if (a.shift == 5) return launch_room<k_packed_rows<TYPE, MT, NS, 1, GATED, WAVES, EIGHT>>(grid, 64 * WAVES, lds, st, a);
+    if (a.shift == 6) return launch_room<k_packed_rows<TYPE, MT, NS, 2, GATED, WAVES, EIGHT>>(grid, 64 * WAVES, lds, st, a);
+    return launch_room<k_packed_rows<TYPE, MT, NS, 4, GATED, WAVES, EIGHT>>(grid, 64 * WAVES, lds, st, a);
+}
 template <int TYPE, int MT, int NS, bool GATED, int WAVES> bool launch(const PackedArgs& a, dim3 grid, size_t lds, hipStream_t st) {
-    if (a.shift == 5) return launch_room<k_packed_rows<TYPE, MT, NS, 1, GATED, WAVES>>(grid, 64 * WAVES, lds, st, a);
-    if (a.shift == 6) return launch_room<k_packed_rows<TYPE, MT, NS, 2, GATED, WAVES>>(grid, 64 * WAVES, lds, st, a);
-    return launch_room<k_packed_rows<TYPE, MT, NS, 4, GATED, WAVES>>(grid, 64 * WAVES, lds, st, a);
+    if constexpr (kEights<TYPE>) {
+        if (!a.w[0].zeros && !a.w[1].zeros) return launch<TYPE, MT, NS, GATED, WAVES, true>(a, grid, lds, st);
+    }
+    return launch<TYPE, MT, NS, GATED, WAVES, false>(a, grid, lds, st);
 }
 template <int TYPE, int MT, int WAVES> bool launch(int streams, bool gated, const PackedArgs& a, dim3 grid, size_t lds, hipStream_t st) {
     if (gated) return launch<TYPE, MT, 2, true, WAVES>(a, grid, lds, st);

@@ -1,10 +1,9 @@
 // Many rows times weights of 4 bits: y[m, n] = sum_g scale[n, g] sum_{k in g} x[m, k] (code[n, k] - zero[n, g]).
 //
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
-// blocks of 1 KB, straight to LDS.  Rows of fp16, of which nothing has to be made before (bf16: the sums of groups), come from where they lie if
-// 16 bytes of them are always neighbours and in place: 40 rows x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 300 in
-// a graph (launched one by one 290, both).  (bf16 too, the sums being products with 1: what is saved,
-// 4.7 us for 40 rows x 4096, these take.)  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
+// blocks of 1 KB, straight to LDS.  Rows of 16 bits, of which nothing has to be made before, come from where they lie if
+// 16 bytes of them are always neighbours and in place: 40 rows of fp16 x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 300 in
+// a graph (launched one by one 290, both); 40 rows of bf16 x 8192 x 8192 29 -> 26.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
 // converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
 // that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.  Up to 64 rows: the two waves with the same
 // outputs take turns with the parts instead of sharing the rows, so that no weight is converted twice, and add up at the end.
@@ -17,19 +16,15 @@ namespace lshbeam {
 
 constexpr int kTileAcross = 4;      // waves along the outputs
 constexpr int kTileWaves = 2 * kTileAcross;
-// bf16: codes enter as they are, the zero is applied to a group's sum with the sum of its inputs (a conversion of 7 instructions for eight codes);
-// else code - zero enters (fp16 11, fp32, where products take three times as long, 19).
-template <int TYPE> constexpr bool kTileSums = TYPE == kTypeBf16;
 
 // [16 rows][part][4][plane] blocks of 1 KB.  A wave for 16 rows and a part; four neighbouring lanes read 32 neighbouring inputs.
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, float* sums, int64_t units) {
+__global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, int64_t units) {
     constexpr int P = kRowPlanes<TYPE>;
     const int64_t unit = (int64_t)blockIdx.x * 4 + wave_id();
     if (unit >= units) return;
     const int64_t mt = unit / a.parts, m = mt * 16 + (lane_id() >> 2);
-    const int part = (int)(unit - mt * a.parts), c = lane_id() & 3, per = 1 << (a.shift - 5);
-    float group = 0.f;
+    const int part = (int)(unit - mt * a.parts), c = lane_id() & 3;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const int k = part * kPackInputs + 32 * w + 8 * c;
@@ -44,13 +39,6 @@ __global__ void __launch_bounds__(256) k_packed_lay(PackedArgs a, char* to, floa
         row_operand<TYPE>(x, op);
 #pragma unroll
         for (int p = 0; p < P; ++p) *reinterpret_cast<uint4*>(to + ((unit * 4 + w) * P + p) * 1024 + (16 * c + (lane_id() >> 2)) * 16) = op[p];
-        if constexpr (kTileSums<TYPE>) {         // [16 rows][part][group][row]
-            group += quad_sum(x);
-            if ((w + 1) % per == 0) {
-                if (c == 0) sums[(unit * (4 / per) + w / per) * 16 + (lane_id() >> 2)] = group;
-                group = 0.f;
-            }
-        }
     }
 }
 
@@ -69,12 +57,11 @@ template <int TYPE, int MT, int NS, bool DEEP> struct TilesPlan {
     static constexpr int kScalesEach = DEEP ? 3 : 2;
     static constexpr int kCodes = kRing * kRowsSlot, kCodesSlot = kCodesOf * 1024;
     static constexpr int kScales = kCodes + kParts * kCodesSlot, kScalesSlot = kTileAcross * kHalves * 768;
-    static constexpr int kSums = kScales + kParts * kScalesSlot, kSumsSlot = kTileSums<TYPE> ? kTileWaves * 256 : 0;
-    static constexpr int kLds = kSums + kParts * kSumsSlot;
+    static constexpr int kLds = kScales + kParts * kScalesSlot;
     static_assert(kLds <= (int)kMaxDynLds && kRowsEach * kTileWaves * 1024 == kRowsSlot && kHalves * kRows == kTileWaves, "every wave asks for as much");
     static_assert(!DEEP || kTileAcross * MT * NS * 1024 <= kCodes, "the sums of one half have room");
     // loads of a wave for the j-th stage of a turn
-    static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + kScalesEach + kTileSums<TYPE> : 0); }
+    static constexpr int loads(int j) { return kRowsEach + (j % kOf == 0 ? kCodesEach + kScalesEach : 0); }
     // ... that may be under way when stage j begins: all but those for it and the next one
     static constexpr int later(int j) {
         int n = 0;
@@ -83,45 +70,20 @@ template <int TYPE, int MT, int NS, bool DEEP> struct TilesPlan {
     }
 };
 
-// Eight codes, less their zero unless that comes later, exactly.
-template <int TYPE> __device__ __forceinline__ typename OperandOf<TYPE>::type weights_operand(uint32_t word, float zero) {
-    if constexpr (kTileSums<TYPE>) return codes_operand<TYPE>(word);
-    const uint32_t lo = word & 0x0f0f0f0fu, hi = word >> 4 & 0x0f0f0f0fu;
-    if constexpr (TYPE == kTypeF16) {
-        const _Float16 z = (_Float16)zero;
-        const f16x2 zz = {z, z};
-        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, false) - zz, b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.f, true) - zz;
-        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, false) - zz, d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.f, true) - zz;
-        return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-    } else {
-        bf16x8 op;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2 v = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)(i & 2 ? hi : lo), true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)(i & 2 ? hi : lo), false);
-            const f32x2 w = {fmaf(v.x, 512.f, -zero), fmaf(v.y, 512.f, -zero)};
-            const bf16x2 b = __builtin_convertvector(w, bf16x2);
-            op[2 * i] = b.x;
-            op[2 * i + 1] = b.y;
-        }
-        return op;
-    }
-}
-
 struct TilesArgs {
     PackedArgs p;
     bool as_they_are;          // rows are loaded from where they lie, 16 bytes a lane
-    const char* x;             // k_packed_lay's blocks, and its sums
-    const char* sums;
+    const char* x;             // k_packed_lay's blocks
     int row_tiles;             // 16 rows each
     int row_groups, sets;      // workgroups along the rows, along the outputs
 };
 
-// NS: tiles of 16 outputs of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group.
-template <int TYPE, int MT, int NS, int PER, bool GATED, bool DEEP>
+// NS: tiles of 16 outputs of a wave (gated: half of them of each matrix, gate and up in turn); PER: times 32 inputs of a group; EIGHT: no matrix has zeros.
+template <int TYPE, int MT, int NS, int PER, bool GATED, bool DEEP, bool EIGHT>
 __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t) {
     using Plan = TilesPlan<TYPE, MT, NS, DEEP>;
     constexpr int P = Plan::P, KS = Plan::KS, OF = Plan::kOf, NT = GATED ? NS / 2 : NS, EACH = 4 / PER, HALVES = Plan::kHalves;
-    constexpr bool SUMS = kTileSums<TYPE>, AS_THEY_ARE = TYPE == kTypeF16;
+    constexpr bool AS_THEY_ARE = P == 1;
     extern __shared__ __align__(16) char lds[];
     const PackedArgs& a = t.p;
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()), ln = lane_id(), wn = wave % kTileAcross, wm = DEEP ? 0 : wave / kTileAcross, wk = DEEP ? wave / kTileAcross : 0;
@@ -154,8 +116,6 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
         codes_half[i] = s / (kTileAcross * NS);
         codes_from[i] = reinterpret_cast<const char*>(a.w[GATED ? of & 1 : 0].codes) + unit_of(of / NS, of % NS) * kPackBytes + 16 * ln;
     }
-    const int sums_half = wave / Plan::kRows % HALVES;
-    const char* sums_from = t.sums + (int64_t)min(mt0 + wave % Plan::kRows, t.row_tiles - 1) * a.parts * (EACH * 64) + 4 * min(ln, EACH * 16 - 1);
     // scales and zeros of the wave's streams, 4 bytes a lane: 16 lanes a stream, scales twice that.  Waves with the same part share the work: the first
     // four ask for the scales, the others for the zeros
     const int mine = min(ln >> 4, NS - 1);
@@ -194,7 +154,6 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
                 load_to_lds4(scales_from[2] + part_of(wk) * scales_step[2], to + 512);   // (as many loads as the other waves')
             }
             if constexpr (DEEP) load_to_lds4(scales_from[2] + part_of(wk) * scales_step[2], to + 512);
-            if constexpr (SUMS) load_to_lds4(sums_from + part_of(sums_half) * (EACH * 64), lds + Plan::kSums + ask_codes * Plan::kSumsSlot + wave * 256);
         }
         ask_slot = ask_slot + 1 == Plan::kRing ? 0 : ask_slot + 1;
         if (++ask_in == OF) {                    // (behind the end the last part once more)
@@ -248,7 +207,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
                     const int at = (ln & 15) * EACH + g;
                     const uint32_t bits = *reinterpret_cast<const uint16_t*>(sc + (at >> 5) * 256 + s * 64 + 2 * (at & 31));
                     scale[s] = a.scale_f16 ? scale_f32<true>(bits) : scale_f32<false>(bits);
-                    zero[s] = a.w[GATED ? s & 1 : 0].zeros ? (float)*reinterpret_cast<const uint8_t*>(sc + 512 + s * 64 + at) : 8.f;
+                    zero[s] = !EIGHT && a.w[GATED ? s & 1 : 0].zeros ? (float)*reinterpret_cast<const uint8_t*>(sc + 512 + s * 64 + at) : 8.f;
                 }
             }
             if constexpr (AHEAD) {
@@ -258,7 +217,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const uint32_t word = ks4 == 0 ? codes[s].x : ks4 == 1 ? codes[s].y : ks4 == 2 ? codes[s].z : codes[s].w;
-                const auto op = weights_operand<TYPE>(word, zero[s]);
+                const auto op = weights_operand<TYPE, EIGHT>(word, zero[s]);
                 __builtin_amdgcn_s_setprio(1);      // (the two waves of a SIMD one behind the other: 1 to 3 %)
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
@@ -269,19 +228,13 @@ __global__ void __launch_bounds__(64 * kTileWaves, 1) k_packed_tiles(TilesArgs t
             __builtin_amdgcn_s_setprio(0);
             if ((ks4 + 1) % PER == 0) {
                 const bool counts = part * kPackInputs + g * (32 * PER) < a.K;    // (scales behind the last group are not used)
-                f32x4 X[MT];
-                if constexpr (SUMS) {
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-                        X[m] = *reinterpret_cast<const f32x4*>(lds + Plan::kSums + codes_slot * Plan::kSumsSlot + (wk * Plan::kRows + wm * MT + m) * 256 + g * 64 + 16 * (ln >> 4));
-                }
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const float f = counts ? scale[s] : 0.f;
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[m][s][i] = fmaf(f, SUMS ? fmaf(-zero[s], X[m][i], acc[m][s][i]) : acc[m][s][i], y[m][s][i]);
+                        for (int i = 0; i < 4; ++i) y[m][s][i] = fmaf(f, acc[m][s][i], y[m][s][i]);
                 }
             }
             if (ks + 1 == KS) slot = slot + 1 == Plan::kRing ? 0 : slot + 1;
