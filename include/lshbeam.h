@@ -371,7 +371,7 @@ lsh_status lsh_packed_quantize(const lsh_packed_params* p, const void* w_dev, co
 lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weights* from, void* out_dev, const lsh_matrix* out,
                              void* hip_stream);
 
-/* Bytes of workspace lsh_packed_linear and lsh_packed_gated need for M rows of any type (0 on invalid arguments). */
+/* Bytes of workspace lsh_packed_linear and lsh_packed_gated need for M rows of any type, or fewer (0 on invalid arguments). */
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M);
 
 /* out[m, n] = sum_k x[m, k] W[n, k] + bias[n] + add[m, n].
@@ -405,7 +405,7 @@ typedef struct {
     float scale;        /* of the results, usually 1 / sqrt(k_dim); finite                             */
 } lsh_delta_params;
 
-/* Bytes of workspace lsh_delta_rule needs, for any type (0 on invalid arguments, and where the call would be LSH_ERR_UNSUPPORTED:
+/* Bytes of workspace lsh_delta_rule needs, for any type and also for fewer rows, tokens or both (0 on invalid arguments, and where the call would be LSH_ERR_UNSUPPORTED:
  * R * T * n_heads > 2^26, or more than 2^24 workgroups). */
 size_t lsh_delta_workspace_bytes(const lsh_delta_params* p);
 

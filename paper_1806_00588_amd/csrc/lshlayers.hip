@@ -106,6 +106,9 @@ struct TilesLaunch {
 bool takes_tiles(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     return M > 128 || (M > (dtype == LSH_F32 ? 16 : kFewRows) && tiles_of(p) * parts_of(p) * (gated ? 2 : 1) >= 16384) || (M > (dtype == LSH_F16 ? 24 : kFewRows) && parts_of(p) > 48);
 }
+size_t tiles_room(const lsh_packed_params* p, int32_t M, int32_t dtype) {
+    return round_up((size_t)ceil_div(M, 16) * parts_of(p) * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1));
+}
 TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     TilesLaunch w{};
     w.row_tiles = (int)ceil_div(M, 16);
@@ -120,11 +123,26 @@ TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, boo
         }
     const int64_t halves = w.deep ? 2 : 1, turns = ceil_div(parts_of(p), halves), wide = w.sets * w.row_groups;
     w.split_parts = (int)(turns * halves);
-    if (turns >= 12 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 4, 256 / wide)) * halves);
+    if (w.deep && turns >= 12 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 4, 256 / wide)) * halves);
     w.splits = (int)ceil_div(parts_of(p), w.split_parts);
-    const size_t units = (size_t)w.row_tiles * parts_of(p);
-    w.room = round_up(units * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1));
+    w.room = tiles_room(p, M, dtype);
     return w;
+}
+
+// What a call needs of the workspace: the rows as operands, and the sums of parts.
+size_t packed_need(const lsh_packed_params* p, int32_t M, bool many, bool gated, const RowsPlan& w, const TilesLaunch& tiles) {
+    const int splits = many ? tiles.splits : w.splits;
+    return (many ? tiles.room : 0) + (splits > 1 ? (size_t)splits * (gated ? 2 : 1) * M * p->N * sizeof(float) : 0);
+}
+// At most that, for these rows or fewer, of any type, of one matrix or two.  Six parts and more are split where `wide` workgroups are 128 at most, into no more than parts / 2
+// and 256 / wide pieces, and a workgroup has 8192 sums at most: 16 tiles of 16 x 16 of each matrix in k_packed_rows, 64 x 128 altogether in k_packed_tiles.
+size_t packed_most(const lsh_packed_params* p, int32_t M) {
+    size_t room = 0;
+    for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16})
+        for (bool gated : {false, true})
+            if (takes_tiles(p, M, dtype, gated)) room = std::max(room, tiles_room(p, M, dtype));
+    const size_t sums = parts_of(p) < 6 ? 0 : std::min((size_t)(parts_of(p) / 2) * 2 * M * p->N, (size_t)1 << 21);
+    return std::max<size_t>(256, room + sums * sizeof(float));
 }
 
 lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* const (&weights)[2], int32_t M, const void* x_dev, const lsh_matrix* x,
@@ -134,10 +152,10 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     if (!packed_ok(p) || !weights_ok(weights[0]) || M < 1 || M > kMaxRows || !matrix_ok(x_dev, x, p->K) || !matrix_ok(out_dev, out, p->N) ||
         !aligned(bias_dev, 4) || (add_dev && (add_ld < p->N || !aligned(add_dev, type_bytes(out->dtype)))) || !workspace_dev || !aligned(workspace_dev, 256))
         return LSH_ERR_INVALID_ARG;
-    if (workspace_bytes < lsh_packed_workspace_bytes(p, M)) return LSH_ERR_WORKSPACE_TOO_SMALL;
     const bool many = takes_tiles(p, M, x->dtype, gated);
     const RowsPlan w = rows_plan(p, M, x->dtype, gated);
     const TilesLaunch tiles = tiles_plan(p, M, x->dtype, gated);
+    if (workspace_bytes < std::max(packed_most(p, M), packed_need(p, M, many, gated, w, tiles))) return LSH_ERR_WORKSPACE_TOO_SMALL;
     if (many ? ceil_div((int64_t)tiles.row_tiles * parts_of(p), 4) > kMaxGrid || tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 4)
         return LSH_ERR_UNSUPPORTED;
     PackedArgs a{};
@@ -184,7 +202,8 @@ bool delta_fits(const lsh_delta_params* p) {
 }
 // Rows of more tokens than this go in chunks of 64 (16 pairs of 128 x 128, bf16, 8 and 16 tokens: token after token 12.6 and 21.7 us, a chunk 17.5; 512 pairs,
 // 16 and 24 tokens: 45 and 61 against 55).
-int most_tokens(const lsh_delta_params* p) { return delta_pairs(p) * delta_slices(p) <= 256 ? 12 : 20; }
+constexpr int kLeastChunked = 12;
+int most_tokens(const lsh_delta_params* p) { return delta_pairs(p) * delta_slices(p) <= 256 ? kLeastChunked : 20; }
 
 // The chunks' operands take turns in the workspace: as many pairs of a row and a head and as many of their chunks at a time as have room.
 struct ChunksPlan {
@@ -202,16 +221,31 @@ template <typename F> void for_dims(int32_t dim, F f) {   // f(std::integral_con
     else if (nk <= 6) f(std::integral_constant<int, 6>());
     else f(std::integral_constant<int, 8>());
 }
+size_t bytes_of_chunk(const lsh_delta_params* p, int32_t dtype) {
+    size_t bytes = 0;
+    for_type(dtype, [&](auto type) {
+        for_dims(p->k_dim, [&](auto nk) { bytes = ChunkPlan<decltype(type)::value, decltype(nk)::value>::kBlocks * 1024; });
+    });
+    return bytes;
+}
 ChunksPlan chunks_plan(const lsh_delta_params* p, int32_t dtype) {
     ChunksPlan w{};
-    for_type(dtype, [&](auto type) {
-        for_dims(p->k_dim, [&](auto nk) { w.of_chunk = ChunkPlan<decltype(type)::value, decltype(nk)::value>::kBlocks * 1024; });
-    });
+    w.of_chunk = bytes_of_chunk(p, dtype);
     const int64_t most = std::max<int64_t>(1, kChunksRoom / w.of_chunk), all = ceil_div(p->T, kChunk);
     w.pairs = std::min(most, delta_pairs(p));
     w.chunks = (int)std::min(std::max<int64_t>(1, most / w.pairs), all);
     w.bytes = w.of_chunk * (size_t)w.pairs * w.chunks;
     return w;
+}
+// At most that, for these rows and tokens or fewer, of any type.
+size_t chunks_most(const lsh_delta_params* p) {
+    size_t bytes = 256;
+    if (p->T > kLeastChunked)
+        for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16}) {
+            const size_t of_chunk = bytes_of_chunk(p, dtype), most = std::max<size_t>(1, kChunksRoom / of_chunk);
+            bytes = std::max(bytes, of_chunk * std::min<size_t>(most, delta_pairs(p) * ceil_div(p->T, kChunk)));
+        }
+    return bytes;
 }
 template <int TYPE, int NK> bool chunks_launch(const lsh_delta_params* p, const DeltaArgs& d, const ChunksPlan& w, char* room, hipStream_t st) {
     ChunkArgs a{};
@@ -269,16 +303,7 @@ lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weight
 }
 
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) {
-    if (!packed_ok(p) || M < 1 || M > kMaxRows) return 0;
-    size_t bytes = 256;          // for rows of any type, of one matrix or two
-    for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16})
-        for (bool gated : {false, true}) {
-            const bool many = takes_tiles(p, M, dtype, gated);
-            const TilesLaunch tiles = tiles_plan(p, M, dtype, gated);
-            const int splits = many ? tiles.splits : rows_plan(p, M, dtype, gated).splits;
-            bytes = std::max(bytes, (many ? tiles.room : 0) + (splits > 1 ? (size_t)splits * (gated ? 2 : 1) * M * p->N * sizeof(float) : 0));
-        }
-    return bytes;
+    return packed_ok(p) && M >= 1 && M <= kMaxRows ? packed_most(p, M) : 0;
 }
 
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
@@ -296,11 +321,7 @@ lsh_status lsh_packed_gated(const lsh_packed_params* p, const lsh_packed_weights
 }
 
 size_t lsh_delta_workspace_bytes(const lsh_delta_params* p) {
-    if (!delta_ok(p) || !delta_fits(p)) return 0;
-    size_t bytes = 256;
-    if (p->T > most_tokens(p))
-        for (int32_t dtype : {LSH_F32, LSH_BF16, LSH_F16}) bytes = std::max(bytes, chunks_plan(p, dtype).bytes);
-    return bytes;
+    return delta_ok(p) && delta_fits(p) ? chunks_most(p) : 0;
 }
 
 lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,
@@ -321,7 +342,9 @@ lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const ls
         if (in < to + size && to < in + size && (parents_dev || in != to)) return LSH_ERR_INVALID_ARG;
     }
     if (heads_overlap(out_rows, R, p->T, p->n_heads, p->v_dim)) return LSH_ERR_INVALID_ARG;
-    if (workspace_bytes < lsh_delta_workspace_bytes(p)) return LSH_ERR_WORKSPACE_TOO_SMALL;
+    const bool chunked = p->T > most_tokens(p);
+    const ChunksPlan w = chunks_plan(p, q_rows->dtype);
+    if (workspace_bytes < std::max(chunks_most(p), chunked ? w.bytes : 0)) return LSH_ERR_WORKSPACE_TOO_SMALL;
     DeltaArgs a{};
     a.S = p->S; a.B = p->B; a.T = p->T; a.heads = p->n_heads; a.k_heads = p->n_k_heads; a.Dk = p->k_dim; a.Dv = p->v_dim;
     a.scale = p->scale;
@@ -337,8 +360,7 @@ lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const ls
     bool ok = true;
     for_type(q_rows->dtype, [&](auto type) {
         constexpr int kType = decltype(type)::value;
-        if (p->T > most_tokens(p)) {
-            const ChunksPlan w = chunks_plan(p, q_rows->dtype);
+        if (chunked) {
             for_dims(p->k_dim, [&](auto nk) { ok = chunks_launch<kType, decltype(nk)::value>(p, a, w, static_cast<char*>(workspace_dev), st); });
             return;
         }
