@@ -363,7 +363,8 @@ typedef struct {
  *   with zeros      lo = min(0, w), hi = max(0, w), scale = (hi - lo) / 15, zero = round(-lo / scale), code = zero + round(w / scale)
  * The scale is rounded to fp32 and then to its type, and used as rounded; the other quotients are exact, rounded to nearest even;
  * zeros and codes are cut to 0 .. 15, and of a group whose scale is 0 they are 8 (without zeros) or 0.  A group with a NaN or an infinity
- * gets a scale that is NaN, and codes 0.  Behind the last output or input codes, scales and zeros are set to 0. */
+ * gets a scale that is NaN, and codes 0.  Behind the last output or input codes, scales and zeros are set to 0.
+ * LSH_ERR_UNSUPPORTED, as of lsh_packed_values: ceil(N / 16) * ceil(K / 128) > 2^26 - 4. */
 lsh_status lsh_packed_quantize(const lsh_packed_params* p, const void* w_dev, const lsh_matrix* w, const lsh_packed_weights* to,
                                void* hip_stream);
 
@@ -371,7 +372,8 @@ lsh_status lsh_packed_quantize(const lsh_packed_params* p, const void* w_dev, co
 lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weights* from, void* out_dev, const lsh_matrix* out,
                              void* hip_stream);
 
-/* Bytes of workspace lsh_packed_linear and lsh_packed_gated need for M rows of any type, or fewer (0 on invalid arguments). */
+/* Bytes of workspace lsh_packed_linear and lsh_packed_gated need for M rows of any type, or fewer (0 on invalid arguments, and where both
+ * would be LSH_ERR_UNSUPPORTED: ceil(M / 16) * ceil(K / 128) > 2^26 - 4). */
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M);
 
 /* out[m, n] = sum_k x[m, k] W[n, k] + bias[n] + add[m, n].
@@ -381,7 +383,9 @@ size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M);
  *   add_dev    [M, N] of out's type, with pitch add_ld, or NULL; it may be out itself (same address and pitch)
  *   out        [M, N] of any of the three types, on none of the inputs but add
  * Codes less their zeros enter the products, which are exact whatever x's type; a group's sum is fp32, its scale is applied to that, the sum of
- * groups is fp32 and rounded once.  A row with a NaN or an infinity gives NaN (or infinities), and no other row does. */
+ * groups is fp32 and rounded once.  A row with a NaN or an infinity gives NaN (or infinities), and no other row does.
+ * LSH_ERR_UNSUPPORTED: where lsh_packed_workspace_bytes is 0 for it, and of more than 2^23 - 1 workgroups, of 64 or 128 rows and 64 to 256 outputs each
+ * (never for M * N <= 2^34). */
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,
                              const float* bias_dev, const void* add_dev, int64_t add_ld, void* workspace_dev, size_t workspace_bytes,
                              void* out_dev, const lsh_matrix* out, void* hip_stream);

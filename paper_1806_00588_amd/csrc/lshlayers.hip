@@ -129,6 +129,8 @@ TilesLaunch tiles_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, boo
     return w;
 }
 
+// Are there workgroups enough to lay out the rows?
+bool packed_fits(const lsh_packed_params* p, int32_t M) { return ceil_div(ceil_div(M, 16) * parts_of(p), 4) <= kMaxGrid; }
 // What a call needs of the workspace: the rows as operands, and the sums of parts.
 size_t packed_need(const lsh_packed_params* p, int32_t M, bool many, bool gated, const RowsPlan& w, const TilesLaunch& tiles) {
     const int splits = many ? tiles.splits : w.splits;
@@ -155,9 +157,8 @@ lsh_status packed_product(const lsh_packed_params* p, const lsh_packed_weights* 
     const bool many = takes_tiles(p, M, x->dtype, gated);
     const RowsPlan w = rows_plan(p, M, x->dtype, gated);
     const TilesLaunch tiles = tiles_plan(p, M, x->dtype, gated);
+    if (!packed_fits(p, M) || (many ? tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 4)) return LSH_ERR_UNSUPPORTED;
     if (workspace_bytes < std::max(packed_most(p, M), packed_need(p, M, many, gated, w, tiles))) return LSH_ERR_WORKSPACE_TOO_SMALL;
-    if (many ? ceil_div((int64_t)tiles.row_tiles * parts_of(p), 4) > kMaxGrid || tiles.sets * tiles.row_groups > kMaxGrid / 2 : w.grid > kMaxGrid / 4)
-        return LSH_ERR_UNSUPPORTED;
     PackedArgs a{};
     a.M = M; a.N = p->N; a.K = p->K; a.tiles = (int)tiles_of(p); a.parts = (int)parts_of(p);
     a.shift = log2_of(p->group);
@@ -303,7 +304,7 @@ lsh_status lsh_packed_values(const lsh_packed_params* p, const lsh_packed_weight
 }
 
 size_t lsh_packed_workspace_bytes(const lsh_packed_params* p, int32_t M) {
-    return packed_ok(p) && M >= 1 && M <= kMaxRows ? packed_most(p, M) : 0;
+    return packed_ok(p) && M >= 1 && M <= kMaxRows && packed_fits(p, M) ? packed_most(p, M) : 0;
 }
 
 lsh_status lsh_packed_linear(const lsh_packed_params* p, const lsh_packed_weights* w, int32_t M, const void* x_dev, const lsh_matrix* x,

@@ -58,3 +58,14 @@ def test_delta_rules_of_fewer_rows_and_tokens_in_the_most_workspace(record):    
                                          out_pitch=(t * heads * v_dim, heads * v_dim, v_dim), bytes=room)) for ty in (0, 1, 2)]
     bad = [(kw, got) for (_, kw), got in zip(calls, record(calls)) if got["status"] != 0]
     assert not bad, bad[:3]
+
+
+@pytest.mark.parametrize("call", ["linear", "gated"])
+def test_products_of_more_than_a_launch_has(record, call):                                     # noqa: F811
+    """Refused before anything is launched, and no size is given for them; the largest that are not refused have one."""
+    size = lambda kw: binding.packed_workspace_bytes(binding.packed_params(kw["N"], kw["K"], kw["group"]), kw["M"])
+    of = lambda M, N, K, group=64: dict(N=N, K=K, group=group, M=M, x_ld=1 << 20, out_ld=1 << 24)
+    too_many_rows, too_many_results, rows, results = of(1 << 20, 100, 1 << 20), of(1 << 20, 1 << 24, 128), of(1 << 20, 100, (1 << 17) - 128), of(1 << 14, 1 << 20, 128)
+    assert size(too_many_rows) == 0 and all(size(kw) > 0 for kw in (too_many_results, rows, results))
+    kinds = [dict(kw, x_type=ty, bytes=size(kw)) for kw in (too_many_rows, too_many_results, rows, results) for ty in (0, 1, 2)]
+    assert [got["status"] for got in record([(call, kw) for kw in kinds])] == [2] * 6 + [0] * 6
