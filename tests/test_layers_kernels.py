@@ -1,0 +1,53 @@
+"""Which kernel a product takes, by the symbols that are launched: no GPU, nothing is run."""
+import json
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+import test_gpu_packed_wide as wide
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+TYPE = {"f32": 0, "bf16": 1, "f16": 2}
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    from test_library_exports import _lib
+    _lib()                       # (built, if it was not)
+    so = str(tmp_path_factory.mktemp("recorder") / "recorder.so")
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-Wall", "-shared", "-fPIC", "-o", so, os.path.join(HERE, "kernel_recorder.cpp"), "-ldl"])
+
+    def run(calls):
+        """For each call (name, arguments) [(kernel, template arguments)]."""
+        done = subprocess.run([sys.executable, os.path.join(HERE, "recorded_layer_kernels.py"), so], input=json.dumps(calls), capture_output=True, text=True)
+        assert done.returncode == 0, (done.returncode, done.stderr[-2000:])
+        out = []
+        for (status, names), call in zip(json.loads(done.stdout), calls):
+            assert status == 0 and names, call
+            out.append([(re.search(r"k_[a-z_]+", n)[0].rstrip("I"), tuple(int(x) for x in re.findall(r"L[ib](\d+)E", n))) for n in names])
+        return out
+    return run
+
+
+def product(name, M, N, K, group, dtype, zeros):
+    """zeros: of each matrix."""
+    kw = dict(N=N, K=K, group=group, M=M, x_type=TYPE[dtype], x_ld=K, out_ld=N)
+    of = [dict(zeros=1 << 20) if z else {} for z in zeros]
+    return name, dict(kw, gate=of[0], up=of[1]) if name == "gated" else dict(kw, **of[0])
+
+
+def test_the_wide_cases_take_every_kernel_of_128_rows(kernels):
+    """k_packed_tiles<type, row tiles, tiles of outputs, times 32 inputs of a group, gated, 64 rows, zeros of 8>."""
+    calls = [product("linear", *case, (z,)) for case in wide.flat(wide.LINEAR) for z in (0, 1)]
+    calls += [product("gated", *case, z) for case in wide.flat(wide.GATED) for z in ((0, 0), (1, 1), (1, 0), (0, 1))]
+    taken = set()
+    for call, launched in zip(calls, kernels(calls)):
+        tiles = [args for name, args in launched if name == "k_packed_tiles"]
+        assert len(tiles) == 1 and tiles[0][5] == 0, (call, launched)
+        taken.add(tiles[0])
+    want = {(t, 4, ns, per, gated, 0, eight) for t in (0, 1, 2) for ns in (2, 4) for per in (1, 2, 4) for gated in (0, 1) for eight in (0, 1)
+            if not (ns == 4 and per == 1) and not (t == 2 and eight)}       # (no four tiles of groups of 32, and one conversion for fp16)
+    assert taken == want, (want - taken, taken - want)
