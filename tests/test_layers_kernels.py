@@ -7,6 +7,7 @@ import sys
 
 import pytest
 
+import test_gpu_packed_kernels as narrow
 import test_gpu_packed_wide as wide
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -51,3 +52,20 @@ def test_the_wide_cases_take_every_kernel_of_128_rows(kernels):
     want = {(t, 4, ns, per, gated, 0, eight) for t in (0, 1, 2) for ns in (2, 4) for per in (1, 2, 4) for gated in (0, 1) for eight in (0, 1)
             if not (ns == 4 and per == 1) and not (t == 2 and eight)}       # (no four tiles of groups of 32, and one conversion for fp16)
     assert taken == want, (want - taken, taken - want)
+
+
+def built(kernel):
+    """Template arguments of every kernel of that name in the library."""
+    from paper_1806_00588_amd import library_path
+    symbols = subprocess.check_output(["nm", "-D", "--defined-only", library_path()], text=True).split()
+    return {tuple(int(x) for x in re.findall(r"L[ib](\d+)E", s)) for s in symbols if re.match(r"_ZN7lshbeam\d+%sI" % kernel, s)}
+
+
+def test_the_cases_take_every_kernel_of_products(kernels):
+    every = [(lists.LINEAR, lists.GATED) for lists in (wide, narrow)]
+    calls = [product("linear", *case, (z,)) for linear, _ in every for case in wide.flat(linear) for z in (0, 1)]
+    calls += [product("gated", *case, z) for _, gated in every for case in wide.flat(gated) for z in ((0, 0), (1, 0))]
+    taken = {kernel for launched in kernels(calls) for kernel in launched}
+    for name in ("k_packed_rows", "k_packed_tiles", "k_packed_lay"):
+        left_out = built(name) - {args for kernel, args in taken if kernel == name}
+        assert built(name) and not left_out, (name, left_out)
