@@ -1,25 +1,32 @@
 """What lsh_delta_rule holds between its inputs and its results has 32 bits, whatever their type.
 
-A row's tokens ask for what they themselves wrote: q = k, of length 1 exactly (entries of 0 and +-2^-m), beta 1, no decay.  So a result is the token's value, made
-of q's product with the state before the chunk and of what the chunk's tokens wrote, which take each other away: with values of 2^-12 and states of 1 what
-is lost of either shows, also behind a rounding to 16 bits.
+A row's tokens ask for what they themselves wrote: keys of length 1 exactly (entries of 0 and +-2^-m), queries some 0.9 times the keys, beta 1, no decay.  So a result
+is that factor times the token's value, made of the query's product with the state before the chunk and of what the chunk's tokens wrote, which take each other away: with values
+of 2^-12 and states of 1 what is lost of either shows, also behind a rounding to 16 bits.  And the state that is left gives the last key's value for that key.
 
-Tolerance, for the root of the mean square.  A sum of n terms of random sign whose squares add up to a^2 rounds n times, each time by 2^-24 of what has been added up
-at most, a in the mean: 2^-24 sqrt(n) a.  A result is the sum over the keys' entries (twice: in u, and its own) and over a chunk's tokens three times (T, A U, the
-state), so n = 2 k_dim + 192.  What a token's u is off by lies in the state along its key, of length 1; later tokens turn that by maps that make nothing longer, and a
-result sees it through a key: not more than u was off.  There are up to 64 of these in a chunk, each seen with a weight of 1 / sqrt(entries) >= 1 / 16 in the mean,
-some 1 to 2 times a result's own altogether; 4 times is allowed.  a is 1 for random signs; for entries and states of one sign sums grow to
-sqrt(entries) times the states' mean, 0.8.  On top comes the rounding of the result."""
+Tolerance, for the root of the mean square.  A sum of n terms of random sign whose squares add up to a^2 rounds n times, each time evenly over at most half a step of what has been
+added up, a sqrt(i / n) in the mean: 2^-24 sqrt(n / 6) a (1 / 3 from the evenness, 1 / 2 from the sum of i / n).  A result is the sum over the keys' entries (twice: in u, and its own) and
+over a chunk's tokens three times (T, A U, the state), so n = 2 k_dim + 192.  What a token's u is off by lies in the state along its key, of length 1; later tokens turn that by maps
+that make nothing longer, and a result sees it through a key: not more than u was off, and of up to 64 of these, each with a weight of 1 / sqrt(entries) in the mean, once
+to twice a result's own altogether; 3 times is allowed.  a is 1 for random signs; for entries and states of one sign sums grow to sqrt(entries) times the states' mean,
+0.8.  On top comes the rounding of the result."""
 import numpy as np
 import pytest
 
 from test_gpu_packed import TYPES, half_step, in_64, on_gpu, torch_type, workspace
+from test_gpu_packed_precision import rms
 
 pytestmark = pytest.mark.gpu
 
 
-def rms(x):
-    return float(np.sqrt(np.mean(np.square(x))))
+def allowed(Dk, entries, one_sign):
+    return 3 * 2.0 ** -24 * np.sqrt((2 * Dk + 192) / 6) * (0.8 * np.sqrt(entries) if one_sign else 1.0)
+
+
+def keys(rng, shape, Dk, entries, one_sign):
+    k = np.zeros(shape + (Dk,))
+    k[..., rng.permutation(Dk)[:entries]] = (np.ones(shape + (entries,)) if one_sign else rng.choice([-1.0, 1.0], shape + (entries,))) / np.sqrt(entries)
+    return k
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -31,16 +38,17 @@ def test_a_value_that_takes_the_states_place(R, H, T, Dk, entries, Dv, one_sign,
     import torch
     from paper_1806_00588_amd import binding
     rng = np.random.default_rng(Dk + T)
-    k = np.zeros((R, T, H, Dk))
-    sign = np.ones((R, T, H, entries)) if one_sign else rng.choice([-1.0, 1.0], (R, T, H, entries))
-    k[..., rng.permutation(Dk)[:entries]] = sign / np.sqrt(entries)
+    k = keys(rng, (R, T, H), Dk, entries, one_sign)
+    q = in_64(on_gpu(0.9 * k, dtype))
     state = rng.normal(size=(R, H, Dk, Dv))
     v = in_64(on_gpu(rng.normal(size=(R, T, H, Dv)) * 2.0 ** -12, dtype))
     dp = binding.delta_params(R, 1, T, H, H, Dk, Dv, 1.0)
-    key, out = on_gpu(k, dtype), torch.zeros(R, T, H, Dv, dtype=torch_type(dtype), device="cuda")
+    out = torch.zeros(R, T, H, Dv, dtype=torch_type(dtype), device="cuda")
     to, zero = torch.empty(R, H, Dk, Dv, device="cuda"), torch.zeros(R, T, H, device="cuda")
-    binding.delta_rule(dp, key, key, on_gpu(v, dtype), zero, zero + 1, on_gpu(np.abs(state) if one_sign else state), to,
+    binding.delta_rule(dp, on_gpu(q, dtype), on_gpu(k, dtype), on_gpu(v, dtype), zero, zero + 1, on_gpu(np.abs(state) if one_sign else state), to,
                        workspace(binding.delta_workspace_bytes(dp)), out)
-    a = 0.8 * np.sqrt(entries) if one_sign else 1.0
-    off, most = rms(in_64(out) - v), 4 * 2.0 ** -24 * np.sqrt(2 * Dk + 192) * a + rms(half_step(v, dtype))
+    most, want = allowed(Dk, entries, one_sign), v * np.abs(q).max() * np.sqrt(entries)
+    off = rms(in_64(out) - want)
+    assert off <= most + rms(half_step(want, dtype)), (off, most)
+    off = rms((k[:, -1, :, :, None] * in_64(to)).sum(2) - v[:, -1])
     assert off <= most, (off, most)
