@@ -7,6 +7,7 @@ import sys
 
 import pytest
 
+import test_gpu_delta_kernels as delta
 import test_gpu_packed_kernels as narrow
 import test_gpu_packed_wide as wide
 
@@ -67,5 +68,17 @@ def test_the_cases_take_every_kernel_of_products(kernels):
     calls += [product("gated", *case, z) for _, gated in every for case in wide.flat(gated) for z in ((0, 0), (1, 0))]
     taken = {kernel for launched in kernels(calls) for kernel in launched}
     for name in ("k_packed_rows", "k_packed_tiles", "k_packed_lay"):
+        left_out = built(name) - {args for kernel, args in taken if kernel == name}
+        assert built(name) and not left_out, (name, left_out)
+
+
+def test_the_cases_take_every_kernel_of_the_delta_rule(kernels):
+    calls = []
+    for S, H, Hk, T, Dk, Dv in delta.FEW + delta.CHUNKS + delta.MANY:
+        for ty in (0, 1, 2):
+            calls.append(("delta", dict(S=S, B=1, T=T, n_heads=H, n_k_heads=Hk, k_dim=Dk, v_dim=Dv, q_type=ty, k_type=ty, v_type=ty, out_type=ty, q_head=Dk,
+                                        out_pitch=(T * H * Dv, H * Dv, Dv))))
+    taken = {kernel for launched in kernels(calls) for kernel in launched}
+    for name in ("k_delta_tokens", "k_delta_prepare", "k_delta_chain", "k_delta_apart"):
         left_out = built(name) - {args for kernel, args in taken if kernel == name}
         assert built(name) and not left_out, (name, left_out)
