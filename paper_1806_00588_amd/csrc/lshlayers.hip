@@ -59,8 +59,8 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     w.waves = w.row_tiles == 1 && tiles * parts > 8 * 256 ? 16 : 8;
     // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in units of 10 ns -- a wave's tile 40 a
     // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 65 a round, rows to LDS 1 for 400 bytes of operands, in every round
-    // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 in six divisions, 13.6 to 24.6 us, bf16 x 4096 x 4096 in six, 8.3 to 15, and
-    // to 96 rows of these, 42)
+    // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 and of bf16 x 4096 x 4096; of ten divisions each it
+    // takes the quickest, 14.8 us of up to 26.2 and 7.9 of up to 12.8)
     const size_t of_part = planes * packed_plane(w.rows, 1);
     int64_t best = INT64_MAX;
     for (int each = 1; each <= (gated ? 1 : 2); each *= 2)
@@ -100,11 +100,14 @@ struct TilesLaunch {
     int splits, split_parts;   // of the inputs
     size_t room;               // the rows as operands
 };
-// Small matrices are not worth laying out the rows first (4096 x 4096 in bf16, 64 rows: k_packed_rows 18.3 us, k_packed_tiles 23.3; 16384 x 4096 gated, 32 and 40
-// rows: 30.6 and 56 against 31.7 and 33.6; 40000 x 1000 in fp32, 16, 17 and 32 rows: 17 and 44 and 58 against 41 and 40 and 43), unless their rows do not
-// stay in LDS (1000 x 16384 in fp16, 24, 32, 64 and 96 rows: 17.6 and 20.3 and 33 and 57 against 16, 16, 17 and 20, of rows that are laid out 20 to 22).
+// From how many rows on k_packed_tiles is quicker than k_packed_rows goes by the matrix (us of the one and the other, in a graph).  Large ones: 16384 x 4096 gated,
+// bf16, 32 and 40 rows 30.6 and 31.6 against 33.0 and 52.6; fp32, 17, 32 and 33 rows 52 and 56 and 54 against 40 and 60 and 77; 40000 x 1000 in fp32, 17, 32 and 40 rows 39 and 41
+// and 44 against 21 and 37 and 47.  With few parts, where there is little to go through between the first load and the results, 16-bit rows never: 40000 x 1000 in
+// bf16, 40 and 128 rows 34 and 51 against 25 and 44 (40000 x 2048, 40 and 64 rows: 39 and 43 against 33 and 56).  Small ones do not pay for the rounds: 2048 x 2048 in bf16, 64 rows, 15.1 against 8.5.
+// But rows of many parts do not stay in LDS: 1000 x 16384 in fp16, 24, 32 and 96 rows 15.3 and 15.5 and 19.4 against 16.7 and 19.3 and 53; fp32, 20 and 40 rows 24 and 25 against 27 and 48.
 bool takes_tiles(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
-    return M > 128 || (M > (dtype == LSH_F32 ? 16 : kFewRows) && tiles_of(p) * parts_of(p) * (gated ? 2 : 1) >= 16384) || (M > (dtype == LSH_F16 ? 24 : kFewRows) && parts_of(p) > 48);
+    const int64_t parts = parts_of(p), work = tiles_of(p) * parts * (gated ? 2 : 1);
+    return M > 128 || (M > kFewRows && work >= 16384 && (dtype == LSH_F32 || parts >= 16)) || (M > (dtype == LSH_F32 ? kFewRows : 24) && parts > 48);
 }
 size_t tiles_room(const lsh_packed_params* p, int32_t M, int32_t dtype) {
     return round_up((size_t)ceil_div(M, 16) * parts_of(p) * 4 * 1024 * (dtype == LSH_F32 ? 3 : 1));

@@ -82,3 +82,13 @@ def test_the_cases_take_every_kernel_of_the_delta_rule(kernels):
     for name in ("k_delta_tokens", "k_delta_prepare", "k_delta_chain", "k_delta_apart"):
         left_out = built(name) - {args for kernel, args in taken if kernel == name}
         assert built(name) and not left_out, (name, left_out)
+
+
+@pytest.mark.parametrize("name,M,N,K,dtype,kernel", [("linear", 17, 40000, 1000, "f32", "k_packed_rows"), ("linear", 32, 40000, 1000, "f32", "k_packed_rows"),
+                                                     ("gated", 24, 16384, 4096, "f32", "k_packed_rows"), ("linear", 64, 40000, 1000, "bf16", "k_packed_rows"),
+                                                     ("linear", 40, 40000, 1000, "f32", "k_packed_tiles"), ("gated", 40, 16384, 4096, "bf16", "k_packed_tiles"),
+                                                     ("linear", 28, 1000, 16384, "bf16", "k_packed_tiles"), ("linear", 129, 64, 64, "f16", "k_packed_tiles")])
+def test_a_product_takes_the_quicker_kernel(kernels, name, M, N, K, dtype, kernel):
+    """As both were measured (takes_tiles in lshlayers.hip has the times)."""
+    launched, = kernels([product(name, M, N, K, 128, dtype, (0, 0))])
+    assert kernel in [k for k, _ in launched]
