@@ -425,8 +425,8 @@ size_t lsh_delta_workspace_bytes(const lsh_delta_params* p);
  *   n_new_dev           int32 [R], each 0 .. T, or NULL: T.  Behind a row's last token nothing is read, and what stands in out stays
  *   state_out_dev       fp32 as state_in: the states afterwards.  It may be state_in itself if parents is NULL; else the two do not overlap
  * States, sums and everything between the inputs and out are fp32 or more, whatever the type of the inputs (products of 32-bit numbers as sums of bf16
- * products that leave out at most 2^-24 of them, of either sign).  Many tokens of a row go in chunks of 64: what is not finite in a token makes the results of its row
- * and head NaN from the chunk's first token on, not from its own.  Other rows and heads are not reached.
+ * products that leave out at most 2^-24 of them, of either sign).  Many tokens of a row go in chunks of 64: what is not finite in a token (or 3.39e38 and more, the largest
+ * that bf16 has) may make the results of its row and head NaN from the chunk's first token on, not from its own.  Other rows and heads are not reached.
  * Addresses of the states are multiples of 16 bytes. */
 lsh_status lsh_delta_rule(const lsh_delta_params* p, const void* q_dev, const lsh_rows* q_rows, const void* k_dev, const lsh_rows* k_rows,
                           const void* v_dev, const lsh_rows* v_rows, const float* decay_dev, const float* beta_dev,

@@ -303,11 +303,11 @@ template <int PA, int PB> __device__ __forceinline__ void mfma_two(const uint4 (
 
 // A workgroup of four waves for 16 columns of a row's and head's state, or 32.  Wave w has the state's rows of every fourth 32 of k_dim in registers, and of what
 // is made for tokens the tile w; K S, V - e K S and U are exchanged through LDS, three barriers a chunk.  So an operand is loaded by one wave, straight
-// to registers.  Bound by the chain of a chunk: some 400 instructions a wave and tile of columns, 45 of them matrix ones, four phases that wait for each other.
-// 16 heads of 128 x 128 in bf16, 128 workgroups, operands asked for a chunk ahead: 2.15 us a chunk; k_delta_apart 1.74.  (Four waves with columns of their own,
+// to registers.  Bound by the chain of a chunk: some 430 instructions a wave and tile of columns, 54 of them matrix ones, four phases that wait for each other.
+// 16 heads of 128 x 128 in bf16, 128 workgroups, operands asked for a chunk ahead: 2.16 us a chunk; k_delta_apart 1.85.  (Four waves with columns of their own,
 // operands through LDS: each goes through all of a chunk's 182 matrix and 1200 other instructions, 4.0 us a chunk, and a wave alone on its CU 4.5.)
 // Where there are more than 512 workgroups of 16 columns, 32 columns and two workgroups a CU that ask when they need it: 144 heads of 96 x 160 in fp16,
-// up to 700 tokens, 71 to 83 us; 16 columns 65 to 95, asking ahead 74 to 82.
+// up to 700 tokens, with what comes before 119 us; asking ahead 125, 16 columns 124, asking ahead 145.
 // AHEAD: operands are asked for a chunk ahead, for which a workgroup has a CU for itself, or when they are needed.  TILES: times 16 columns.
 template <int TYPE, int NK, bool AHEAD, int TILES>
 __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
@@ -550,8 +550,8 @@ __global__ void __launch_bounds__(256, TILES) k_delta_chain(ChunkArgs ca) {
 
 // Eight waves for 16 columns: four of them as in k_delta_chain, which have the state and make U, and four that make the results, a tile of tokens each, while
 // the others go on: these give the state's planes and U to them through LDS, so that Q S, A U and the results are out of the chunk's chain.  16 heads of
-// 128 x 128 in bf16, 8192 tokens: 224 us, 1.74 a chunk (k_delta_chain 252; keys and queries straight from where they lie, rows a few KB apart, 254).  A workgroup has a CU for itself; of more than two rounds of them k_delta_chain is quicker
-// (144 heads of 96 x 160 in fp16, 700 tokens: with what comes before 196 us, this 226).
+// 128 x 128 in bf16, 8192 tokens: 237 us, 1.85 a chunk (k_delta_chain 277; keys and queries straight from where they lie, rows a few KB apart, 30 more when tried).  A workgroup has a CU for itself; of more than two rounds of them k_delta_chain is quicker
+// (144 heads of 96 x 160 in fp16, up to 700 tokens: with what comes before 119 us, this 133).
 // AHEAD: chunks that operands are asked for ahead, what there are registers for.
 template <int TYPE, int NK, int AHEAD>
 __global__ void __launch_bounds__(512, 1) k_delta_apart(ChunkArgs ca) {

@@ -60,7 +60,7 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
     // waves side by side or on the same outputs, and how many tiles each: what the rounds of 256 workgroups come to, in units of 10 ns -- a wave's tile 40 a
     // part (fp32 57), its rows' operands 10 a part and plane, adding up and the results 65 a round, rows to LDS 1 for 400 bytes of operands, in every round
     // if they do not all stay there (fitted to 12 rows of fp32 x 40000 x 1000 and of bf16 x 4096 x 4096; of ten divisions each it
-    // takes the quickest, 14.8 us of up to 26.2 and 7.9 of up to 12.8)
+    // takes the quickest, 14.9 us of up to 26.0 and 7.7 of up to 12.1)
     const size_t of_part = planes * packed_plane(w.rows, 1);
     int64_t best = INT64_MAX;
     for (int each = 1; each <= (gated ? 1 : 2); each *= 2)
@@ -72,7 +72,7 @@ RowsPlan rows_plan(const lsh_packed_params* p, int32_t M, int32_t dtype, bool ga
             if (cost < best) { best = cost; w.streams = (int)streams; w.log_across = lg; w.sets = sets; }
         }
     const int deep = w.waves >> w.log_across;
-    // few workgroups that go through many parts: the parts are split (a launch more, some 3 us; 16 rows x 1000 x 16384 in fp16 25.9 -> 13.1 us)
+    // few workgroups that go through many parts: the parts are split (a launch more, some 3 us; 16 rows x 1000 x 16384 in fp16 24.5 -> 12.5 us)
     const int64_t turns = ceil_div(parts, deep), wide = w.sets * w.groups;
     w.split_parts = (int)parts;
     if (turns >= 6 && wide <= 128) w.split_parts = (int)(ceil_div(turns, std::min(turns / 2, 256 / wide)) * deep);
@@ -101,10 +101,10 @@ struct TilesLaunch {
     size_t room;               // the rows as operands
 };
 // From how many rows on k_packed_tiles is quicker than k_packed_rows goes by the matrix (us of the one and the other, in a graph).  Large ones: 16384 x 4096 gated,
-// bf16, 32 and 40 rows 30.6 and 31.6 against 33.0 and 52.6; fp32, 17, 32 and 33 rows 52 and 56 and 54 against 40 and 60 and 77; 40000 x 1000 in fp32, 17, 32 and 40 rows 39 and 41
-// and 44 against 21 and 37 and 47.  With few parts, where there is little to go through between the first load and the results, 16-bit rows never: 40000 x 1000 in
-// bf16, 40 and 128 rows 34 and 51 against 25 and 44 (40000 x 2048, 40 and 64 rows: 39 and 43 against 33 and 56).  Small ones do not pay for the rounds: 2048 x 2048 in bf16, 64 rows, 15.1 against 8.5.
-// But rows of many parts do not stay in LDS: 1000 x 16384 in fp16, 24, 32 and 96 rows 15.3 and 15.5 and 19.4 against 16.7 and 19.3 and 53; fp32, 20 and 40 rows 24 and 25 against 27 and 48.
+// bf16, 24, 32 and 40 rows 28.5 and 29.0 and 30.1 against 28.4 and 31.6 and 49.8; fp32, 17, 32 and 33 rows 51 and 54 and 52 against 39 and 58 and 74; 40000 x 1000 in fp32, 17, 32, 33 and 40 rows
+// 42 and 44 and 45 and 47 against 22 and 38 and 33 and 48.  With few parts, where there is little to go through between the first load and the results, 16-bit rows never: 40000 x 1000 in
+// bf16, 40 and 128 rows 33 and 50 against 24 and 44 (40000 x 2048, 40 and 64 rows: 38 and 42 against 31 and 54).  Small ones do not pay for the rounds: 2048 x 2048 in bf16, 64 rows, 14.9 against 8.0.
+// But rows of many parts do not stay in LDS: 1000 x 16384 in fp16, 24, 32 and 96 rows 15.3 and 15.6 and 19.2 against 16.9 and 19.1 and 53; fp32, 20 and 40 rows 24 and 24 against 26 and 47.
 bool takes_tiles(const lsh_packed_params* p, int32_t M, int32_t dtype, bool gated) {
     const int64_t parts = parts_of(p), work = tiles_of(p) * parts * (gated ? 2 : 1);
     return M > 128 || (M > kFewRows && work >= 16384 && (dtype == LSH_F32 || parts >= 16)) || (M > (dtype == LSH_F32 ? kFewRows : 24) && parts > 48);
@@ -204,8 +204,8 @@ int64_t delta_pairs(const lsh_delta_params* p) { return (int64_t)p->S * p->B * p
 bool delta_fits(const lsh_delta_params* p) {
     return delta_pairs(p) <= kMaxGrid && delta_pairs(p) * p->T <= (int64_t)1 << 26 && ceil_div(delta_pairs(p), 8) * 8 * (p->v_dim / 16) <= kMaxGrid;
 }
-// Rows of more tokens than this go in chunks of 64 (16 pairs of 128 x 128, bf16, 8 and 16 tokens: token after token 12.6 and 21.7 us, a chunk 17.5; 512 pairs,
-// 16 and 24 tokens: 45 and 61 against 55).
+// Rows of more tokens than this go in chunks of 64 (16 pairs of 128 x 128, bf16, 8 and 16 tokens: token after token 12.6 and 21.4 us, a chunk 17.4; 512 pairs,
+// 16 and 24 tokens: 44 and 59 against 55 and 57).
 constexpr int kLeastChunked = 12;
 int most_tokens(const lsh_delta_params* p) { return delta_pairs(p) * delta_slices(p) <= 256 ? kLeastChunked : 20; }
 

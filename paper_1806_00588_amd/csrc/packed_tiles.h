@@ -2,8 +2,8 @@
 //
 // k_packed_lay brings the rows into the order of the matrix operands (fp32: three planes of bf16), so that everything k_packed_tiles loads are
 // blocks of 1 KB, straight to LDS.  Rows of 16 bits, of which nothing has to be made before, come from where they lie if
-// 16 bytes of them are always neighbours and in place: 40 rows of fp16 x 1000 x 16384 20 -> 16 us, 2048 x 8192 x 8192 327 -> 300 in
-// a graph (launched one by one 290, both); 40 rows of bf16 x 8192 x 8192 29 -> 26.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
+// 16 bytes of them are always neighbours and in place: 40 rows of fp16 x 1000 x 16384 20 -> 16 us, 40 of bf16 x 8192 x 8192 29 -> 26,
+// 2048 x 8192 x 8192 291 -> 286 in a graph.  A workgroup of eight waves makes 128 rows, two waves side by side along them and four along the outputs.  Weights are
 // converted in registers, once by each of the two.  A group's products are summed up by themselves, then scaled and added to what came before, so
 // that nothing but fp32 sums rounds; that takes two accumulators, and 64 x 64 results of a wave are what has room for both in 256 registers.  Up to 64 rows: the two waves with the same
 // outputs take turns with the parts instead of sharing the rows, so that no weight is converted twice, and add up at the end.
