@@ -361,7 +361,7 @@ typedef struct {
 /* W [N, K] (fp32, bf16 or fp16; ld >= K) to codes.  For a group of weights w:
  *   without zeros   scale = max |w| / 7, code = 8 + round(w / scale)
  *   with zeros      lo = min(0, w), hi = max(0, w), scale = (hi - lo) / 15, zero = round(-lo / scale), code = zero + round(w / scale)
- * The scale is rounded to fp32 and then to its type, and used as rounded; the other quotients are exact, rounded to nearest even;
+ * The scale is rounded to fp32 and then to its type (in fp16 infinite from 65520 on, and such a group's weights no numbers), and used as rounded; the other quotients are exact, rounded to nearest even;
  * zeros and codes are cut to 0 .. 15, and of a group whose scale is 0 they are 8 (without zeros) or 0.  A group with a NaN or an infinity
  * gets a scale that is NaN, and codes 0.  Behind the last output or input codes, scales and zeros are set to 0.
  * LSH_ERR_UNSUPPORTED, as of lsh_packed_values: ceil(N / 16) * ceil(K / 128) > 2^26 - 4. */
